@@ -585,6 +585,91 @@ SAR_API sar_status sar_bn_bwd_apply_act(int64_t n, int32_t C, sar_dtype t, const
                                         const float *sum_gy_xhat, float inv_count, void *gx, void *stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Checkpoints of node arrays in 8 bits.  The paper saves memory by building the attention again in the backward pass
+ * (Sec. 3.3); what a layer then still keeps is its input or its aggregate, 2 or 4 bytes a value.  A checkpoint keeps
+ * 1 + 1/32 bytes a value and is read by the backward passes below in the place of the array (the paper has no counterpart).
+ * Format: codes int8 [n, C] and one byte s for every SAR_CKPT8_BLOCK = 32 consecutive columns of a row, scales uint8
+ * [n, (C + 31) / 32] (a row's last block may be shorter).  A code stands for code * 2^(s - 127); s = 0 stands for zeros and
+ * s = 255 for NaN, whatever the codes.
+ *   sar_ckpt8_pack    x [n, C] (type t) -> codes, scales.  With top the largest |x| of a block and E = floor(log2(top)):
+ *                     s = max(E - 6, -126) + 127 and code = x / 2^(s - 127) rounded to nearest, ties to even, within -127..127
+ *                     (only 127.5 and more is cut off); s = 0 where top is 0; s = 255 and codes 0 where the block holds
+ *                     anything infinite or NaN.  Every value comes back within 2^(s - 127), a 64th of top at most; the bytes
+ *                     are the same on every path and device.
+ *   sar_ckpt8_unpack  the values that the checkpoint stands for (exact in float32; in bf16 as well).
+ * x and codes as they may be: rows whose columns are a multiple of 8 (or 4) with x aligned to 16 bytes and codes to 8 (or 4)
+ * move several columns at a time.  n = 0 is allowed.  Errors: SAR_ERR_INVALID_ARG, SAR_ERR_UNSUPPORTED (C > 2^20),
+ * SAR_ERR_ALIGNMENT (x not aligned to its type).
+ * ------------------------------------------------------------------------------------------- */
+#define SAR_CKPT8_BLOCK 32
+SAR_API sar_status sar_ckpt8_pack(int64_t n, int32_t C, sar_dtype t, const void *x, int8_t *codes, uint8_t *scales, void *stream);
+SAR_API sar_status sar_ckpt8_unpack(int64_t n, int32_t C, sar_dtype t, const int8_t *codes, const uint8_t *scales, void *x,
+                                    void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Layer normalisation: every row of x [n, C] (type t) over its own C columns, so that, unlike batch normalisation, no
+ * statistics cross the workers.  xhat = (x - mean) * rstd with mean and rstd = 1 / sqrt(variance + eps) of the row (variance:
+ * the mean of the squared deviations), y = gamma * xhat + beta.  gamma, beta [C] float32 may be NULL (1 / 0).
+ *   sar_ln_fwd         y [n, C] (type t; may be x); mean, rstd [n] float32, each may be NULL.
+ *   sar_ln_bwd         with g = gamma * gy: gx = rstd * (g - <g, 1>/C - xhat * <g, xhat>/C) (may be gy or x), dgamma[c] = sum over
+ *                      the rows of gy * xhat, dbeta[c] = sum of gy ([C] float32, written; either may be NULL).
+ *   sar_ln_fwd_ckpt8   sar_ln_fwd that leaves the checkpoint of xhat as well (codes, scales as sar_ckpt8_pack would give
+ *                      them for xhat in float32): with rstd all that the backward pass needs.
+ *   sar_ln_bwd_ckpt8   sar_ln_bwd with xhat = what the checkpoint stands for (gx may be gy).
+ * Scratch of the backward calls where dgamma or dbeta is asked for: sar_ln_workspace_bytes(C).  Sums over the rows are formed in
+ * a fixed order (no atomics), block partials are added in float64.  n = 0 is allowed (dgamma, dbeta are written as zeros).
+ * Errors: SAR_ERR_INVALID_ARG (NULL arrays, eps < 0 or NaN), SAR_ERR_UNSUPPORTED (C > 2^20), SAR_ERR_ALIGNMENT (arrays not
+ * aligned to their type), SAR_ERR_WORKSPACE.
+ * ------------------------------------------------------------------------------------------- */
+SAR_API size_t sar_ln_workspace_bytes(int32_t C);
+SAR_API sar_status sar_ln_fwd(int64_t n, int32_t C, sar_dtype t, const void *x, const float *gamma, const float *beta, float eps,
+                              void *y, float *mean, float *rstd, void *stream);
+SAR_API sar_status sar_ln_bwd(int64_t n, int32_t C, sar_dtype t, const void *x, const float *mean, const float *rstd,
+                              const float *gamma, const void *gy, void *gx, float *dgamma, float *dbeta, void *workspace,
+                              size_t workspace_bytes, void *stream);
+SAR_API sar_status sar_ln_fwd_ckpt8(int64_t n, int32_t C, sar_dtype t, const void *x, const float *gamma, const float *beta, float eps,
+                                    void *y, float *rstd, int8_t *codes, uint8_t *scales, void *stream);
+SAR_API sar_status sar_ln_bwd_ckpt8(int64_t n, int32_t C, sar_dtype t, const int8_t *codes, const uint8_t *scales, const float *rstd,
+                                    const float *gamma, const void *gy, void *gx, float *dgamma, float *dbeta, void *workspace,
+                                    size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * The projection of nodes of several types, one weight matrix for each (Appendix A's W_r with the relation's rows lying
+ * together): rows offsets[g] .. offsets[g+1] of the node arrays belong to group g.  offsets: DEVICE, int64 [groups + 1],
+ * ascending, within 0 .. n; the sizes are read on the device alone, groups may be empty and of any length, and the calls can be
+ * captured once and replayed with other offsets; NULL with groups = 1 means all rows.  (Offsets that descend or leave the array are read as the largest one before
+ * them and as the array's ends.)  Weights [groups, d_in, d_out].
+ *   sar_linear_grouped             z[i] = h[i] W[g]                (bf16 out)
+ *   sar_linear_grouped_bwd_input   dh[i] = dz[i] W[g]^T            (bf16 out)
+ *   sar_linear_grouped_bwd_weight  dw[g] = sum over g's rows of h[i]^T dz[i]   (float32 out; zeros for an empty group; sums in
+ *                                  float32 over at most 512 rows on the tensor cores, those added rounding to nearest, in a
+ *                                  fixed order)
+ *   sar_linear_grouped_bwd_weight_ckpt8  the same with h = gamma * v + beta, v what the checkpoint (codes, scales) stands for;
+ *                                  gamma, beta [d_in] float32 may be NULL (1 / 0): the weight gradient behind sar_ln_fwd_ckpt8.
+ * Rows of no group (before offsets[0], from offsets[groups] on) take part in nothing; z and dh are left there as they were, or
+ * written as zeros with flags = SAR_GROUPED_ZERO_REST.  flag (DEVICE int, may be NULL) is set to 1 if a wait inside the kernel
+ * ran out of its bound (seconds), which leaves results unwritten; the library's tests check that it stays 0.
+ * Arrays are 16-byte aligned (codes 8), t must be SAR_BF16, d_in and d_out multiples of 8 up to 2^20, groups <= SAR_MAX_GROUPS,
+ * n < 2^31 - 128 (SAR_ERR_UNSUPPORTED otherwise).  Scratch of the weight calls: sar_linear_grouped_workspace_bytes.  n = 0 is
+ * allowed (dw is then written as zeros).
+ * ------------------------------------------------------------------------------------------- */
+#define SAR_MAX_GROUPS 1024
+#define SAR_GROUPED_ZERO_REST 1u
+SAR_API size_t sar_linear_grouped_workspace_bytes(int64_t n, int32_t groups, int32_t d_in, int32_t d_out);
+SAR_API sar_status sar_linear_grouped(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, sar_dtype t, const int64_t *offsets,
+                                      const void *h, const void *w, void *z, uint32_t flags, int32_t *flag, void *stream);
+SAR_API sar_status sar_linear_grouped_bwd_input(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, sar_dtype t,
+                                                const int64_t *offsets, const void *dz, const void *w, void *dh, uint32_t flags,
+                                                int32_t *flag, void *stream);
+SAR_API sar_status sar_linear_grouped_bwd_weight(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, sar_dtype t,
+                                                 const int64_t *offsets, const void *h, const void *dz, float *dw, int32_t *flag,
+                                                 void *workspace, size_t workspace_bytes, void *stream);
+SAR_API sar_status sar_linear_grouped_bwd_weight_ckpt8(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, sar_dtype t,
+                                                       const int64_t *offsets, const int8_t *codes, const uint8_t *scales,
+                                                       const float *gamma, const float *beta, const void *dz, float *dw,
+                                                       int32_t *flag, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Backward pass without any caller-provided scratch.  (The paper has no counterpart: this is a
  * convenience of this library.)
  *

@@ -552,3 +552,76 @@ def propagate(indptr, indices, x0, alpha: float, iters: int, src_scale=None, dst
     for _ in range(iters):
         x = (1.0 - alpha) * x0 + alpha * spmm_scaled(indptr, indices, x, src_scale, dst_scale)
     return x
+
+
+# --------------------------------------------------------------------------------------
+# layer normalisation, checkpoints in 8 bits, products by groups of rows: numpy float64
+# --------------------------------------------------------------------------------------
+
+def ln_forward(x, eps=1e-5, gamma=None, beta=None):
+    """(y, mean, rstd, xhat): every row over its own columns."""
+    x = np.asarray(x, np.float64)
+    mean = x.mean(axis=1)
+    d = x - mean[:, None]
+    rstd = 1.0 / np.sqrt((d * d).mean(axis=1) + eps)
+    xhat = d * rstd[:, None]
+    y = xhat if gamma is None else xhat * np.asarray(gamma, np.float64)
+    return y if beta is None else y + np.asarray(beta, np.float64), mean, rstd, xhat
+
+
+def ln_backward(xhat, rstd, gy, gamma=None):
+    """(gx, dgamma, dbeta) of y = gamma xhat + beta, from the normalised rows."""
+    xhat, gy = np.asarray(xhat, np.float64), np.asarray(gy, np.float64)
+    g = gy if gamma is None else gy * np.asarray(gamma, np.float64)
+    c = g.shape[1]
+    gx = np.asarray(rstd, np.float64)[:, None] * (g - g.sum(axis=1, keepdims=True) / c - xhat * (g * xhat).sum(axis=1, keepdims=True) / c)
+    return gx, (gy * xhat).sum(axis=0), gy.sum(axis=0)
+
+
+def ckpt8_pack(x):
+    """(codes int8 [n, C], scales uint8 [n, ceil(C / 32)]) of float32 values, block by block from the format's definition."""
+    x = np.asarray(x, np.float64)
+    n, c = x.shape
+    codes, scales = np.zeros((n, c), np.int8), np.zeros((n, (c + 31) // 32), np.uint8)
+    for b in range(scales.shape[1]):
+        v = x[:, 32 * b:32 * b + 32]
+        fine = np.isfinite(v).all(axis=1)
+        top = np.abs(np.where(fine[:, None], v, 0.0)).max(axis=1)
+        _, e = np.frexp(top)                       # top = m 2^e with m in [0.5, 1): floor(log2(top)) = e - 1
+        s = np.maximum(e - 1 - 6, -126)
+        code = np.clip(np.rint(np.ldexp(np.where(fine[:, None], v, 0.0), -s[:, None])), -127, 127)
+        codes[:, 32 * b:32 * b + 32] = np.where(top[:, None] > 0, code, 0)
+        scales[:, b] = np.where(fine, np.where(top > 0, s + 127, 0), 255)
+    return codes, scales
+
+
+def ckpt8_unpack(codes, scales):
+    """The values that a checkpoint stands for, float64."""
+    s = np.repeat(np.asarray(scales, np.int64), 32, axis=1)[:, :codes.shape[1]]
+    v = np.ldexp(np.asarray(codes, np.float64), s - 127)
+    return np.where(s == 0, 0.0, np.where(s == 255, np.nan, v))
+
+
+def group_rows(offsets, n):
+    """(first, end) of every group: offsets brought into 0 .. n and to the largest one before them."""
+    first = np.maximum.accumulate(np.clip(np.asarray(offsets, np.int64), 0, n))
+    return list(zip(first[:-1].tolist(), first[1:].tolist()))
+
+
+def grouped_linear(h, w, offsets, rest=0.0):
+    """z[i] = h[i] w[g] for the rows of group g; `rest` in the rows of no group."""
+    h, w = np.asarray(h, np.float64), np.asarray(w, np.float64)
+    z = np.full((h.shape[0], w.shape[2]), rest, np.float64)
+    for g, (a, b) in enumerate(group_rows(offsets, h.shape[0])):
+        z[a:b] = h[a:b] @ w[g]
+    return z
+
+
+def grouped_linear_bwd(h, w, offsets, dz, rest=0.0):
+    """(dh, dw) of grouped_linear for the upstream gradient dz."""
+    h, w, dz = (np.asarray(x, np.float64) for x in (h, w, dz))
+    dh, dw = np.full(h.shape, rest, np.float64), np.zeros(w.shape, np.float64)
+    for g, (a, b) in enumerate(group_rows(offsets, h.shape[0])):
+        dh[a:b] = dz[a:b] @ w[g].T
+        dw[g] = h[a:b].T @ dz[a:b]
+    return dh, dw

@@ -433,20 +433,127 @@ def rgcn_basis_backward(a: torch.Tensor, V: torch.Tensor, dW: torch.Tensor):
 # accumulate into one output.  The aggregation has no parameters ("case 1" of Sec. 3.2): the backward pass
 # needs no source features, only the graph.  Marshalling only.
 
-def sage_layer_forward(g: Graph, h: torch.Tensor, W: torch.Tensor, W_res: torch.Tensor, inv: Optional[torch.Tensor] = None):
-    """h [n, d_in], W and W_res [d_in, d_out] (bf16).  Returns (pre [n, d_out] before the activation, saved)."""
+def sage_layer_forward(g: Graph, h: torch.Tensor, W: torch.Tensor, W_res: torch.Tensor, inv: Optional[torch.Tensor] = None,
+                       checkpoint: bool = False):
+    """h [n, d_in], W and W_res [d_in, d_out] (bf16).  Returns (pre [n, d_out] before the activation, saved).
+    checkpoint=True keeps the aggregate for the backward pass as a Checkpoint8 (1.03 bytes a value in place of 2)."""
     if inv is None:
         inv = rgcn_inv_degrees([g])[0]
     parts, bounds = _pieces(g)
     pre, agg = B.native().sage_forward([p.addr for p in parts], bounds, h, W, W_res, inv)
-    return pre, (agg, inv)
+    return pre, (ckpt8_pack(agg) if checkpoint else agg, inv)
 
 
 def sage_layer_backward(g: Graph, h: torch.Tensor, W: torch.Tensor, W_res: torch.Tensor, saved, gpre: torch.Tensor):
     """Returns (dh [n, d_in], dW, dW_res [d_in, d_out] float32) for the upstream gradient gpre [n, d_out]."""
     agg, inv = saved
     parts, bounds = _pieces(g)
-    return B.native().sage_backward([p.addr for p in parts], bounds, h, W, W_res, agg, inv, gpre)
+    parts = [p.addr for p in parts]
+    if isinstance(agg, Checkpoint8):
+        return B.native().sage_backward_ckpt8(parts, bounds, h, W, W_res, agg.codes, agg.scales, inv, gpre)
+    return B.native().sage_backward(parts, bounds, h, W, W_res, agg, inv, gpre)
+
+
+# ----------------------------------------------------------------------------------------------
+# checkpoints of node arrays in 8 bits: what a layer keeps for its backward pass in 1 + 1/32 bytes a value.
+
+@dataclass
+class Checkpoint8:
+    """codes int8 [n, C] and scales uint8 [n, ceil(C / 32)]: 32 columns of a row share the scale 2^(s - 127)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    @property
+    def nbytes(self) -> int:
+        return self.codes.numel() + self.scales.numel()
+
+
+def ckpt8_pack(x: torch.Tensor) -> Checkpoint8:
+    """The checkpoint of x [n, C] (float32 or bf16).  Every value comes back within a 64th of the largest of its block."""
+    return Checkpoint8(*B.native().ckpt8_pack(x))
+
+
+def ckpt8_unpack(c: Checkpoint8, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """The values that the checkpoint stands for (exact in float32 and in bf16)."""
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"unsupported storage dtype {dtype}")
+    return B.native().ckpt8_unpack(c.codes, c.scales, dtype == torch.bfloat16)
+
+
+# ----------------------------------------------------------------------------------------------
+# layer normalisation of the rows.
+
+def ln_forward(x: torch.Tensor, eps: float = 1e-5, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+               checkpoint: bool = False):
+    """Returns (y, saved) for ln_backward; x is [n, C].  saved = (mean, rstd), with which the backward pass needs x again,
+    or with checkpoint=True (Checkpoint8 of the normalised rows, rstd), with which it needs no other node array."""
+    y, *saved = B.native().ln_forward(x, eps, gamma, beta, checkpoint)
+    return y, (Checkpoint8(*saved[:2]), saved[2]) if checkpoint else tuple(saved)
+
+
+def ln_backward(x: Optional[torch.Tensor], gy: torch.Tensor, saved, gamma: Optional[torch.Tensor] = None):
+    """Returns (gx, dgamma, dbeta); x may be None where saved holds a checkpoint."""
+    first, rstd = saved
+    if isinstance(first, Checkpoint8):
+        return B.native().ln_backward_ckpt8(first.codes, first.scales, gy, rstd, gamma)
+    return B.native().ln_backward(x, gy, first, rstd, gamma)
+
+
+# ----------------------------------------------------------------------------------------------
+# projection of nodes of several types: rows offsets[t] .. offsets[t+1] (int64, on the device) have type t and its matrix.
+
+def typed_linear_forward(h: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None):
+    """z[i] = h[i] W[type(i)]; h [n, d_in], W [types, d_in, d_out] (bf16).  Rows of no type (before offsets[0], from the last
+    offset on) are zeros, or left as they were in a given out."""
+    return B.native().typed_forward(h, W, offsets, out)
+
+
+def typed_linear_backward_input(gz: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None):
+    """dh[i] = gz[i] W[type(i)]^T; rows of no type as in typed_linear_forward."""
+    return B.native().typed_backward_input(gz, W, offsets, out)
+
+
+def typed_linear_backward_weight(h, offsets: torch.Tensor, gz: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+                                 beta: Optional[torch.Tensor] = None):
+    """dW [types, d_in, d_out] float32 = h^T gz over every type's rows.  h: the rows (bf16), or a Checkpoint8 of v with
+    h = gamma v + beta (what ln_forward(checkpoint=True) keeps; gamma and beta are taken with a checkpoint alone)."""
+    if isinstance(h, Checkpoint8):
+        return B.native().typed_backward_weight_ckpt8(h.codes, h.scales, offsets, gz, gamma, beta)
+    assert gamma is None and beta is None, "gamma and beta belong to a checkpoint"
+    return B.native().typed_backward_weight(h, offsets, gz)
+
+
+def typed_linear_backward(h, W: torch.Tensor, offsets: torch.Tensor, gz: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+                          beta: Optional[torch.Tensor] = None):
+    """Returns (dh, dW) for the upstream gradient gz [n, d_out]; h, gamma and beta as in typed_linear_backward_weight."""
+    return typed_linear_backward_input(gz, W, offsets), typed_linear_backward_weight(h, offsets, gz, gamma, beta)
+
+
+def typed_layer_forward(x: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+                        beta: Optional[torch.Tensor] = None, eps: float = 1e-5, checkpoint: bool = True):
+    """z = LN(x) W[type]: the normalised projection that feeds an aggregation over nodes of several types.  Returns (z, saved);
+    with checkpoint=True saved is 1.03 bytes a value and a float a row, otherwise x and LN(x) are kept."""
+    y, saved = ln_forward(x, eps, gamma, beta, checkpoint)
+    z = typed_linear_forward(y, W, offsets)
+    return z, saved if checkpoint else (x, y, *saved)
+
+
+def typed_layer_backward(W: torch.Tensor, offsets: torch.Tensor, saved, gz: torch.Tensor, gamma: Optional[torch.Tensor] = None,
+                         beta: Optional[torch.Tensor] = None):
+    """Returns (gx, dW, dgamma, dbeta) for the upstream gradient gz [n, d_out]."""
+    gy = typed_linear_backward_input(gz, W, offsets)
+    if isinstance(saved[0], Checkpoint8):
+        dW = typed_linear_backward_weight(saved[0], offsets, gz, gamma, beta)
+        gx, dgamma, dbeta = ln_backward(None, gy, saved, gamma)
+    else:
+        x, y, mean, rstd = saved
+        dW = typed_linear_backward_weight(y, offsets, gz)
+        gx, dgamma, dbeta = ln_backward(x, gy, (mean, rstd), gamma)
+    return gx, dW, dgamma, dbeta
 
 
 # ----------------------------------------------------------------------------------------------

@@ -21,6 +21,9 @@ SAR_OK = 0
 SAR_F32, SAR_BF16 = 0, 1
 SAR_FIRST, SAR_LAST, SAR_MEAN, SAR_KEEP_NUMERATOR, SAR_RELU_OUT, SAR_SAME_WORKSPACE = 1, 2, 4, 8, 16, 32
 SAR_MAX_PARTS = 64
+SAR_CKPT8_BLOCK = 32       # columns of a row that share a checkpoint's scale
+SAR_MAX_GROUPS = 1024
+SAR_GROUPED_ZERO_REST = 1
 
 EXPORTS = [
     "sar_status_string", "sar_built_for_sm", "sar_graph_workspace_bytes", "sar_csr_from_coo", "sar_csr_transpose",
@@ -38,6 +41,9 @@ EXPORTS = [
     "sar_bn_combine_sums", "sar_degree_order_workspace_bytes", "sar_degree_order", "sar_relabel", "sar_permute_rows", "sar_linear_project", "sar_linear_bwd_input_relu",
     "sar_graph_from_coo", "sar_plan_many_workspace_bytes", "sar_plan_count_many", "sar_plan_fill_many", "sar_gather_i64",
     "sar_propagate_workspace_bytes", "sar_propagate_workspace_bytes_at", "sar_propagate",
+    "sar_ln_workspace_bytes", "sar_ln_fwd", "sar_ln_bwd", "sar_ln_fwd_ckpt8", "sar_ln_bwd_ckpt8", "sar_ckpt8_pack", "sar_ckpt8_unpack",
+    "sar_linear_grouped_workspace_bytes", "sar_linear_grouped", "sar_linear_grouped_bwd_input", "sar_linear_grouped_bwd_weight",
+    "sar_linear_grouped_bwd_weight_ckpt8",
 ]
 
 
@@ -81,7 +87,8 @@ def lib() -> ctypes.CDLL:
         for name in ("sar_graph_workspace_bytes", "sar_gat_workspace_bytes", "sar_spmm_workspace_bytes",
                      "sar_gat_stack_arena_bytes", "sar_gat_bwd_noalloc_limit", "sar_gat_project_workspace_bytes",
                      "sar_bn_workspace_bytes", "sar_linear_workspace_bytes", "sar_gat_storing_workspace_bytes",
-                     "sar_degree_order_workspace_bytes", "sar_plan_many_workspace_bytes", "sar_propagate_workspace_bytes", "sar_propagate_workspace_bytes_at"):
+                     "sar_degree_order_workspace_bytes", "sar_plan_many_workspace_bytes", "sar_propagate_workspace_bytes", "sar_propagate_workspace_bytes_at",
+                     "sar_ln_workspace_bytes", "sar_linear_grouped_workspace_bytes"):
             getattr(L, name).restype = c_size_t
         _lib = L
     return _lib
@@ -827,6 +834,164 @@ def sar_round_to(acc: torch.Tensor, y: torch.Tensor) -> None:
     _check("sar_round_to", lib().sar_round_to(c_int64(acc.numel()), ctypes.c_int(_dtype(y)), _ptr(acc), _ptr(y),
                                               _stream()))
 
-
 def sar_relu_bwd(y: torch.Tensor, g: torch.Tensor) -> None:
     _check("sar_relu_bwd", lib().sar_relu_bwd(c_int64(y.numel()), ctypes.c_int(_dtype(y)), _ptr(y), _ptr(g), _stream()))
+
+
+# ----------------------------------------------------------------------------------------------
+# layer normalisation, checkpoints in 8 bits, products by groups of rows.  All tensors of a call lie on the current device.
+# ----------------------------------------------------------------------------------------------
+
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    dev = torch.cuda.current_device()
+    assert all(t is None or (t.is_cuda and t.device.index == dev) for t in tensors), "tensors on the current device expected"
+
+
+def _holds(t: Optional[torch.Tensor], dtype: torch.dtype, n: int, what: str) -> None:
+    assert t is None or (t.dtype == dtype and t.numel() >= n), f"{what}: expected {dtype} and at least {n} elements"
+
+
+def _checkpoint_holds(codes: torch.Tensor, scales: torch.Tensor, n: int, C: int) -> None:
+    _holds(codes, torch.int8, n * C, "codes")
+    _holds(scales, torch.uint8, n * ((C + SAR_CKPT8_BLOCK - 1) // SAR_CKPT8_BLOCK), "scales")
+
+
+def sar_ckpt8_pack(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor) -> None:
+    n, C = x.shape
+    _here(x, codes, scales)
+    _checkpoint_holds(codes, scales, n, C)
+    _check("sar_ckpt8_pack", lib().sar_ckpt8_pack(c_int64(n), c_int32(C), ctypes.c_int(_dtype(x)), _ptr(x), _ptr(codes),
+                                                  _ptr(scales), _stream()))
+
+
+def sar_ckpt8_unpack(codes: torch.Tensor, scales: torch.Tensor, x: torch.Tensor) -> None:
+    n, C = x.shape
+    _here(x, codes, scales)
+    _checkpoint_holds(codes, scales, n, C)
+    _check("sar_ckpt8_unpack", lib().sar_ckpt8_unpack(c_int64(n), c_int32(C), ctypes.c_int(_dtype(x)), _ptr(codes),
+                                                      _ptr(scales), _ptr(x), _stream()))
+
+
+def sar_ln_workspace_bytes(C: int) -> int:
+    return int(lib().sar_ln_workspace_bytes(c_int32(C)))
+
+
+def sar_ln_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float, y: torch.Tensor,
+               mean: Optional[torch.Tensor], rstd: Optional[torch.Tensor]) -> None:
+    n, C = x.shape
+    _here(x, gamma, beta, y, mean, rstd)
+    _holds(y, x.dtype, n * C, "y")
+    for t, k in ((gamma, C), (beta, C), (mean, n), (rstd, n)):
+        _holds(t, torch.float32, k, "gamma, beta, mean, rstd")
+    _check("sar_ln_fwd", lib().sar_ln_fwd(c_int64(n), c_int32(C), ctypes.c_int(_dtype(x)), _ptr(x), _ptr(gamma), _ptr(beta),
+                                          c_float(eps), _ptr(y), _ptr(mean), _ptr(rstd), _stream()))
+
+
+def sar_ln_fwd_ckpt8(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float, y: torch.Tensor,
+                     rstd: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor) -> None:
+    n, C = x.shape
+    _here(x, gamma, beta, y, rstd, codes, scales)
+    _holds(y, x.dtype, n * C, "y")
+    for t, k in ((gamma, C), (beta, C), (rstd, n)):
+        _holds(t, torch.float32, k, "gamma, beta, rstd")
+    _checkpoint_holds(codes, scales, n, C)
+    _check("sar_ln_fwd_ckpt8", lib().sar_ln_fwd_ckpt8(c_int64(n), c_int32(C), ctypes.c_int(_dtype(x)), _ptr(x), _ptr(gamma),
+                                                      _ptr(beta), c_float(eps), _ptr(y), _ptr(rstd), _ptr(codes), _ptr(scales),
+                                                      _stream()))
+
+
+def sar_ln_bwd(x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma: Optional[torch.Tensor], gy: torch.Tensor,
+               gx: torch.Tensor, dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor],
+               workspace: Optional[torch.Tensor]) -> None:
+    n, C = x.shape
+    _here(x, mean, rstd, gamma, gy, gx, dgamma, dbeta, workspace)
+    for t in (gy, gx):
+        _holds(t, x.dtype, n * C, "gy, gx")
+    for t, k in ((mean, n), (rstd, n), (gamma, C), (dgamma, C), (dbeta, C)):
+        _holds(t, torch.float32, k, "mean, rstd, gamma, dgamma, dbeta")
+    w, wb = _ws(workspace)
+    _check("sar_ln_bwd", lib().sar_ln_bwd(c_int64(n), c_int32(C), ctypes.c_int(_dtype(x)), _ptr(x), _ptr(mean), _ptr(rstd),
+                                          _ptr(gamma), _ptr(gy), _ptr(gx), _ptr(dgamma), _ptr(dbeta), w, wb, _stream()))
+
+
+def sar_ln_bwd_ckpt8(codes: torch.Tensor, scales: torch.Tensor, rstd: torch.Tensor, gamma: Optional[torch.Tensor],
+                     gy: torch.Tensor, gx: torch.Tensor, dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor],
+                     workspace: Optional[torch.Tensor]) -> None:
+    n, C = gy.shape
+    _here(codes, scales, rstd, gamma, gy, gx, dgamma, dbeta, workspace)
+    _holds(gx, gy.dtype, n * C, "gx")
+    for t, k in ((rstd, n), (gamma, C), (dgamma, C), (dbeta, C)):
+        _holds(t, torch.float32, k, "rstd, gamma, dgamma, dbeta")
+    _checkpoint_holds(codes, scales, n, C)
+    w, wb = _ws(workspace)
+    _check("sar_ln_bwd_ckpt8", lib().sar_ln_bwd_ckpt8(c_int64(n), c_int32(C), ctypes.c_int(_dtype(gy)), _ptr(codes),
+                                                      _ptr(scales), _ptr(rstd), _ptr(gamma), _ptr(gy), _ptr(gx), _ptr(dgamma),
+                                                      _ptr(dbeta), w, wb, _stream()))
+
+
+def sar_linear_grouped_workspace_bytes(n: int, groups: int, d_in: int, d_out: int) -> int:
+    return int(lib().sar_linear_grouped_workspace_bytes(c_int64(n), c_int32(groups), c_int32(d_in), c_int32(d_out)))
+
+
+def _group_offsets(offsets: Optional[torch.Tensor], groups: int) -> None:
+    assert offsets is not None or groups == 1, "offsets expected"
+    assert offsets is None or (offsets.dtype == torch.int64 and offsets.numel() == groups + 1), "int64 offsets [groups + 1] expected"
+
+
+def sar_linear_grouped(h: torch.Tensor, w: torch.Tensor, offsets: Optional[torch.Tensor], z: torch.Tensor, flags: int = 0,
+                       flag: Optional[torch.Tensor] = None) -> None:
+    """z[i] = h[i] w[g], rows offsets[g] .. offsets[g+1] being group g's (None: one group of all rows)."""
+    n, d_in = h.shape
+    groups, _, d_out = w.shape
+    _here(h, w, offsets, z, flag)
+    _group_offsets(offsets, groups)
+    assert w.shape[1] == d_in and w.dtype == h.dtype and (flag is None or flag.dtype == torch.int32)
+    _holds(z, h.dtype, n * d_out, "z")
+    _check("sar_linear_grouped", lib().sar_linear_grouped(c_int64(n), c_int32(groups), c_int32(d_in), c_int32(d_out),
+                                                          ctypes.c_int(_dtype(h)), _ptr(offsets), _ptr(h), _ptr(w), _ptr(z),
+                                                          c_uint32(flags), _ptr(flag), _stream()))
+
+
+def sar_linear_grouped_bwd_input(dz: torch.Tensor, w: torch.Tensor, offsets: Optional[torch.Tensor], dh: torch.Tensor,
+                                 flags: int = 0, flag: Optional[torch.Tensor] = None) -> None:
+    n, d_out = dz.shape
+    groups, d_in, _ = w.shape
+    _here(dz, w, offsets, dh, flag)
+    _group_offsets(offsets, groups)
+    assert w.shape[2] == d_out and w.dtype == dz.dtype and (flag is None or flag.dtype == torch.int32)
+    _holds(dh, dz.dtype, n * d_in, "dh")
+    _check("sar_linear_grouped_bwd_input", lib().sar_linear_grouped_bwd_input(
+        c_int64(n), c_int32(groups), c_int32(d_in), c_int32(d_out), ctypes.c_int(_dtype(dz)), _ptr(offsets), _ptr(dz), _ptr(w),
+        _ptr(dh), c_uint32(flags), _ptr(flag), _stream()))
+
+
+def sar_linear_grouped_bwd_weight(h: torch.Tensor, dz: torch.Tensor, offsets: Optional[torch.Tensor], dw: torch.Tensor,
+                                  workspace: torch.Tensor, flag: Optional[torch.Tensor] = None) -> None:
+    """dw [groups, d_in, d_out] float32."""
+    n, d_in = h.shape
+    groups, _, d_out = dw.shape
+    _here(h, dz, offsets, dw, workspace, flag)
+    _group_offsets(offsets, groups)
+    assert dw.shape[1] == d_in and dz.shape == (n, d_out) and dz.dtype == h.dtype and dw.dtype == torch.float32
+    assert flag is None or flag.dtype == torch.int32
+    ws, wb = _ws(workspace)
+    _check("sar_linear_grouped_bwd_weight", lib().sar_linear_grouped_bwd_weight(
+        c_int64(n), c_int32(groups), c_int32(d_in), c_int32(d_out), ctypes.c_int(_dtype(h)), _ptr(offsets), _ptr(h), _ptr(dz),
+        _ptr(dw), _ptr(flag), ws, wb, _stream()))
+
+
+def sar_linear_grouped_bwd_weight_ckpt8(codes: torch.Tensor, scales: torch.Tensor, gamma: Optional[torch.Tensor],
+                                        beta: Optional[torch.Tensor], dz: torch.Tensor, offsets: Optional[torch.Tensor],
+                                        dw: torch.Tensor, workspace: torch.Tensor, flag: Optional[torch.Tensor] = None) -> None:
+    n, d_out = dz.shape
+    groups, d_in, _ = dw.shape
+    _here(codes, scales, gamma, beta, dz, offsets, dw, workspace, flag)
+    _group_offsets(offsets, groups)
+    _checkpoint_holds(codes, scales, n, d_in)
+    assert dw.shape[2] == d_out and dw.dtype == torch.float32 and (flag is None or flag.dtype == torch.int32)
+    for t in (gamma, beta):
+        _holds(t, torch.float32, d_in, "gamma, beta")
+    ws, wb = _ws(workspace)
+    _check("sar_linear_grouped_bwd_weight_ckpt8", lib().sar_linear_grouped_bwd_weight_ckpt8(
+        c_int64(n), c_int32(groups), c_int32(d_in), c_int32(d_out), ctypes.c_int(_dtype(dz)), _ptr(offsets), _ptr(codes),
+        _ptr(scales), _ptr(gamma), _ptr(beta), _ptr(dz), _ptr(dw), _ptr(flag), ws, wb, _stream()))

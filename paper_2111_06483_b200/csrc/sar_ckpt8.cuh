@@ -1,0 +1,52 @@
+// Activation checkpoints in 8 bits (internal): how a block of 32 columns is held, shared by the kernels that write checkpoints
+// and those that read them.  The format is in include/sar.h.
+//
+// The scale of a block is a power of two.  So x / scale is exact, the code is the one rounding of the format, and every kernel
+// that packs the same values gives the same bytes; and code * scale has at most 7 significant bits, so it is exact in bf16 and
+// the tensor cores take it as it is.  What a free scale (max / 127) would gain is at most one bit: with E = floor(log2(max))
+// the step is 2^(E-6), max / 127 to max / 63.5.
+#pragma once
+
+#include "sar_common.cuh"
+
+namespace sar {
+
+constexpr int kCkptBlock = SAR_CKPT8_BLOCK;   // columns that share a scale
+
+// |x| as an unsigned key: larger magnitudes have larger keys, and NaN the largest (a maximum of floats would drop it)
+__device__ __forceinline__ unsigned ckpt_magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// the scale byte of a block whose largest magnitude has this key: 0 all zero, 255 anything infinite or NaN, else
+// max(E - 6, -126) + 127, which is 1 to 248
+__device__ __forceinline__ unsigned ckpt_scale_byte(unsigned top) {
+    const unsigned e = top >> 23;
+    return top == 0u ? 0u : e == 255u ? 255u : e > 7u ? e - 6u : 1u;
+}
+// 2^(127 - s); 0 for the bytes 0 and 255, whose codes are 0
+__device__ __forceinline__ float ckpt_inverse(unsigned s) { return (s == 0u || s == 255u) ? 0.f : __uint_as_float((254u - s) << 23); }
+// 2^(s - 127): 0 for the byte 0, NaN for 255
+__device__ __forceinline__ float ckpt_scale(unsigned s) { return __uint_as_float(s == 255u ? 0x7fc00000u : s << 23); }
+
+// The code of x in the low byte, to be masked where s is 255.  Added to 1.5 * 2^23 the quotient is rounded to the nearest whole
+// number, ties to even, and its two's complement is the sum's low byte (a conversion instruction runs at a quarter of the rate).
+__device__ __forceinline__ unsigned ckpt_code(float x, float inverse) {
+    return __float_as_uint(fminf(fmaxf(x * inverse, -127.f), 127.f) + 12582912.f);
+}
+__device__ __forceinline__ unsigned ckpt_code4(const float *x, float inverse, unsigned s) {
+    const unsigned lo = __byte_perm(ckpt_code(x[0], inverse), ckpt_code(x[1], inverse), 0x0040);
+    const unsigned hi = __byte_perm(ckpt_code(x[2], inverse), ckpt_code(x[3], inverse), 0x0040);
+    return s == 255u ? 0u : __byte_perm(lo, hi, 0x5410);
+}
+// code i of a word of four as a float: 2^23 + 128 + code is put together from its bytes, and the subtraction is exact
+__device__ __forceinline__ float ckpt_decode(unsigned flipped /* the word ^ 0x80808080 */, int i) {
+    return __uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7540u | i)) - 8388736.f;
+}
+template <int N>   // N codes (a multiple of 4, or 1) -> N values
+__device__ __forceinline__ void ckpt_decode_n(const unsigned (&w)[(N + 3) / 4], float scale, float *x) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = ckpt_decode(w[i / 4] ^ 0x80808080u, i & 3) * scale;
+}
+
+static inline int64_t ckpt_blocks(int32_t C) { return ((int64_t)C + kCkptBlock - 1) / kCkptBlock; }
+
+}  // namespace sar

@@ -1,0 +1,834 @@
+// Products of node rows with a matrix for each group of rows (contracts in include/sar.h): rows offsets[g] .. offsets[g+1] of an
+// array belong to group g (a node type), the groups' sizes are known on the device only.
+//   z = h W[g],  dh = dz W[g]^T       grouped_rows_kernel: tiles of 128 rows, each within one group
+//   dW[g] = h^T dz over g's rows      grouped_weight_kernel: the rows are cut into equal chunks; a chunk's part of every group
+//                                     that it meets is a partial result, and a second launch adds them up
+// bf16 operands, tensor-core products (tcgen05) with float32 sums in tensor memory, operands staged by tiled copies.
+#include "sar_ckpt8.cuh"
+#include "sar_dispatch.cuh"
+#include "sar_tc.cuh"
+
+namespace sar {
+
+constexpr int kTileRows = 128;      // rows of a product's tile: all lanes of tensor memory
+constexpr int kStep = 64;           // contraction per stage: 128 bytes of bf16
+constexpr int kPanel = 64 * 128;    // 64 rows of 128 bytes
+constexpr int kGroupsMax = SAR_MAX_GROUPS;
+
+sar_status tc_tensor_map(CUtensorMap *map, const void *base, int rank, const uint64_t *dims, const uint32_t *box) {
+    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static Encode encode = [] {   // the driver's function: the library links against the runtime alone
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+        if (e != cudaSuccess) (void)cudaGetLastError();
+        return e == cudaSuccess && found == cudaDriverEntryPointSuccess ? reinterpret_cast<Encode>(f) : nullptr;
+    }();
+    if (!encode) return SAR_ERR_CUDA;
+    cuuint64_t size[3], stride[2];
+    cuuint32_t tile[3], one[3] = {1, 1, 1};
+    uint64_t bytes = 2;
+    for (int i = 0; i < rank; ++i) {
+        size[i] = dims[i];
+        tile[i] = box[i];
+        bytes *= dims[i];
+        if (i + 1 < rank) stride[i] = bytes;
+    }
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(base), size, stride, tile, one,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SAR_OK : SAR_ERR_CUDA;
+}
+
+// First row of every group, and what precedes each group in tiles, by the block's first warp.  Offsets that lead backwards or out
+// of the array are brought to the last one seen and to the array's ends: whatever they hold, every access stays in bounds.
+struct GroupTable {
+    int first[kGroupsMax + 1];   // first[g] .. first[g + 1]: g's rows
+    int tiles[kGroupsMax + 1];   // tiles of 128 rows before group g
+};
+__device__ __forceinline__ void group_table(GroupTable &t, const int64_t *__restrict__ offsets, int G, int n) {
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x;
+        int top = 0, tiles = 0;
+        for (int g0 = 0; g0 <= G; g0 += 32) {
+            const int g = g0 + lane;
+            long long o = g > G ? 0 : offsets ? __ldg(reinterpret_cast<const long long *>(offsets) + g) : g ? n : 0;
+            int lo = o < 0 ? 0 : o > n ? n : (int)o;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, lo, d);
+                if (lane >= d) lo = max(lo, y);
+            }
+            lo = max(lo, top);
+            const int before = __shfl_up_sync(0xffffffffu, lo, 1);
+            // tiles of the group that ends here
+            int k = g == 0 || g > G ? 0 : (lo - (lane ? before : top) + kTileRows - 1) / kTileRows;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, k, d);
+                if (lane >= d) k += y;
+            }
+            k += tiles;
+            if (g <= G) {
+                t.first[g] = lo;
+                t.tiles[g] = k;
+            }
+            top = __shfl_sync(0xffffffffu, lo, 31);
+            tiles = __shfl_sync(0xffffffffu, k, 31);
+        }
+    }
+    __syncthreads();
+}
+
+// ---- rows: z = h W[g], dh = dz W[g]^T ----------------------------------------------------------------------------------------
+//
+// One block per SM.  A block keeps one slice of columns (all of them, up to 256) and walks a run of row tiles, so that
+// the weights of a group, which are read again for every tile, are loaded once and stay in shared memory as long as the tiles
+// belong to the group; each row is read once per slice and written once.  Warp 0 issues the copies, warp 1 the products into
+// one of two accumulators, warps 2 to 5 round the other one to bf16 and store it.  A tile that ends inside a group's last rows
+// reads the next group's along with them (a row's result depends on no other row) and stores its own rows alone.
+struct RowsArgs {
+    CUtensorMap a, w, d;
+    const int64_t *offsets;
+    __nv_bfloat16 *out;
+    int *flag;
+    int n, G, K, N;
+    int cols;        // columns per slice (a multiple of 64 up to 256)
+    int slices;      // slices of columns
+    int steps;       // of 64 along the contraction
+    int stages;      // of the ring
+    int slots;       // sets of weights in shared memory; 0: they pass through the ring with the rows
+    int zero_rest;   // rows of no group are written as zeros
+};
+constexpr int kRowsThreads = 192;
+constexpr int kStoreBuf = 32 * 128;   // a warp's 32 rows of 64 columns
+constexpr int kSlotsMax = 4, kStagesMax = 8;
+struct RowsShared {
+    alignas(8) uint64_t full[kStagesMax], empty[kStagesMax], w_full[kSlotsMax], w_empty[kSlotsMax], acc_full[2], acc_empty[2];
+    uint32_t tmem;
+    int failed;
+    GroupTable table;
+};
+
+template <bool WT>
+__global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __grid_constant__ RowsArgs p) {
+    after_predecessor();
+    extern __shared__ uint8_t dyn[];
+    RowsShared &sh = *reinterpret_cast<RowsShared *>(dyn);
+    const int panels = p.cols / 64, w_step = panels * kPanel;
+    const uint32_t w_set = (uint32_t)p.steps * w_step;
+    const uint32_t base = (smem_addr(dyn) + (uint32_t)sizeof(RowsShared) + 1023u) & ~1023u;
+    const uint32_t stage_bytes = kTileRows * 128 + (p.slots ? 0 : w_step);
+    const uint32_t ring = base + 8 * kStoreBuf, weights = ring + p.stages * stage_bytes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int *failed = &sh.failed;
+
+    group_table(sh.table, p.offsets, p.G, p.n);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < p.stages; ++i) bar_init(smem_addr(&sh.full[i]), 1), bar_init(smem_addr(&sh.empty[i]), 1);
+        for (int i = 0; i < kSlotsMax; ++i) bar_init(smem_addr(&sh.w_full[i]), 1), bar_init(smem_addr(&sh.w_empty[i]), 1);
+        for (int i = 0; i < 2; ++i) bar_init(smem_addr(&sh.acc_full[i]), 1), bar_init(smem_addr(&sh.acc_empty[i]), 4);
+        sh.failed = 0;
+        bar_init_fence();
+    }
+    if (warp == 1) tmem_alloc(smem_addr(&sh.tmem));
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    const uint32_t tmem = sh.tmem;
+
+    // this block's slice and its run of tiles
+    const int teams = gridDim.x / p.slices, team = blockIdx.x / p.slices;   // the grid is teams x slices
+    const int n0 = (blockIdx.x % p.slices) * p.cols, cols = min(p.cols, p.N - n0);
+    const int total = sh.table.tiles[p.G];
+    const int t0 = (int)((long long)total * team / teams), t1 = (int)((long long)total * (team + 1) / teams);
+    int g0 = 0;
+    {
+        int hi = p.G;   // the group of tile t0: tiles[g0] <= t0 < tiles[g0 + 1]
+        while (hi - g0 > 1) {
+            const int mid = (g0 + hi) / 2;
+            (sh.table.tiles[mid] <= t0 ? g0 : hi) = mid;
+        }
+    }
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t use = 0, set = 0;   // stages and sets of weights used so far
+            int g = g0, held = -1;
+            bool ok = true;
+            for (int t = t0; ok && t < t1; ++t) {
+                while (t >= sh.table.tiles[g + 1]) ++g;
+                if (p.slots && g != held) {
+                    const uint32_t slot = set % p.slots, bar = smem_addr(&sh.w_full[slot]);
+                    ok = set < (uint32_t)p.slots || bar_wait(smem_addr(&sh.w_empty[slot]), (set / p.slots + 1) & 1, failed);
+                    if (!ok) break;
+                    bar_expect(bar, w_set);
+                    for (int k = 0; k < p.steps; ++k) {
+                        const uint32_t at = weights + slot * w_set + k * w_step;
+                        if (WT) tile_load_3d(at, &p.w, k * kStep, n0, g, bar);
+                        else
+                            for (int c = 0; c < panels; ++c) tile_load_3d(at + c * kPanel, &p.w, n0 + c * 64, k * kStep, g, bar);
+                    }
+                    held = g;
+                    ++set;
+                }
+                const int row = sh.table.first[g] + (t - sh.table.tiles[g]) * kTileRows;
+                for (int k = 0; k < p.steps; ++k, ++use) {
+                    const uint32_t s = use % p.stages, bar = smem_addr(&sh.full[s]), at = ring + s * stage_bytes;
+                    ok = use < (uint32_t)p.stages || bar_wait(smem_addr(&sh.empty[s]), (use / p.stages + 1) & 1, failed);
+                    if (!ok) break;
+                    bar_expect(bar, stage_bytes);
+                    tile_load_2d(at, &p.a, k * kStep, row, bar);
+                    if (!p.slots) {
+                        const uint32_t b = at + kTileRows * 128;
+                        if (WT) tile_load_3d(b, &p.w, k * kStep, n0, g, bar);
+                        else
+                            for (int c = 0; c < panels; ++c) tile_load_3d(b + c * kPanel, &p.w, n0 + c * 64, k * kStep, g, bar);
+                    }
+                }
+            }
+            if (!ok) {   // the copies in flight end before the block does
+                for (uint32_t s = 0; s < (uint32_t)p.stages && s < use; ++s) bar_drain(smem_addr(&sh.full[s]), ((use - 1 - s) / p.stages) & 1);
+                for (uint32_t s = 0; s < (uint32_t)p.slots && s < set; ++s) bar_drain(smem_addr(&sh.w_full[s]), ((set - 1 - s) / p.slots) & 1);
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t instr = tc_instr((cols + 15) & ~15, false, !WT);
+            uint32_t use = 0, set = 0;
+            int g = g0, held = -1;
+            bool ok = true;
+            for (int t = t0; ok && t < t1; ++t) {
+                const uint32_t i = t - t0, buf = i & 1;
+                while (t >= sh.table.tiles[g + 1]) ++g;
+                if (p.slots && g != held) {
+                    if (held >= 0) tc_commit(smem_addr(&sh.w_empty[(set - 1) % p.slots]));   // all products with the last set
+                    ok = bar_wait(smem_addr(&sh.w_full[set % p.slots]), (set / p.slots) & 1, failed);
+                    if (!ok) break;
+                    held = g;
+                    ++set;
+                }
+                ok = i < 2 || bar_wait(smem_addr(&sh.acc_empty[buf]), (i / 2 + 1) & 1, failed);
+                if (!ok) break;
+                tc_after_sync();
+                const uint32_t wset = weights + (p.slots ? (set - 1) % p.slots * w_set : 0);
+                for (int k = 0; k < p.steps; ++k, ++use) {
+                    const uint32_t s = use % p.stages, at = ring + s * stage_bytes;
+                    ok = bar_wait(smem_addr(&sh.full[s]), (use / p.stages) & 1, failed);
+                    if (!ok) break;
+                    tc_after_sync();
+                    const uint32_t b = p.slots ? wset + k * w_step : at + kTileRows * 128;
+                    const int left = (min(kStep, p.K - k * kStep) + 15) / 16;   // copies fill what lies beyond K with zeros
+                    for (int j = 0; j < left; ++j) {
+                        const uint64_t da = tc_operand(at + j * 32, 16, 1024);
+                        const uint64_t db = WT ? tc_operand(b + j * 32, 16, 1024) : tc_operand(b + j * 2048, kPanel, 1024);
+                        tc_mma(tmem + buf * 256, da, db, instr, k > 0 || j > 0);
+                    }
+                    tc_commit(smem_addr(&sh.empty[s]));
+                }
+                if (ok) tc_commit(smem_addr(&sh.acc_full[buf]));
+            }
+        }
+    } else {
+        const int quad = warp & 3;   // the lanes of tensor memory that this warp may read
+        const uint32_t stage = base + (warp - 2) * 2 * kStoreBuf;
+        uint32_t stored = 0;
+        int g = g0;
+        for (int t = t0; t < t1; ++t) {
+            const uint32_t i = t - t0, buf = i & 1;
+            while (t >= sh.table.tiles[g + 1]) ++g;
+            if (!bar_wait(smem_addr(&sh.acc_full[buf]), (i / 2) & 1, failed)) break;
+            tc_after_sync();
+            const int row = sh.table.first[g] + (t - sh.table.tiles[g]) * kTileRows + quad * 32;
+            const int rows = min(32, sh.table.first[g + 1] - row);   // may be <= 0
+            for (int c = 0; c < cols; c += 64, ++stored) {
+                const uint32_t at = stage + (stored & 1) * kStoreBuf;
+                store_wait_read<1>();   // lane 0's copy out of this buffer, two ago
+                __syncwarp();
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float x[32];
+                    tmem_load32(tmem + buf * 256 + c + h * 32 + ((uint32_t)(quad * 32) << 16), x);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float(&v)[8] = *reinterpret_cast<const float(*)[8]>(x + q * 8);
+                        const uint4 r = Elem<__nv_bfloat16>::pack(v);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + lane * 128 + (((h * 4 + q) ^ (lane & 7)) << 4)), "r"(r.x),
+                                     "r"(r.y), "r"(r.z), "r"(r.w)
+                                     : "memory");
+                    }
+                }
+                if (rows == 32) {
+                    async_proxy_fence();
+                    __syncwarp();
+                    if (lane == 0) tile_store_2d(&p.d, n0 + c, row, at);
+                } else {   // the group ends here: its rows alone
+                    __syncwarp();
+                    const int chunk = lane & 7;
+                    if (n0 + c + chunk * 8 < p.N)
+                        for (int r = lane >> 3; r < rows; r += 4) {
+                            uint4 v;
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at + r * 128 + ((chunk ^ (r & 7)) << 4)));
+                            *reinterpret_cast<uint4 *>(p.out + (long long)(row + r) * p.N + n0 + c + chunk * 8) = v;
+                        }
+                    __syncwarp();
+                }
+                if (lane == 0) store_commit();
+            }
+            tc_before_sync();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&sh.acc_empty[buf]));
+        }
+        if (p.zero_rest) {
+            const int head = sh.table.first[0], tail = sh.table.first[p.G], rest = head + p.n - tail;
+            for (int i = team * 4 + warp - 2; i < rest; i += teams * 4) {
+                const int r = i < head ? i : tail + i - head;
+                for (int c = lane * 8; c < cols; c += 256) *reinterpret_cast<uint4 *>(p.out + (long long)r * p.N + n0 + c) = make_uint4(0, 0, 0, 0);
+            }
+        }
+        if (lane == 0) store_wait_all();
+    }
+    __syncwarp();
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    if (warp == 1) tmem_free(tmem);
+    if (threadIdx.x == 0 && sh.failed && p.flag) *p.flag = 1;
+}
+
+// ---- weights: dW[g] = h^T dz ---------------------------------------------------------------------------------------------------
+//
+// The contraction runs along the rows, so both operands are read as they lie (contraction along a tile's rows).  A block owns a
+// tile of 128 x (up to) 256 of dW and a chunk of rows; the blocks of a chunk's tiles run side by side and share its rows in L2.
+//
+// The tensor cores add to a float32 sum by cutting off what does not fit: every step of 16 rows takes up to one unit of the last
+// place towards zero, and 16,384 rows in one sum are 2e-5 to 3e-5 off (256 rows 2e-7, 1,024 rows 1e-6, 65,536 rows 8e-5 and
+// more).  So a sum runs over kRunRows rows at most, in one of two accumulators, and eight warps add it, rounding to nearest, to
+// sums that they hold in registers while the next run goes on.
+//
+// With a checkpoint the same warps make the first operand: codes times scale, exact in bf16, written where a copy would have put
+// them.  Its rows stand for gamma v + beta, and  (gamma v + beta)^T dz = gamma (v^T dz) + beta (column sums of dz):  gamma and
+// beta enter in float32 after the product instead of rounding every value, and the column sums are taken from the tiles of dz
+// that are in shared memory anyway.
+constexpr int kRunRows = 512;
+struct WeightArgs {
+    CUtensorMap h, dz;
+    const int64_t *offsets;
+    const int8_t *codes;
+    const uint8_t *scales;
+    float *part;     // [chunks + G][d_in][d_out]: chunk c's part of group g in record c + g (along the way both only grow)
+    float *sums;     // [chunks + G][2][d_out]: sums of dz's columns over either half of the rows, or null
+    int *flag;
+    int n, G, d_in, d_out, nb;
+    int cols;        // of a tile (a multiple of 64 up to 256)
+    int m_tiles, n_tiles;
+    int chunk_rows;  // a multiple of 64
+    int stages;
+};
+constexpr int kWorkers = 8;
+constexpr int kWeightThreads = 64 + kWorkers * 32;
+struct WeightShared {
+    alignas(8) uint64_t full[kStagesMax], empty[kStagesMax], made[kStagesMax], mended, acc_full[2], acc_empty[2];
+    uint32_t tmem;
+    int failed;
+    GroupTable table;
+};
+
+template <bool CK>
+__global__ void __launch_bounds__(kWeightThreads, 1) grouped_weight_kernel(const __grid_constant__ WeightArgs p) {
+    after_predecessor();
+    extern __shared__ uint8_t dyn[];
+    WeightShared &sh = *reinterpret_cast<WeightShared *>(dyn);
+    const uint32_t ring = (smem_addr(dyn) + (uint32_t)sizeof(WeightShared) + 1023u) & ~1023u;
+    const int panels = p.cols / 64;
+    const uint32_t stage_bytes = (2 + panels) * kPanel;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int *failed = &sh.failed;
+
+    group_table(sh.table, p.offsets, p.G, p.n);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < p.stages; ++i) bar_init(smem_addr(&sh.full[i]), 1), bar_init(smem_addr(&sh.empty[i]), 1), bar_init(smem_addr(&sh.made[i]), kWorkers);
+        for (int i = 0; i < 2; ++i) bar_init(smem_addr(&sh.acc_full[i]), 1), bar_init(smem_addr(&sh.acc_empty[i]), kWorkers);
+        bar_init(smem_addr(&sh.mended), kWorkers);
+        sh.failed = 0;
+        bar_init_fence();
+    }
+    if (warp == 1) tmem_alloc(smem_addr(&sh.tmem));
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    const uint32_t tmem = sh.tmem;
+
+    const int tiles = p.m_tiles * p.n_tiles;
+    const int chunk = blockIdx.x / tiles, tile = blockIdx.x % tiles;
+    const int m0 = tile / p.n_tiles * 128, n0 = tile % p.n_tiles * p.cols, cols = min(p.cols, p.d_out - n0);
+    const int h_panels = p.d_in - m0 > 64 ? 2 : 1;
+    const int chunk0 = (int)min((long long)p.n, (long long)chunk * p.chunk_rows), chunk1 = (int)min((long long)p.n, (long long)chunk0 + p.chunk_rows);
+    int g0 = 0;   // the first group that ends behind the chunk's start
+    for (int hi = p.G; g0 < hi;) {
+        const int mid = (g0 + hi) / 2;
+        if (sh.table.first[mid + 1] > chunk0) hi = mid;
+        else g0 = mid + 1;
+    }
+    // every role walks the same segments: group g's rows within the chunk
+    const auto segment = [&](int g, int &lo, int &hi) {
+        lo = max(chunk0, sh.table.first[g]);
+        hi = min(chunk1, sh.table.first[g + 1]);
+        return lo < hi;
+    };
+    const auto more = [&](int g) { return g < p.G && sh.table.first[g] < chunk1; };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t use = 0;
+            bool ok = true;
+            for (int g = g0; ok && more(g); ++g) {
+                int lo, hi;
+                if (!segment(g, lo, hi)) continue;
+                for (int r = lo; r < hi; r += kStep, ++use) {
+                    const uint32_t s = use % p.stages, bar = smem_addr(&sh.full[s]), at = ring + s * stage_bytes;
+                    ok = use < (uint32_t)p.stages || bar_wait(smem_addr(&sh.empty[s]), (use / p.stages + 1) & 1, failed);
+                    if (!ok) break;
+                    bar_expect(bar, ((CK ? 0 : h_panels) + panels) * kPanel);
+                    if (!CK)
+                        for (int c = 0; c < h_panels; ++c) tile_load_2d(at + c * kPanel, &p.h, m0 + c * 64, r, bar);
+                    for (int c = 0; c < panels; ++c) tile_load_2d(at + (2 + c) * kPanel, &p.dz, n0 + c * 64, r, bar);
+                }
+            }
+            if (!ok)
+                for (uint32_t s = 0; s < (uint32_t)p.stages && s < use; ++s) bar_drain(smem_addr(&sh.full[s]), ((use - 1 - s) / p.stages) & 1);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t instr = tc_instr((cols + 15) & ~15, true, true);
+            uint32_t use = 0, run = 0, mends = 0;
+            bool ok = true;
+            for (int g = g0; ok && more(g); ++g) {
+                int lo, hi;
+                if (!segment(g, lo, hi)) continue;
+                for (int r0 = lo; ok && r0 < hi; r0 += kRunRows, ++run) {
+                    const uint32_t buf = run & 1;
+                    ok = run < 2 || bar_wait(smem_addr(&sh.acc_empty[buf]), (run / 2 + 1) & 1, failed);
+                    if (!ok) break;
+                    tc_after_sync();
+                    const int r1 = min(hi, r0 + kRunRows);
+                    for (int r = r0; r < r1; r += kStep, ++use) {
+                        const uint32_t s = use % p.stages, at = ring + s * stage_bytes;
+                        const int rows = min(kStep, hi - r);
+                        ok = bar_wait(smem_addr(&sh.full[s]), (use / p.stages) & 1, failed);
+                        if (CK) ok = ok && bar_wait(smem_addr(&sh.made[s]), (use / p.stages) & 1, failed);
+                        else if (rows % 16) ok = ok && bar_wait(smem_addr(&sh.mended), mends++ & 1, failed);
+                        if (!ok) break;
+                        tc_after_sync();
+                        for (int j = 0; j < (rows + 15) / 16; ++j)
+                            tc_mma(tmem + buf * 256, tc_operand(at + j * 2048, kPanel, 1024), tc_operand(at + 2 * kPanel + j * 2048, kPanel, 1024), instr, r > r0 || j > 0);
+                        tc_commit(smem_addr(&sh.empty[s]));
+                    }
+                    if (ok) tc_commit(smem_addr(&sh.acc_full[buf]));
+                }
+            }
+        }
+    } else {
+        const int w = warp - 2, quad = warp & 3, half = w / 4, me = threadIdx.x - 64;
+        float sum[4][32];   // columns (2 c + half) 32 .. + 31 of row m0 + 32 quad + lane of dW
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 32; ++e) sum[c][e] = 0.f;
+        const bool want_sums = CK && p.sums && m0 == 0;
+        float2 cs = make_float2(0.f, 0.f);   // columns 2 (me % 128) and the next of dz, over every other 32 rows of a step
+        uint32_t use = 0, run = 0;
+        bool ok = true;
+        // the part of h: 8 columns of four rows a step and thread
+        const int hc = me & 15, hr = me >> 4;
+        uint2 code[4];
+        unsigned scale[4];
+        const bool h_cols = m0 + hc * 8 < p.d_in;
+        const auto ask = [&](int r, int rows) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = hr + 16 * i;
+                code[i] = make_uint2(0u, 0u);
+                scale[i] = 0;
+                if (h_cols && row < rows) {
+                    code[i] = __ldg(reinterpret_cast<const uint2 *>(p.codes + (long long)(r + row) * p.d_in + m0 + hc * 8));
+                    scale[i] = __ldg(p.scales + (long long)(r + row) * p.nb + (m0 + hc * 8) / kCkptBlock);
+                }
+            }
+        };
+        // add the accumulator of a finished run to the sums
+        const auto drain = [&](uint32_t of) {
+            const uint32_t buf = of & 1;
+            if (!bar_wait(smem_addr(&sh.acc_full[buf]), (of / 2) & 1, failed)) return false;
+            tc_after_sync();
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int col = (2 * c + half) * 32;
+                if (col < cols) {
+                    float x[32];
+                    tmem_load32(tmem + buf * 256 + col + ((uint32_t)(quad * 32) << 16), x);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) sum[c][e] += x[e];
+                }
+            }
+            tc_before_sync();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&sh.acc_empty[buf]));
+            return true;
+        };
+        // rows from `rows` to the next multiple of 16 of a tile take part in the products: they are another group's
+        const auto clear = [&](uint32_t at, int rows, int from, int to) {
+            const int rest = (16 - rows % 16) % 16;
+            for (int i = me; i < rest * 8 * (to - from); i += kWorkers * 32) {
+                const uint32_t where = at + (from + i / (rest * 8)) * kPanel + (rows + i / 8 % rest) * 128 + (i % 8) * 16;
+                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};\n" ::"r"(where), "r"(0) : "memory");
+            }
+        };
+        for (int g = g0; ok && more(g); ++g) {
+            int lo, hi;
+            if (!segment(g, lo, hi)) continue;
+            if (CK) ask(lo, min(kStep, hi - lo));
+            bool pending = false;   // the run before this one is still to be added
+            for (int r0 = lo; ok && r0 < hi; r0 += kRunRows, ++run) {
+                const int r1 = min(hi, r0 + kRunRows);
+                float2 cr = make_float2(0.f, 0.f);
+                for (int r = r0; r < r1; r += kStep, ++use) {
+                    const uint32_t s = use % p.stages, at = ring + s * stage_bytes;
+                    const int rows = min(kStep, hi - r);
+                    if (CK) {
+                        ok = use < (uint32_t)p.stages || bar_wait(smem_addr(&sh.empty[s]), (use / p.stages + 1) & 1, failed);
+                        if (!ok) break;
+                        if (h_cols) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int row = hr + 16 * i;
+                                const unsigned word[2] = {code[i].x, code[i].y};
+                                float v[8];
+                                ckpt_decode_n<8>(word, ckpt_scale(scale[i]), v);
+                                const uint4 b = Elem<__nv_bfloat16>::pack(v);
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + (hc >> 3) * kPanel + row * 128 + (((hc & 7) ^ (row & 7)) << 4)),
+                                             "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                                             : "memory");
+                            }
+                        }
+                        if (r + kStep < hi) ask(r + kStep, min(kStep, hi - r - kStep));
+                        if (rows % 16 || want_sums) {
+                            ok = bar_wait(smem_addr(&sh.full[s]), (use / p.stages) & 1, failed);
+                            if (!ok) break;
+                        }
+                        if (want_sums) {
+                            const int pair = me & 127;
+                            if (pair * 2 < cols) {
+                                const uint32_t col = at + (2 + pair / 32) * kPanel + (pair & 3) * 4;
+                                for (int q = (me >> 7) * 32; q < min((me >> 7) * 32 + 32, rows); ++q) {
+                                    uint32_t v;
+                                    asm volatile("ld.shared.b32 %0, [%1];\n" : "=r"(v) : "r"(col + q * 128 + (((pair >> 2 & 7) ^ (q & 7)) << 4)));
+                                    cr.x += __uint_as_float(v << 16);
+                                    cr.y += __uint_as_float(v & 0xffff0000u);
+                                }
+                            }
+                        }
+                        if (rows % 16) clear(at, rows, 2, 2 + panels);   // h's rows are zeros already
+                        async_proxy_fence();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_addr(&sh.made[s]));
+                    } else if (rows % 16) {
+                        ok = bar_wait(smem_addr(&sh.full[s]), (use / p.stages) & 1, failed);
+                        if (!ok) break;
+                        clear(at, rows, 0, h_panels);
+                        clear(at, rows, 2, 2 + panels);
+                        async_proxy_fence();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(smem_addr(&sh.mended));
+                    }
+                    if (pending) {   // the products of this run's first step go on meanwhile
+                        ok = drain(run - 1);
+                        pending = false;
+                        if (!ok) break;
+                    }
+                }
+                cs.x += cr.x;
+                cs.y += cr.y;
+                pending = true;
+            }
+            ok = ok && drain(run - 1);
+            if (!ok) break;
+            const long long record = chunk + g;
+            const int m = m0 + quad * 32 + lane;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int col = (2 * c + half) * 32;
+                if (m < p.d_in) {
+                    float4 *out = reinterpret_cast<float4 *>(p.part + (record * p.d_in + m) * p.d_out + n0 + col);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (col + q * 4 < cols) out[q] = make_float4(sum[c][4 * q], sum[c][4 * q + 1], sum[c][4 * q + 2], sum[c][4 * q + 3]);
+                }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) sum[c][e] = 0.f;
+            }
+            if (want_sums && (me & 127) * 2 < cols)   // one of the two halves of every step's rows
+                *reinterpret_cast<float2 *>(p.sums + (record * 2 + (me >> 7)) * p.d_out + n0 + (me & 127) * 2) = cs;
+            cs = make_float2(0.f, 0.f);
+        }
+    }
+    __syncwarp();
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    if (warp == 1) tmem_free(tmem);
+    if (threadIdx.x == 0 && sh.failed && p.flag) *p.flag = 1;
+}
+
+// dW[g] = the sum of group g's records in the order of the chunks, times gamma, plus beta times the sums of dz's columns
+__global__ void __launch_bounds__(256) grouped_weight_reduce_kernel(const int64_t *__restrict__ offsets, int G, long long n, int d_in, int d_out, int chunk_rows,
+                                                                    const float *__restrict__ part, const float *__restrict__ sums,
+                                                                    const float *__restrict__ gamma, const float *__restrict__ beta, float *__restrict__ dw) {
+    after_predecessor();
+    const int g = blockIdx.y;
+    __shared__ int from, count;
+    __shared__ float4 red[4][64];
+    if (threadIdx.x < 32 && threadIdx.y == 0) {
+        // the group's rows as group_table reads them: the largest offset so far
+        long long lo = 0, hi;
+        for (int j = threadIdx.x; offsets && j <= g; j += 32) lo = max(lo, (long long)offsets[j]);
+        for (int d = 16; d > 0; d >>= 1) lo = max(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+        lo = min(lo, n);
+        hi = offsets ? min(max(lo, (long long)offsets[g + 1]), n) : n;
+        if (threadIdx.x == 0) {
+            from = (int)(lo / chunk_rows);
+            count = hi > lo ? (int)((hi - 1) / chunk_rows) - from + 1 : 0;
+        }
+    }
+    __syncthreads();
+    const long long size = (long long)d_in * d_out, x = (blockIdx.x * 64ll + threadIdx.x) * 4;   // 4 outputs a thread, 4 shares of the records
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f), col = acc;
+    if (x < size) {
+        const int c = (int)(x % d_out);
+#pragma unroll 4
+        for (int s = threadIdx.y; s < count; s += 4) {
+            const float4 v = *reinterpret_cast<const float4 *>(part + (from + s + g) * size + x);
+            acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
+            if (sums) {
+                const float4 *u = reinterpret_cast<const float4 *>(sums + (long long)(from + s + g) * 2 * d_out + c), a = u[0], b = u[d_out / 4];
+                col.x += a.x + b.x, col.y += a.y + b.y, col.z += a.z + b.z, col.w += a.w + b.w;
+            }
+        }
+        if (gamma) {
+            const float k = __ldg(gamma + x / d_out);
+            acc.x *= k, acc.y *= k, acc.z *= k, acc.w *= k;
+        }
+        if (sums) {
+            const float k = __ldg(beta + x / d_out);
+            acc.x = fmaf(k, col.x, acc.x), acc.y = fmaf(k, col.y, acc.y), acc.z = fmaf(k, col.z, acc.z), acc.w = fmaf(k, col.w, acc.w);
+        }
+    }
+    red[threadIdx.y][threadIdx.x] = acc;
+    __syncthreads();
+    if (threadIdx.y == 0 && x < size) {
+        const float4 b = red[1][threadIdx.x], c = red[2][threadIdx.x], d = red[3][threadIdx.x];
+        *reinterpret_cast<float4 *>(dw + g * size + x) =
+            make_float4((acc.x + b.x) + (c.x + d.x), (acc.y + b.y) + (c.y + d.y), (acc.z + b.z) + (c.z + d.z), (acc.w + b.w) + (c.w + d.w));
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------------
+constexpr int kSms = 148;
+constexpr size_t kSharedMost = 227 * 1024;
+
+static sar_status grouped_check(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, sar_dtype t, const int64_t *offsets, std::initializer_list<const void *> ps) {
+    if (n < 0 || groups < 1 || d_in < 1 || d_out < 1 || (!offsets && groups > 1)) return SAR_ERR_INVALID_ARG;
+    if (t != SAR_BF16) return t == SAR_F32 ? SAR_ERR_UNSUPPORTED : SAR_ERR_INVALID_ARG;
+    if (n > INT32_MAX - kTileRows || groups > kGroupsMax || d_in % 8 || d_out % 8 || d_in > (1 << 20) || d_out > (1 << 20)) return SAR_ERR_UNSUPPORTED;
+    if (offsets && !sar_aligned(offsets, 8)) return SAR_ERR_ALIGNMENT;
+    for (const void *p : ps)
+        if (!p) return SAR_ERR_INVALID_ARG;
+        else if (!sar_aligned(p, 16)) return SAR_ERR_ALIGNMENT;
+    return SAR_OK;
+}
+
+static int round_up_int(int x, int a) { return (x + a - 1) / a * a; }
+
+// out [n, N] = rows [n, K] times W[g] (WT: its transpose)
+template <bool WT>
+static sar_status grouped_rows(int64_t n, int32_t groups, int K, int N, const int64_t *offsets, const void *rows, const void *w, void *out, uint32_t flags,
+                               int32_t *flag, cudaStream_t st, const char *name) {
+    RowsArgs p{};
+    p.offsets = offsets;
+    p.out = static_cast<__nv_bfloat16 *>(out);
+    p.flag = flag;
+    p.n = (int)n;
+    p.G = groups;
+    p.K = K;
+    p.N = N;
+    p.zero_rest = (flags & SAR_GROUPED_ZERO_REST) != 0;
+    p.steps = (K + kStep - 1) / kStep;
+    // Weights stay in shared memory where 64 K of their elements are a slice of at least 128 columns: every row tile
+    // then costs the loads of its rows alone.  Longer contractions take both operands through the ring in slices of 256 columns.
+    const int widest = p.steps <= 4 ? 256 : p.steps <= 8 ? 128 : 256;
+    p.slices = (N + widest - 1) / widest;
+    p.cols = round_up_int((N + p.slices - 1) / p.slices, 64);
+    p.slices = (N + p.cols - 1) / p.cols;
+    const size_t w_step = (size_t)(p.cols / 64) * kPanel, w_set = p.steps * w_step, fixed = sizeof(RowsShared) + 1024 + 8 * kStoreBuf, row_stage = kTileRows * 128;
+    size_t smem;
+    if (p.steps <= 8) {
+        const size_t room = kSharedMost - fixed;
+        p.slots = (int)((room - 3 * row_stage) / w_set);
+        p.slots = p.slots > kSlotsMax ? kSlotsMax : p.slots;
+        p.stages = (int)((room - p.slots * w_set) / row_stage);
+        p.stages = p.stages > kStagesMax ? kStagesMax : p.stages;
+        smem = fixed + p.slots * w_set + p.stages * row_stage;
+    } else {
+        p.slots = 0;
+        p.stages = (int)((kSharedMost - fixed) / (row_stage + w_step));
+        p.stages = p.stages > kStagesMax ? kStagesMax : p.stages;
+        smem = fixed + p.stages * (row_stage + w_step);
+    }
+    const uint64_t a_dims[2] = {(uint64_t)K, (uint64_t)n}, d_dims[2] = {(uint64_t)N, (uint64_t)n};
+    const uint64_t w_dims[3] = {(uint64_t)(WT ? K : N), (uint64_t)(WT ? N : K), (uint64_t)groups};
+    const uint32_t a_box[2] = {64, kTileRows}, d_box[2] = {64, 32}, w_box[3] = {64, (uint32_t)(WT ? p.cols : kStep), 1};
+    SAR_TRY(tc_tensor_map(&p.a, rows, 2, a_dims, a_box));
+    SAR_TRY(tc_tensor_map(&p.w, w, 3, w_dims, w_box));
+    SAR_TRY(tc_tensor_map(&p.d, out, 2, d_dims, d_box));
+    const long long most_tiles = (n + kTileRows - 1) / kTileRows + groups;   // what the groups' ragged ends can add
+    long long teams = kSms / p.slices;
+    teams = teams < 1 ? 1 : teams > most_tiles ? most_tiles : teams;
+    auto kern = grouped_rows_kernel<WT>;
+    SAR_TRY(ensure_smem(kern, smem));
+    SAR_LAUNCH(name, st, launch_if(n * (K + N) <= kOverlapElems, kern, (unsigned)(teams * p.slices), kRowsThreads, smem, st, p));
+    return sar_after_launch();
+}
+
+struct WeightPlan {
+    int cols, m_tiles, n_tiles, chunks, chunk_rows, stages;
+    size_t smem, part_bytes, sum_bytes;
+};
+static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out) {
+    WeightPlan w;
+    w.n_tiles = (d_out + 255) / 256;
+    w.cols = round_up_int((d_out + w.n_tiles - 1) / w.n_tiles, 64);
+    w.n_tiles = (d_out + w.cols - 1) / w.cols;
+    w.m_tiles = (d_in + 127) / 128;
+    const int tiles = w.m_tiles * w.n_tiles;
+    long long chunks = kSms / tiles;
+    if (chunks > n / 256) chunks = n / 256;   // rows below which a chunk is not worth its record
+    if (chunks < 1) chunks = 1;
+    long long rows = (n + chunks - 1) / chunks;
+    rows = (rows + kStep - 1) / kStep * kStep;
+    w.chunk_rows = (int)rows;
+    w.chunks = (int)((n + rows - 1) / rows);
+    const size_t fixed = sizeof(WeightShared) + 1024, stage = (size_t)(2 + w.cols / 64) * kPanel;
+    w.stages = (int)((kSharedMost - fixed) / stage);
+    w.stages = w.stages > kStagesMax ? kStagesMax : w.stages;
+    w.smem = fixed + w.stages * stage;
+    w.part_bytes = sar_round_up((size_t)(w.chunks + groups) * d_in * d_out * 4, 256);
+    w.sum_bytes = sar_round_up((size_t)(w.chunks + groups) * 2 * d_out * 4, 256);
+    return w;
+}
+
+static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, const int64_t *offsets, const void *h, const int8_t *codes,
+                                 const uint8_t *scales, const float *gamma, const float *beta, const void *dz, float *dw, int32_t *flag,
+                                 void *workspace, size_t workspace_bytes, cudaStream_t st) {
+    const WeightPlan w = weight_plan(n, groups, d_in, d_out);
+    if (!workspace || !sar_aligned(workspace, 16) || workspace_bytes < w.part_bytes + w.sum_bytes) return SAR_ERR_WORKSPACE;
+    WeightArgs p{};
+    p.offsets = offsets;
+    p.codes = codes;
+    p.scales = scales;
+    p.part = static_cast<float *>(workspace);
+    p.sums = beta ? reinterpret_cast<float *>(static_cast<char *>(workspace) + w.part_bytes) : nullptr;
+    p.flag = flag;
+    p.n = (int)n;
+    p.G = groups;
+    p.d_in = d_in;
+    p.d_out = d_out;
+    p.nb = (int)ckpt_blocks(d_in);
+    p.cols = w.cols;
+    p.m_tiles = w.m_tiles;
+    p.n_tiles = w.n_tiles;
+    p.chunk_rows = w.chunk_rows;
+    p.stages = w.stages;
+    const uint32_t box[2] = {64, kStep};
+    const uint64_t h_dims[2] = {(uint64_t)d_in, (uint64_t)n}, z_dims[2] = {(uint64_t)d_out, (uint64_t)n};
+    if (h) SAR_TRY(tc_tensor_map(&p.h, h, 2, h_dims, box));
+    SAR_TRY(tc_tensor_map(&p.dz, dz, 2, z_dims, box));
+    const bool overlap = n * (d_in + d_out) <= kOverlapElems;
+    const unsigned blocks = (unsigned)(w.chunks * w.m_tiles * w.n_tiles);
+    if (h) {
+        SAR_TRY(ensure_smem(grouped_weight_kernel<false>, w.smem));
+        SAR_LAUNCH("linear_grouped_bwd_weight", st, launch_if(overlap, grouped_weight_kernel<false>, blocks, kWeightThreads, w.smem, st, p));
+    } else {
+        SAR_TRY(ensure_smem(grouped_weight_kernel<true>, w.smem));
+        SAR_LAUNCH("linear_grouped_bwd_weight_ckpt8", st, launch_if(overlap, grouped_weight_kernel<true>, blocks, kWeightThreads, w.smem, st, p));
+    }
+    SAR_TRY(sar_after_launch());
+    const long long quads = (long long)d_in * d_out / 4;
+    SAR_LAUNCH("linear_grouped_bwd_weight_reduce", st,
+               launch(grouped_weight_reduce_kernel, dim3((unsigned)((quads + 63) / 64), (unsigned)groups), dim3(64, 4), 0, st, offsets, (int)groups, (long long)n,
+                      (int)d_in, (int)d_out, w.chunk_rows, p.part, p.sums, gamma, beta, dw));
+    return sar_after_launch();
+}
+
+}  // namespace sar
+
+using namespace sar;
+
+extern "C" {
+
+sar_status sar_linear_grouped(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, sar_dtype t, const int64_t *offsets, const void *h,
+                              const void *w, void *z, uint32_t flags, int32_t *flag, void *stream) {
+    if (flags & ~(uint32_t)SAR_GROUPED_ZERO_REST) return SAR_ERR_INVALID_ARG;
+    if (n == 0) return grouped_check(n, groups, d_in, d_out, t, offsets, {});
+    SAR_TRY(grouped_check(n, groups, d_in, d_out, t, offsets, {h, w, z}));
+    return grouped_rows<false>(n, groups, d_in, d_out, offsets, h, w, z, flags, flag, static_cast<cudaStream_t>(stream), "linear_grouped");
+}
+
+sar_status sar_linear_grouped_bwd_input(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, sar_dtype t, const int64_t *offsets,
+                                        const void *dz, const void *w, void *dh, uint32_t flags, int32_t *flag, void *stream) {
+    if (flags & ~(uint32_t)SAR_GROUPED_ZERO_REST) return SAR_ERR_INVALID_ARG;
+    if (n == 0) return grouped_check(n, groups, d_in, d_out, t, offsets, {});
+    SAR_TRY(grouped_check(n, groups, d_in, d_out, t, offsets, {dz, w, dh}));
+    return grouped_rows<true>(n, groups, d_out, d_in, offsets, dz, w, dh, flags, flag, static_cast<cudaStream_t>(stream), "linear_grouped_bwd_input");
+}
+
+size_t sar_linear_grouped_workspace_bytes(int64_t n, int32_t groups, int32_t d_in, int32_t d_out) {
+    if (n < 1 || n > INT32_MAX || groups < 1 || d_in < 1 || d_out < 1) return 0;
+    const WeightPlan w = weight_plan(n, groups, d_in, d_out);
+    return w.part_bytes + w.sum_bytes + 256;
+}
+
+static sar_status grouped_zero(int32_t groups, int32_t d_in, int32_t d_out, float *dw, void *stream) {
+    if (!dw) return SAR_ERR_INVALID_ARG;
+    SAR_CUDA_TRY(cudaMemsetAsync(dw, 0, (size_t)groups * d_in * d_out * 4, static_cast<cudaStream_t>(stream)));
+    return SAR_OK;
+}
+
+sar_status sar_linear_grouped_bwd_weight(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, sar_dtype t, const int64_t *offsets,
+                                         const void *h, const void *dz, float *dw, int32_t *flag, void *workspace, size_t workspace_bytes,
+                                         void *stream) {
+    if (n == 0) {
+        SAR_TRY(grouped_check(n, groups, d_in, d_out, t, offsets, {}));
+        return grouped_zero(groups, d_in, d_out, dw, stream);
+    }
+    SAR_TRY(grouped_check(n, groups, d_in, d_out, t, offsets, {h, dz, dw}));
+    return grouped_weight(n, groups, d_in, d_out, offsets, h, nullptr, nullptr, nullptr, nullptr, dz, dw, flag, workspace, workspace_bytes,
+                          static_cast<cudaStream_t>(stream));
+}
+
+sar_status sar_linear_grouped_bwd_weight_ckpt8(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, sar_dtype t, const int64_t *offsets,
+                                               const int8_t *codes, const uint8_t *scales, const float *gamma, const float *beta,
+                                               const void *dz, float *dw, int32_t *flag, void *workspace, size_t workspace_bytes,
+                                               void *stream) {
+    if (n == 0) {
+        SAR_TRY(grouped_check(n, groups, d_in, d_out, t, offsets, {}));
+        return grouped_zero(groups, d_in, d_out, dw, stream);
+    }
+    SAR_TRY(grouped_check(n, groups, d_in, d_out, t, offsets, {dz, dw}));
+    if (!codes || !scales) return SAR_ERR_INVALID_ARG;
+    if (!sar_aligned(codes, 8)) return SAR_ERR_ALIGNMENT;
+    SAR_TRY(check_elem_align({gamma, beta}, 4));
+    return grouped_weight(n, groups, d_in, d_out, offsets, nullptr, codes, scales, gamma, beta, dz, dw, flag, workspace, workspace_bytes,
+                          static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

@@ -10,6 +10,7 @@
 
 #include <ATen/cuda/CUDAContext.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <dlfcn.h>
 
 #include <vector>
@@ -26,7 +27,10 @@ namespace {
     X(sar_linear_bwd_input) X(sar_linear_bwd_input_relu) X(sar_linear_bwd_weight) X(sar_bn_workspace_bytes)            \
     X(sar_bn_stats) X(sar_bn_rstd) X(sar_bn_apply) X(sar_bn_bwd_stats) X(sar_bn_bwd_apply)                             \
     X(sar_graph_workspace_bytes) X(sar_graph_from_coo) X(sar_csr_split_indptr) X(sar_csr_split_indices)                \
-    X(sar_csc_slice_indptr) X(sar_plan_many_workspace_bytes) X(sar_plan_count_many) X(sar_plan_fill_many) X(sar_gather_i64)
+    X(sar_csc_slice_indptr) X(sar_plan_many_workspace_bytes) X(sar_plan_count_many) X(sar_plan_fill_many) X(sar_gather_i64) \
+    X(sar_ln_workspace_bytes) X(sar_ln_fwd) X(sar_ln_bwd) X(sar_ln_fwd_ckpt8) X(sar_ln_bwd_ckpt8) X(sar_ckpt8_pack) X(sar_ckpt8_unpack) \
+    X(sar_linear_grouped_workspace_bytes) X(sar_linear_grouped) X(sar_linear_grouped_bwd_input) X(sar_linear_grouped_bwd_weight) \
+    X(sar_linear_grouped_bwd_weight_ckpt8)
 
 struct Lib {
 #define X(f) decltype(&::f) f;
@@ -126,6 +130,10 @@ void require_like(const at::Tensor &t, const at::Tensor &like, int64_t n) {
 void require_matrix(const at::Tensor &t, const at::Tensor &like, int64_t rows, int64_t cols) {
     require(t.dim() == 2 && t.size(0) == rows && t.size(1) == cols, "a weight matrix of another shape");
     require(t.scalar_type() == like.scalar_type(), "tensors of one storage type expected");
+}
+void require_checkpoint(const at::Tensor &codes, const at::Tensor &scales, int64_t n, int64_t C) {
+    require(codes.scalar_type() == at::kChar && codes.numel() >= n * C, "expected int8 codes, one per value");
+    require(scales.scalar_type() == at::kByte && scales.numel() >= n * ((C + SAR_CKPT8_BLOCK - 1) / SAR_CKPT8_BLOCK), "expected a uint8 scale per block");
 }
 void require_rows(const at::Tensor &t, int64_t n) { require(t.dim() > 0 && t.size(0) >= n, "a node array has fewer rows than the graph"); }
 // ... of every piece of a graph: its destinations and its slice of the sources
@@ -543,20 +551,30 @@ PyObject *sage_forward(Args &a) {   // parts, bounds, h, W, W_res, inv
     return tuple(pre, agg);
 }
 
-PyObject *sage_backward(Args &a) {   // parts, bounds, h, W, W_res, agg, inv, gpre
+// The weight gradient's operand is the aggregate, or its checkpoint (codes and scales) where the forward call kept that.
+PyObject *sage_backward_of(Args &a, bool ckpt) {
     const auto parts = a.integers(), bounds = a.integers();
-    const at::Tensor &h = a.tensor(), &W = a.tensor(), &Wr = a.tensor(), &agg = a.tensor(), &inv = a.tensor(), &g = a.tensor();
+    const at::Tensor &h = a.tensor(), &W = a.tensor(), &Wr = a.tensor(), &agg = a.tensor();
+    const at::Tensor scales = ckpt ? a.tensor() : at::Tensor();
+    const at::Tensor &inv = a.tensor(), &g = a.tensor();
     const int64_t n = h.size(0);
     const int32_t d_in = (int32_t)h.size(1), d_out = (int32_t)W.size(1);
     const sar_dtype t = code(h);
     require_pieces(parts, bounds, n, n);
     require_matrix(W, h, d_in, d_out);
     require_matrix(Wr, h, d_in, d_out);
-    require_like(agg, h, n * d_in);
+    if (ckpt) require_checkpoint(agg, scales, n, d_in);
+    else require_like(agg, h, n * d_in);
     require_like(g, h, n * d_out);
     const at::Tensor ws = bytes(L.sar_linear_workspace_bytes(n, d_in, d_out), h);
     const at::Tensor dW = empty({d_in, d_out}, at::kFloat, h), dWr = empty({d_in, d_out}, at::kFloat, h);
-    SAR(sar_linear_bwd_weight, n, d_in, d_out, t, ptr(agg), ptr(g), f32m(dW), ptrm(ws), ws.nbytes(), stream());
+    if (ckpt) {
+        const at::Tensor gws = bytes(L.sar_linear_grouped_workspace_bytes(n, 1, d_in, d_out), h);
+        SAR(sar_linear_grouped_bwd_weight_ckpt8, n, 1, d_in, d_out, t, nullptr, static_cast<const int8_t *>(ptr(agg)), static_cast<const uint8_t *>(ptr(scales)),
+            nullptr, nullptr, ptr(g), f32m(dW), nullptr, ptrm(gws), gws.nbytes(), stream());
+    } else {
+        SAR(sar_linear_bwd_weight, n, d_in, d_out, t, ptr(agg), ptr(g), f32m(dW), ptrm(ws), ws.nbytes(), stream());
+    }
     SAR(sar_linear_bwd_weight, n, d_in, d_out, t, ptr(h), ptr(g), f32m(dWr), ptrm(ws), ws.nbytes(), stream());
     const at::Tensor dh = empty(h.sizes(), h.scalar_type(), h), dagg = empty(h.sizes(), h.scalar_type(), h);
     SAR(sar_linear_bwd_input, n, d_in, d_out, t, ptr(g), ptr(Wr), ptrm(dh), ptrm(ws), ws.nbytes(), stream());   // the residual path
@@ -565,6 +583,8 @@ PyObject *sage_backward(Args &a) {   // parts, bounds, h, W, W_res, agg, inv, gp
     scatter(parts, bounds, dagg, inv, dh, 0u, sws);   // plus what every out-edge hands back
     return tuple(dh, dW, dWr);
 }
+PyObject *sage_backward(Args &a) { return sage_backward_of(a, false); }         // parts, bounds, h, W, W_res, agg, inv, gpre
+PyObject *sage_backward_ckpt8(Args &a) { return sage_backward_of(a, true); }    // parts, bounds, h, W, W_res, codes, scales, inv, gpre
 
 // ---- batch normalisation (one worker) ------------------------------------------------------------------------------------
 PyObject *bn_forward(Args &a) {   // x, eps, gamma, beta
@@ -597,6 +617,158 @@ PyObject *bn_backward(Args &a) {   // x, gy, mean, rstd, gamma, count
     SAR(sar_bn_bwd_stats, n, C, t, ptr(x), pm, pr, ptr(gy), f32m(s0), f32m(s1), ptrm(ws), ws.nbytes(), stream());
     SAR(sar_bn_bwd_apply, n, C, t, ptr(x), pm, pr, pg, ptr(gy), f32(s0, C), f32(s1, C), (float)(1.0 / (double)(count > 1 ? count : 1)), ptrm(gx), stream());
     return tuple(gx, s1, s0);
+}
+
+// ---- layer normalisation, checkpoints, products by node type ---------------------------------------------------------------
+// Runs on its tensors' device, whichever is the current one, on that device's current stream.
+struct On {
+    c10::cuda::CUDAGuard guard;
+    template <typename... Ts>
+    explicit On(const at::Tensor &x, const Ts &...ts) : guard(x.device()) {
+        require(((!ts.defined() || ts.device() == x.device()) && ...), "tensors on one device expected");
+    }
+};
+struct Matrix {
+    int64_t n;
+    int32_t C;
+    sar_dtype t;
+    explicit Matrix(const at::Tensor &x) {
+        if (x.dim() != 2) fail(PyExc_ValueError, "expected [n, columns]");
+        n = x.size(0);
+        C = (int32_t)x.size(1);
+        t = code(x);
+    }
+};
+at::Tensor scales_for(int64_t n, int64_t C, const at::Tensor &like) { return empty({n, (C + SAR_CKPT8_BLOCK - 1) / SAR_CKPT8_BLOCK}, at::kByte, like); }
+int8_t *i8m(const at::Tensor &t) { return static_cast<int8_t *>(t.mutable_data_ptr()); }
+uint8_t *u8m(const at::Tensor &t) { return static_cast<uint8_t *>(t.mutable_data_ptr()); }
+const int8_t *i8(const at::Tensor &t) { return static_cast<const int8_t *>(t.const_data_ptr()); }
+const uint8_t *u8(const at::Tensor &t) { return static_cast<const uint8_t *>(t.const_data_ptr()); }
+
+PyObject *ckpt8_pack(Args &a) {   // x -> codes, scales
+    const at::Tensor &x = a.tensor();
+    const On on(x);
+    const Matrix m(x);
+    const at::Tensor codes = empty(x.sizes(), at::kChar, x), scales = scales_for(m.n, m.C, x);
+    SAR(sar_ckpt8_pack, m.n, m.C, m.t, ptr(x), i8m(codes), u8m(scales), stream());
+    return tuple(codes, scales);
+}
+
+PyObject *ckpt8_unpack(Args &a) {   // codes, scales, bf16?
+    const at::Tensor &codes = a.tensor(), &scales = a.tensor();
+    const bool bf16 = a.flag();
+    const On on(codes, scales);
+    require(codes.dim() == 2, "expected codes [n, columns]");
+    const int64_t n = codes.size(0), C = codes.size(1);
+    require_checkpoint(codes, scales, n, C);
+    const at::Tensor x = empty(codes.sizes(), bf16 ? at::kBFloat16 : at::kFloat, codes);
+    SAR(sar_ckpt8_unpack, n, (int32_t)C, bf16 ? SAR_BF16 : SAR_F32, i8(codes), u8(scales), ptrm(x), stream());
+    return wrap(x);
+}
+
+PyObject *ln_forward(Args &a) {   // x, eps, gamma, beta, checkpoint -> y, mean, rstd or y, codes, scales, rstd
+    const at::Tensor &x = a.tensor();
+    const double eps = a.real();
+    const at::Tensor gamma = a.optional(), beta = a.optional();
+    const bool checkpoint = a.flag();
+    const On on(x, gamma, beta);
+    const Matrix m(x);
+    const float *pg = f32(gamma, m.C), *pb = f32(beta, m.C);
+    const at::Tensor y = empty(x.sizes(), x.scalar_type(), x), rstd = empty({m.n}, at::kFloat, x);
+    if (checkpoint) {
+        const at::Tensor codes = empty(x.sizes(), at::kChar, x), scales = scales_for(m.n, m.C, x);
+        SAR(sar_ln_fwd_ckpt8, m.n, m.C, m.t, ptr(x), pg, pb, (float)eps, ptrm(y), f32m(rstd), i8m(codes), u8m(scales), stream());
+        return tuple(y, codes, scales, rstd);
+    }
+    const at::Tensor mean = empty({m.n}, at::kFloat, x);
+    SAR(sar_ln_fwd, m.n, m.C, m.t, ptr(x), pg, pb, (float)eps, ptrm(y), f32m(mean), f32m(rstd), stream());
+    return tuple(y, mean, rstd);
+}
+
+PyObject *ln_backward(Args &a) {   // x, gy, mean, rstd, gamma
+    const at::Tensor &x = a.tensor(), &gy = a.tensor(), &mean = a.tensor(), &rstd = a.tensor();
+    const at::Tensor gamma = a.optional();
+    const On on(x, gy, mean, rstd, gamma);
+    const Matrix m(x);
+    require(gy.sizes() == x.sizes(), "gy of another shape than x");
+    require_like(gy, x, m.n * m.C);
+    const float *pm = f32(mean, m.n), *pr = f32(rstd, m.n), *pg = f32(gamma, m.C);
+    const at::Tensor ws = bytes(L.sar_ln_workspace_bytes(m.C), x);
+    const at::Tensor gx = empty(x.sizes(), x.scalar_type(), x), dg = empty({m.C}, at::kFloat, x), db = empty({m.C}, at::kFloat, x);
+    SAR(sar_ln_bwd, m.n, m.C, m.t, ptr(x), pm, pr, pg, ptr(gy), ptrm(gx), f32m(dg), f32m(db), ptrm(ws), ws.nbytes(), stream());
+    return tuple(gx, dg, db);
+}
+
+PyObject *ln_backward_ckpt8(Args &a) {   // codes, scales, gy, rstd, gamma
+    const at::Tensor &codes = a.tensor(), &scales = a.tensor(), &gy = a.tensor(), &rstd = a.tensor();
+    const at::Tensor gamma = a.optional();
+    const On on(gy, codes, scales, rstd, gamma);
+    const Matrix m(gy);
+    require(gy.sizes() == codes.sizes(), "gy of another shape than the checkpoint");
+    require_checkpoint(codes, scales, m.n, m.C);
+    const float *pr = f32(rstd, m.n), *pg = f32(gamma, m.C);
+    const at::Tensor ws = bytes(L.sar_ln_workspace_bytes(m.C), gy);
+    const at::Tensor gx = empty(gy.sizes(), gy.scalar_type(), gy), dg = empty({m.C}, at::kFloat, gy), db = empty({m.C}, at::kFloat, gy);
+    SAR(sar_ln_bwd_ckpt8, m.n, m.C, m.t, i8(codes), u8(scales), pr, pg, ptr(gy), ptrm(gx), f32m(dg), f32m(db), ptrm(ws), ws.nbytes(), stream());
+    return tuple(gx, dg, db);
+}
+
+const int64_t *group_offsets(const at::Tensor &o, int64_t groups) {
+    require(o.scalar_type() == at::kLong && o.dim() == 1 && o.numel() == groups + 1, "expected int64 offsets, one more than matrices");
+    return static_cast<const int64_t *>(o.const_data_ptr());
+}
+// rows [n, K] times W [types, d_in, d_out] or its transposes; rows of no type: zeros in a new array, kept in a given one
+PyObject *typed_rows(Args &a, bool transposed) {   // rows, W, offsets, out or None
+    const at::Tensor &x = a.tensor(), &W = a.tensor(), &o = a.tensor();
+    at::Tensor out = a.optional();
+    const On on(x, W, o, out);
+    const Matrix m(x);
+    require(W.dim() == 3 && W.size(transposed ? 2 : 1) == m.C && W.scalar_type() == x.scalar_type(), "a weight matrix per type of the rows' width and type expected");
+    const int64_t T = W.size(0), N = W.size(transposed ? 1 : 2);
+    const int64_t *po = group_offsets(o, T);
+    const unsigned flags = out.defined() ? 0u : SAR_GROUPED_ZERO_REST;
+    if (out.defined()) {
+        require_like(out, x, m.n * N);
+        require(out.dim() == 2 && out.size(0) == m.n && out.size(1) == N, "out of another shape");
+        require(out.const_data_ptr() != x.const_data_ptr() || m.n == 0, "the products cannot be written over the rows");
+    } else {
+        out = empty({m.n, N}, x.scalar_type(), x);
+    }
+    if (transposed) SAR(sar_linear_grouped_bwd_input, m.n, (int32_t)T, (int32_t)N, m.C, m.t, po, ptr(x), ptr(W), ptrm(out), flags, nullptr, stream());
+    else SAR(sar_linear_grouped, m.n, (int32_t)T, m.C, (int32_t)N, m.t, po, ptr(x), ptr(W), ptrm(out), flags, nullptr, stream());
+    return wrap(out);
+}
+PyObject *typed_forward(Args &a) { return typed_rows(a, false); }
+PyObject *typed_backward_input(Args &a) { return typed_rows(a, true); }
+
+PyObject *typed_backward_weight(Args &a) {   // h, offsets, gz
+    const at::Tensor &h = a.tensor(), &o = a.tensor(), &g = a.tensor();
+    const On on(h, o, g);
+    const Matrix m(h), z(g);
+    require(z.n == m.n && z.t == m.t, "gz of other rows or another type than h");
+    require(o.numel() > 1, "expected int64 offsets, one more than matrices");
+    const int64_t T = o.numel() - 1;
+    const int64_t *po = group_offsets(o, T);
+    const at::Tensor dW = empty({T, m.C, z.C}, at::kFloat, h), ws = bytes(L.sar_linear_grouped_workspace_bytes(m.n, (int32_t)T, m.C, z.C), h);
+    SAR(sar_linear_grouped_bwd_weight, m.n, (int32_t)T, m.C, z.C, m.t, po, ptr(h), ptr(g), f32m(dW), nullptr, ptrm(ws), ws.nbytes(), stream());
+    return wrap(dW);
+}
+
+PyObject *typed_backward_weight_ckpt8(Args &a) {   // codes, scales, offsets, gz, gamma, beta
+    const at::Tensor &codes = a.tensor(), &scales = a.tensor(), &o = a.tensor(), &g = a.tensor();
+    const at::Tensor gamma = a.optional(), beta = a.optional();
+    const On on(g, codes, scales, o, gamma, beta);
+    const Matrix z(g);
+    require(codes.dim() == 2 && codes.size(0) == z.n, "gz of other rows than the checkpoint");
+    const int64_t C = codes.size(1), T = o.numel() - 1;
+    require(o.numel() > 1, "expected int64 offsets, one more than matrices");
+    require_checkpoint(codes, scales, z.n, C);
+    const float *pg = f32(gamma, C), *pb = f32(beta, C);
+    const int64_t *po = group_offsets(o, T);
+    const at::Tensor dW = empty({T, C, z.C}, at::kFloat, g), ws = bytes(L.sar_linear_grouped_workspace_bytes(z.n, (int32_t)T, (int32_t)C, z.C), g);
+    SAR(sar_linear_grouped_bwd_weight_ckpt8, z.n, (int32_t)T, (int32_t)C, z.C, z.t, po, i8(codes), u8(scales), pg, pb, ptr(g), f32m(dW), nullptr, ptrm(ws),
+        ws.nbytes(), stream());
+    return wrap(dW);
 }
 
 // ---- module --------------------------------------------------------------------------------------------------------------
@@ -633,6 +805,8 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
 #define M(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<f>)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {M(init), M(from_coo), M(gat_forward), M(gat_backward), M(gat_forward_parts), M(gat_backward_parts), M(spmm), M(spmm_scaled),
                            M(propagate), M(layer_forward), M(layer_backward), M(sage_forward), M(sage_backward), M(bn_forward), M(bn_backward),
+                           M(sage_backward_ckpt8), M(ckpt8_pack), M(ckpt8_unpack), M(ln_forward), M(ln_backward), M(ln_backward_ckpt8), M(typed_forward),
+                           M(typed_backward_input), M(typed_backward_weight), M(typed_backward_weight_ckpt8),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_sar_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
