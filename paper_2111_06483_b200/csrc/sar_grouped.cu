@@ -303,10 +303,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
 //
 // The tensor cores add to a float32 sum by cutting off what does not fit: every step of 16 rows takes up to one unit of the last
 // place towards zero, and 16,384 rows in one sum are 2e-5 to 3e-5 off (256 rows 2e-7, 1,024 rows 1e-6, 65,536 rows 8e-5 and
-// more).  So a sum runs over kRunRows rows at most, in one of two accumulators, and eight warps add it, rounding to nearest, to
-// sums that they hold in registers while the next run goes on.
+// more).  So a sum runs over kRunRows rows at most; then four warps add it, rounding to nearest, to sums that lie beside it
+// in tensor memory (128 x 256 sums would take half of the register file).
 //
-// With a checkpoint the same warps make the first operand: codes times scale, exact in bf16, written where a copy would have put
+// With a checkpoint eight more warps make the first operand: codes times scale, exact in bf16, written where a copy would have put
 // them.  Its rows stand for gamma v + beta, and  (gamma v + beta)^T dz = gamma (v^T dz) + beta (column sums of dz):  gamma and
 // beta enter in float32 after the product instead of rounding every value, and the column sums are taken from the tiles of dz
 // that are in shared memory anyway.
@@ -317,7 +317,7 @@ struct WeightArgs {
     const int8_t *codes;
     const uint8_t *scales;
     float *part;     // [chunks + G][d_in][d_out]: chunk c's part of group g in record c + g (along the way both only grow)
-    float *sums;     // [chunks + G][2][d_out]: sums of dz's columns over either half of the rows, or null
+    float *sums;     // [chunks + G][2 m_tiles][d_out]: sums of dz's columns, a share of the rows each, or null
     int *flag;
     int n, G, d_in, d_out, nb;
     int cols;        // of a tile (a multiple of 64 up to 256)
@@ -325,31 +325,32 @@ struct WeightArgs {
     int chunk_rows;  // a multiple of 64
     int stages;
 };
-constexpr int kWorkers = 8;
-constexpr int kWeightThreads = 64 + kWorkers * 32;
+constexpr int kAdders = 4, kMakers = 8;   // warps
+constexpr int kWeightThreads = 64 + kAdders * 32, kWeightThreads8 = kWeightThreads + kMakers * 32;
+constexpr uint32_t kSumCols = 256;        // where the sums lie in tensor memory, behind the accumulators
 struct WeightShared {
-    alignas(8) uint64_t full[kStagesMax], empty[kStagesMax], made[kStagesMax], mended, acc_full[2], acc_empty[2];
+    alignas(8) uint64_t full[kStagesMax], empty[kStagesMax], made[kStagesMax], acc_full[2], acc_empty[2];
     uint32_t tmem;
     int failed;
     GroupTable table;
 };
 
 template <bool CK>
-__global__ void __launch_bounds__(kWeightThreads, 1) grouped_weight_kernel(const __grid_constant__ WeightArgs p) {
+__global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grouped_weight_kernel(const __grid_constant__ WeightArgs p) {
     after_predecessor();
     extern __shared__ uint8_t dyn[];
     WeightShared &sh = *reinterpret_cast<WeightShared *>(dyn);
     const uint32_t ring = (smem_addr(dyn) + (uint32_t)sizeof(WeightShared) + 1023u) & ~1023u;
     const int panels = p.cols / 64;
     const uint32_t stage_bytes = (2 + panels) * kPanel;
+    const uint32_t bufs = p.cols <= 128 ? 2 : 1;   // accumulators of 128 columns each, or one of up to 256
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *failed = &sh.failed;
 
     group_table(sh.table, p.offsets, p.G, p.n);
     if (threadIdx.x == 0) {
-        for (int i = 0; i < p.stages; ++i) bar_init(smem_addr(&sh.full[i]), 1), bar_init(smem_addr(&sh.empty[i]), 1), bar_init(smem_addr(&sh.made[i]), kWorkers);
-        for (int i = 0; i < 2; ++i) bar_init(smem_addr(&sh.acc_full[i]), 1), bar_init(smem_addr(&sh.acc_empty[i]), kWorkers);
-        bar_init(smem_addr(&sh.mended), kWorkers);
+        for (int i = 0; i < p.stages; ++i) bar_init(smem_addr(&sh.full[i]), 1), bar_init(smem_addr(&sh.empty[i]), 1), bar_init(smem_addr(&sh.made[i]), kMakers);
+        for (int i = 0; i < 2; ++i) bar_init(smem_addr(&sh.acc_full[i]), 1), bar_init(smem_addr(&sh.acc_empty[i]), kAdders);
         sh.failed = 0;
         bar_init_fence();
     }
@@ -360,8 +361,8 @@ __global__ void __launch_bounds__(kWeightThreads, 1) grouped_weight_kernel(const
     const uint32_t tmem = sh.tmem;
 
     const int tiles = p.m_tiles * p.n_tiles;
-    const int chunk = blockIdx.x / tiles, tile = blockIdx.x % tiles;
-    const int m0 = tile / p.n_tiles * 128, n0 = tile % p.n_tiles * p.cols, cols = min(p.cols, p.d_out - n0);
+    const int chunk = blockIdx.x / tiles, tile = blockIdx.x % tiles, m_tile = tile / p.n_tiles;
+    const int m0 = m_tile * 128, n0 = tile % p.n_tiles * p.cols, cols = min(p.cols, p.d_out - n0);
     const int h_panels = p.d_in - m0 > 64 ? 2 : 1;
     const int chunk0 = (int)min((long long)p.n, (long long)chunk * p.chunk_rows), chunk1 = (int)min((long long)p.n, (long long)chunk0 + p.chunk_rows);
     int g0 = 0;   // the first group that ends behind the chunk's start
@@ -377,6 +378,15 @@ __global__ void __launch_bounds__(kWeightThreads, 1) grouped_weight_kernel(const
         return lo < hi;
     };
     const auto more = [&](int g) { return g < p.G && sh.table.first[g] < chunk1; };
+    // rows from `rows` to the next multiple of 16 of a tile take part in the products, but are another group's: zeros in the
+    // panels from .. to - 1 of the stage, by the threads me = 0 .. of - 1
+    const auto clear = [&](uint32_t at, int rows, int from, int to, int me, int of) {
+        const int rest = 16 - rows % 16;
+        for (int i = me; i < rest * 8 * (to - from); i += of) {
+            const uint32_t where = at + (from + i / (rest * 8)) * kPanel + (rows + i / 8 % rest) * 128 + (i % 8) * 16;
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};\n" ::"r"(where), "r"(0) : "memory");
+        }
+    };
 
     if (warp == 0) {
         if (lane == 0) {
@@ -398,178 +408,183 @@ __global__ void __launch_bounds__(kWeightThreads, 1) grouped_weight_kernel(const
             if (!ok)
                 for (uint32_t s = 0; s < (uint32_t)p.stages && s < use; ++s) bar_drain(smem_addr(&sh.full[s]), ((use - 1 - s) / p.stages) & 1);
         }
-    } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t instr = tc_instr((cols + 15) & ~15, true, true);
-            uint32_t use = 0, run = 0, mends = 0;
-            bool ok = true;
-            for (int g = g0; ok && more(g); ++g) {
-                int lo, hi;
-                if (!segment(g, lo, hi)) continue;
-                for (int r0 = lo; ok && r0 < hi; r0 += kRunRows, ++run) {
-                    const uint32_t buf = run & 1;
-                    ok = run < 2 || bar_wait(smem_addr(&sh.acc_empty[buf]), (run / 2 + 1) & 1, failed);
-                    if (!ok) break;
-                    tc_after_sync();
-                    const int r1 = min(hi, r0 + kRunRows);
-                    for (int r = r0; r < r1; r += kStep, ++use) {
-                        const uint32_t s = use % p.stages, at = ring + s * stage_bytes;
-                        const int rows = min(kStep, hi - r);
-                        ok = bar_wait(smem_addr(&sh.full[s]), (use / p.stages) & 1, failed);
-                        if (CK) ok = ok && bar_wait(smem_addr(&sh.made[s]), (use / p.stages) & 1, failed);
-                        else if (rows % 16) ok = ok && bar_wait(smem_addr(&sh.mended), mends++ & 1, failed);
-                        if (!ok) break;
-                        tc_after_sync();
-                        for (int j = 0; j < (rows + 15) / 16; ++j)
-                            tc_mma(tmem + buf * 256, tc_operand(at + j * 2048, kPanel, 1024), tc_operand(at + 2 * kPanel + j * 2048, kPanel, 1024), instr, r > r0 || j > 0);
-                        tc_commit(smem_addr(&sh.empty[s]));
-                    }
-                    if (ok) tc_commit(smem_addr(&sh.acc_full[buf]));
-                }
-            }
-        }
-    } else {
-        const int w = warp - 2, quad = warp & 3, half = w / 4, me = threadIdx.x - 64;
-        float sum[4][32];   // columns (2 c + half) 32 .. + 31 of row m0 + 32 quad + lane of dW
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int e = 0; e < 32; ++e) sum[c][e] = 0.f;
-        const bool want_sums = CK && p.sums && m0 == 0;
-        float2 cs = make_float2(0.f, 0.f);   // columns 2 (me % 128) and the next of dz, over every other 32 rows of a step
+    } else if (warp == 1) {   // all lanes wait, the first one issues
+        const uint32_t instr = tc_instr((cols + 15) & ~15, true, true);
         uint32_t use = 0, run = 0;
         bool ok = true;
-        // the part of h: 8 columns of four rows a step and thread
-        const int hc = me & 15, hr = me >> 4;
-        uint2 code[4];
-        unsigned scale[4];
-        const bool h_cols = m0 + hc * 8 < p.d_in;
-        const auto ask = [&](int r, int rows) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = hr + 16 * i;
-                code[i] = make_uint2(0u, 0u);
-                scale[i] = 0;
-                if (h_cols && row < rows) {
-                    code[i] = __ldg(reinterpret_cast<const uint2 *>(p.codes + (long long)(r + row) * p.d_in + m0 + hc * 8));
-                    scale[i] = __ldg(p.scales + (long long)(r + row) * p.nb + (m0 + hc * 8) / kCkptBlock);
-                }
-            }
-        };
-        // add the accumulator of a finished run to the sums
-        const auto drain = [&](uint32_t of) {
-            const uint32_t buf = of & 1;
-            if (!bar_wait(smem_addr(&sh.acc_full[buf]), (of / 2) & 1, failed)) return false;
-            tc_after_sync();
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int col = (2 * c + half) * 32;
-                if (col < cols) {
-                    float x[32];
-                    tmem_load32(tmem + buf * 256 + col + ((uint32_t)(quad * 32) << 16), x);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) sum[c][e] += x[e];
-                }
-            }
-            tc_before_sync();
-            __syncwarp();
-            if (lane == 0) bar_arrive(smem_addr(&sh.acc_empty[buf]));
-            return true;
-        };
-        // rows from `rows` to the next multiple of 16 of a tile take part in the products: they are another group's
-        const auto clear = [&](uint32_t at, int rows, int from, int to) {
-            const int rest = (16 - rows % 16) % 16;
-            for (int i = me; i < rest * 8 * (to - from); i += kWorkers * 32) {
-                const uint32_t where = at + (from + i / (rest * 8)) * kPanel + (rows + i / 8 % rest) * 128 + (i % 8) * 16;
-                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};\n" ::"r"(where), "r"(0) : "memory");
-            }
-        };
         for (int g = g0; ok && more(g); ++g) {
             int lo, hi;
             if (!segment(g, lo, hi)) continue;
-            if (CK) ask(lo, min(kStep, hi - lo));
-            bool pending = false;   // the run before this one is still to be added
             for (int r0 = lo; ok && r0 < hi; r0 += kRunRows, ++run) {
+                const uint32_t buf = run % bufs;
+                ok = run < bufs || bar_wait(smem_addr(&sh.acc_empty[buf]), (run / bufs + 1) & 1, failed);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_after_sync();
                 const int r1 = min(hi, r0 + kRunRows);
-                float2 cr = make_float2(0.f, 0.f);
                 for (int r = r0; r < r1; r += kStep, ++use) {
                     const uint32_t s = use % p.stages, at = ring + s * stage_bytes;
                     const int rows = min(kStep, hi - r);
-                    if (CK) {
-                        ok = use < (uint32_t)p.stages || bar_wait(smem_addr(&sh.empty[s]), (use / p.stages + 1) & 1, failed);
-                        if (!ok) break;
-                        if (h_cols) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int row = hr + 16 * i;
-                                const unsigned word[2] = {code[i].x, code[i].y};
-                                float v[8];
-                                ckpt_decode_n<8>(word, ckpt_scale(scale[i]), v);
-                                const uint4 b = Elem<__nv_bfloat16>::pack(v);
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + (hc >> 3) * kPanel + row * 128 + (((hc & 7) ^ (row & 7)) << 4)),
-                                             "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
-                                             : "memory");
-                            }
-                        }
-                        if (r + kStep < hi) ask(r + kStep, min(kStep, hi - r - kStep));
-                        if (rows % 16 || want_sums) {
-                            ok = bar_wait(smem_addr(&sh.full[s]), (use / p.stages) & 1, failed);
-                            if (!ok) break;
-                        }
-                        if (want_sums) {
-                            const int pair = me & 127;
-                            if (pair * 2 < cols) {
-                                const uint32_t col = at + (2 + pair / 32) * kPanel + (pair & 3) * 4;
-                                for (int q = (me >> 7) * 32; q < min((me >> 7) * 32 + 32, rows); ++q) {
-                                    uint32_t v;
-                                    asm volatile("ld.shared.b32 %0, [%1];\n" : "=r"(v) : "r"(col + q * 128 + (((pair >> 2 & 7) ^ (q & 7)) << 4)));
-                                    cr.x += __uint_as_float(v << 16);
-                                    cr.y += __uint_as_float(v & 0xffff0000u);
-                                }
-                            }
-                        }
-                        if (rows % 16) clear(at, rows, 2, 2 + panels);   // h's rows are zeros already
+                    ok = bar_wait(smem_addr(&sh.full[s]), (use / p.stages) & 1, failed);
+                    if (CK) ok = ok && bar_wait(smem_addr(&sh.made[s]), (use / p.stages) & 1, failed);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    if (!CK && rows % 16) {
+                        clear(at, rows, 0, h_panels, lane, 32);
+                        clear(at, rows, 2, 2 + panels, lane, 32);
                         async_proxy_fence();
                         __syncwarp();
-                        if (lane == 0) bar_arrive(smem_addr(&sh.made[s]));
-                    } else if (rows % 16) {
-                        ok = bar_wait(smem_addr(&sh.full[s]), (use / p.stages) & 1, failed);
-                        if (!ok) break;
-                        clear(at, rows, 0, h_panels);
-                        clear(at, rows, 2, 2 + panels);
-                        async_proxy_fence();
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(smem_addr(&sh.mended));
                     }
-                    if (pending) {   // the products of this run's first step go on meanwhile
-                        ok = drain(run - 1);
-                        pending = false;
-                        if (!ok) break;
+                    tc_after_sync();
+                    if (lane == 0) {
+                        for (int j = 0; j < (rows + 15) / 16; ++j)
+                            tc_mma(tmem + buf * 128, tc_operand(at + j * 2048, kPanel, 1024), tc_operand(at + 2 * kPanel + j * 2048, kPanel, 1024), instr, r > r0 || j > 0);
+                        tc_commit(smem_addr(&sh.empty[s]));
                     }
                 }
-                cs.x += cr.x;
-                cs.y += cr.y;
-                pending = true;
+                if (ok && lane == 0) tc_commit(smem_addr(&sh.acc_full[buf]));
             }
-            ok = ok && drain(run - 1);
-            if (!ok) break;
-            const long long record = chunk + g;
-            const int m = m0 + quad * 32 + lane;
+        }
+    } else if (warp < 2 + kAdders) {
+        const uint32_t quad = warp & 3, lanes = quad * 32 << 16;   // rows m0 + 32 quad + lane of dW
+        const int m = m0 + quad * 32 + lane;
+        uint32_t run = 0;
+        bool ok = true;
+        for (int g = g0; ok && more(g); ++g) {
+            int lo, hi;
+            if (!segment(g, lo, hi)) continue;
+            float *out = p.part + ((long long)(chunk + g) * p.d_in + m) * p.d_out + n0;
+            for (int r0 = lo; r0 < hi; r0 += kRunRows, ++run) {
+                const uint32_t buf = run % bufs;
+                ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&sh.acc_full[buf]), (run / bufs) & 1, failed));
+                if (!ok) break;
+                tc_after_sync();
+                const bool first = r0 == lo, last = r0 + kRunRows >= hi;
+                for (int c = 0; c < cols; c += 32) {
+                    uint32_t x[32], y[32];
+                    tmem_ask32(tmem + buf * 128 + c + lanes, x);
+                    if (!first) tmem_ask32(tmem + kSumCols + c + lanes, y);
+                    tmem_wait_load(x);
+                    if (!first) {
+                        tmem_tie32(y);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int col = (2 * c + half) * 32;
-                if (m < p.d_in) {
-                    float4 *out = reinterpret_cast<float4 *>(p.part + (record * p.d_in + m) * p.d_out + n0 + col);
+                        for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) + __uint_as_float(y[e]));
+                    }
+                    if (!last) {
+                        tmem_store32(tmem + kSumCols + c + lanes, x);
+                    } else if (m < p.d_in) {
 #pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        if (col + q * 4 < cols) out[q] = make_float4(sum[c][4 * q], sum[c][4 * q + 1], sum[c][4 * q + 2], sum[c][4 * q + 3]);
+                        for (int q = 0; q < 8; ++q)
+                            if (c + q * 4 < cols) *reinterpret_cast<uint4 *>(out + c + q * 4) = make_uint4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+                    }
                 }
-#pragma unroll
-                for (int e = 0; e < 32; ++e) sum[c][e] = 0.f;
+                tmem_wait_store();
+                tc_before_sync();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_addr(&sh.acc_empty[buf]));
             }
-            if (want_sums && (me & 127) * 2 < cols)   // one of the two halves of every step's rows
-                *reinterpret_cast<float2 *>(p.sums + (record * 2 + (me >> 7)) * p.d_out + n0 + (me & 127) * 2) = cs;
-            cs = make_float2(0.f, 0.f);
+        }
+    } else if constexpr (CK) {
+        const int w = warp - 2 - kAdders, me = w * 32 + lane;
+        // the part of h: 8 columns of four rows a step and thread, asked for kAhead steps before they are used
+        constexpr int kAhead = 3;
+        const int hc = me & 15, hr = me >> 4;
+        uint2 code[kAhead][4];
+        unsigned scale[kAhead][4];
+        const bool h_cols = m0 + hc * 8 < p.d_in;
+        const auto ask = [&](uint2 (&code)[4], unsigned (&scale)[4], int r, int hi) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = r + hr + 16 * i;
+                code[i] = make_uint2(0u, 0u);
+                scale[i] = 0;
+                if (h_cols && row < hi) {
+                    code[i] = __ldg(reinterpret_cast<const uint2 *>(p.codes + (long long)row * p.d_in + m0 + hc * 8));
+                    scale[i] = __ldg(p.scales + (long long)row * p.nb + (m0 + hc * 8) / kCkptBlock);
+                }
+            }
+        };
+        // the column sums: 8 columns of every fourth row of one half of a step, the steps shared by the blocks of a chunk
+        const bool want_sums = p.sums != nullptr && (w & 3) < panels;
+        const int half = w >> 2;
+        const uint32_t sum_at = (2 + (w & 3)) * kPanel + (half * 32 + (lane >> 3)) * 128;
+        float cs[8];
+        uint32_t use = 0;
+        bool ok = true;
+        for (int g = g0; ok && more(g); ++g) {
+            int lo, hi;
+            if (!segment(g, lo, hi)) continue;
+#pragma unroll
+            for (int d = 0; d < kAhead; ++d) ask(code[d], scale[d], lo + d * kStep, hi);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) cs[e] = 0.f;
+            int step = 0;
+            for (int r3 = lo; ok && r3 < hi; r3 += kAhead * kStep) {
+#pragma unroll
+                for (int d = 0; d < kAhead; ++d) {   // unrolled: the sets are registers
+                    const int r = r3 + d * kStep;
+                    if (r >= hi) break;
+                    const uint32_t s = use % p.stages, at = ring + s * stage_bytes;
+                    const int rows = min(kStep, hi - r);
+                    ok = __all_sync(0xffffffffu, use < (uint32_t)p.stages || bar_wait(smem_addr(&sh.empty[s]), (use / p.stages + 1) & 1, failed));
+                    if (!ok) break;
+                    if (h_cols) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int row = hr + 16 * i;
+                            const unsigned word[2] = {code[d][i].x, code[d][i].y};
+                            float v[8];
+                            ckpt_decode_n<8>(word, ckpt_scale(scale[d][i]), v);
+                            const uint4 b = Elem<__nv_bfloat16>::pack(v);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + (hc >> 3) * kPanel + row * 128 + (((hc & 7) ^ (row & 7)) << 4)),
+                                         "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                                         : "memory");
+                        }
+                    }
+                    ask(code[d], scale[d], r + kAhead * kStep, hi);
+                    const bool sum = want_sums && step % p.m_tiles == m_tile;
+                    if (rows % 16 || sum) {
+                        ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&sh.full[s]), (use / p.stages) & 1, failed));
+                        if (!ok) break;
+                    }
+                    if (rows % 16) clear(at, rows, 2, 2 + panels, me, kMakers * 32);   // h's rows are zeros already
+                    async_proxy_fence();
+                    if (sum) {
+                        float cr[8];   // a step's sums first: long sums of single values lose digits
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) cr[e] = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int row = half * 32 + (lane >> 3) + 4 * i;
+                            uint4 v;
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at + sum_at + i * 512 + (((lane & 7) ^ (row & 7)) << 4)));
+                            float x[8];
+                            Elem<__nv_bfloat16>::unpack(v, x);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) cr[e] += row < rows ? x[e] : 0.f;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) cs[e] += cr[e];
+                    }
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_addr(&sh.made[s]));
+                    ++use;
+                    ++step;
+                }
+            }
+            if (ok && want_sums) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    cs[e] += __shfl_xor_sync(0xffffffffu, cs[e], 8);
+                    cs[e] += __shfl_xor_sync(0xffffffffu, cs[e], 16);
+                }
+                const int col = (w & 3) * 64 + lane * 8;
+                if (lane < 8 && col < cols) {
+                    float4 *out = reinterpret_cast<float4 *>(p.sums + ((long long)(chunk + g) * 2 * p.m_tiles + m_tile * 2 + half) * p.d_out + n0 + col);
+                    out[0] = make_float4(cs[0], cs[1], cs[2], cs[3]);
+                    out[1] = make_float4(cs[4], cs[5], cs[6], cs[7]);
+                }
+            }
         }
     }
     __syncwarp();
@@ -582,7 +597,7 @@ __global__ void __launch_bounds__(kWeightThreads, 1) grouped_weight_kernel(const
 
 // dW[g] = the sum of group g's records in the order of the chunks, times gamma, plus beta times the sums of dz's columns
 __global__ void __launch_bounds__(256) grouped_weight_reduce_kernel(const int64_t *__restrict__ offsets, int G, long long n, int d_in, int d_out, int chunk_rows,
-                                                                    const float *__restrict__ part, const float *__restrict__ sums,
+                                                                    int shares, const float *__restrict__ part, const float *__restrict__ sums,
                                                                     const float *__restrict__ gamma, const float *__restrict__ beta, float *__restrict__ dw) {
     after_predecessor();
     const int g = blockIdx.y;
@@ -610,8 +625,8 @@ __global__ void __launch_bounds__(256) grouped_weight_reduce_kernel(const int64_
             const float4 v = *reinterpret_cast<const float4 *>(part + (from + s + g) * size + x);
             acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
             if (sums) {
-                const float4 *u = reinterpret_cast<const float4 *>(sums + (long long)(from + s + g) * 2 * d_out + c), a = u[0], b = u[d_out / 4];
-                col.x += a.x + b.x, col.y += a.y + b.y, col.z += a.z + b.z, col.w += a.w + b.w;
+                const float4 *u = reinterpret_cast<const float4 *>(sums + (long long)(from + s + g) * shares * d_out + c);
+                for (int i = 0; i < shares; ++i) col.x += u[i * (d_out / 4)].x, col.y += u[i * (d_out / 4)].y, col.z += u[i * (d_out / 4)].z, col.w += u[i * (d_out / 4)].w;
             }
         }
         if (gamma) {
@@ -722,7 +737,7 @@ static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out) {
     w.stages = w.stages > kStagesMax ? kStagesMax : w.stages;
     w.smem = fixed + w.stages * stage;
     w.part_bytes = sar_round_up((size_t)(w.chunks + groups) * d_in * d_out * 4, 256);
-    w.sum_bytes = sar_round_up((size_t)(w.chunks + groups) * 2 * d_out * 4, 256);
+    w.sum_bytes = sar_round_up((size_t)(w.chunks + groups) * 2 * w.m_tiles * d_out * 4, 256);
     return w;
 }
 
@@ -759,13 +774,13 @@ static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_
         SAR_LAUNCH("linear_grouped_bwd_weight", st, launch_if(overlap, grouped_weight_kernel<false>, blocks, kWeightThreads, w.smem, st, p));
     } else {
         SAR_TRY(ensure_smem(grouped_weight_kernel<true>, w.smem));
-        SAR_LAUNCH("linear_grouped_bwd_weight_ckpt8", st, launch_if(overlap, grouped_weight_kernel<true>, blocks, kWeightThreads, w.smem, st, p));
+        SAR_LAUNCH("linear_grouped_bwd_weight_ckpt8", st, launch_if(overlap, grouped_weight_kernel<true>, blocks, kWeightThreads8, w.smem, st, p));
     }
     SAR_TRY(sar_after_launch());
     const long long quads = (long long)d_in * d_out / 4;
     SAR_LAUNCH("linear_grouped_bwd_weight_reduce", st,
                launch(grouped_weight_reduce_kernel, dim3((unsigned)((quads + 63) / 64), (unsigned)groups), dim3(64, 4), 0, st, offsets, (int)groups, (long long)n,
-                      (int)d_in, (int)d_out, w.chunk_rows, p.part, p.sums, gamma, beta, dw));
+                      (int)d_in, (int)d_out, w.chunk_rows, 2 * w.m_tiles, p.part, p.sums, gamma, beta, dw));
     return sar_after_launch();
 }
 

@@ -143,6 +143,30 @@ def test_weight_sums_do_not_drift():
     assert ((dw[0].double() - want).norm() / want.norm()).item() < 2e-6
 
 
+@pytest.mark.parametrize("d_in,d_out,types", [(256, 256, 8), (136, 72, 64), (64, 128, 200), (264, 40, 5)])
+def test_long_chunks_with_many_ragged_ends(d_in, d_out, types):
+    """Hundreds of steps a block, several segments with ragged ends in each: what a role takes for the stage that it waits for must be
+    that stage's latest round.  The bound is the one above, of the whole result."""
+    from paper_2111_06483_b200 import api
+    n = 1_000_000
+    gen = torch.Generator(device="cuda").manual_seed(d_in)
+    h, dz = (torch.randn(n, d, generator=gen, device="cuda").bfloat16() for d in (d_in, d_out))
+    cut = torch.randint(0, n, (types - 1,), generator=gen, device="cuda").sort().values
+    o = torch.cat([cut.new_zeros(1), cut, cut.new_full((1,), n)])
+    host = o.tolist()
+    want = torch.stack([h[a:b].double().t() @ dz[a:b].double() for a, b in zip(host, host[1:])])
+    for _ in range(3):
+        dw = api.typed_linear_backward_weight(h, o, dz)
+        assert ((dw.double() - want).norm() / want.norm()).item() < 2e-6
+    p = api.ckpt8_pack(h)
+    v = api.ckpt8_unpack(p, torch.float32).double()
+    want = torch.stack([(v[a:b] + 0.5).t() @ dz[a:b].double() for a, b in zip(host, host[1:])])
+    half = torch.full((d_in,), 0.5, device="cuda")
+    for _ in range(3):
+        dw = api.typed_linear_backward_weight(p, o, dz, beta=half)
+        assert ((dw.double() - want).norm() / want.norm()).item() < 2e-6
+
+
 def checkpoint_of(h):
     codes, scales = oracle.ckpt8_pack(np64(h.float()))
     return torch.tensor(codes).cuda(), torch.tensor(scales).cuda()
