@@ -3,154 +3,167 @@
 #include "sar_ckpt8.cuh"
 #include "sar_dispatch.cuh"
 
+#include <type_traits>
+
 namespace sar {
 
-// EPT columns a thread (8, 4 or 1), so 32 / EPT consecutive threads a block of 32 columns: a thread's share is one or two
-// 16-byte vectors (8 bytes for 4 bf16) and EPT codes.  Rows whose columns are no multiple of 32 end in a shorter block, whose
-// last threads have no columns; with whole blocks the rows do not matter and the blocks are counted through.
-template <typename T, int EPT>
-struct CkptVec;
-template <int EPT>
-struct CkptVec<float, EPT> {
-    __device__ __forceinline__ static void load(const float *p, float (&x)[EPT]) {
-        if constexpr (EPT >= 4) {
+// Division by the blocks of a row, as a product: exact for numerators below 2^31 (q = (n * ceil(2^(31 + l) / d)) >> (31 + l) with
+// l = ceil(log2 d): the product's excess is below n / 2^31 of a unit).
+struct RowDivide {
+    unsigned long long mul;
+    int shift;
+    int d;
+};
+static RowDivide row_divide(int d) {
+    int l = 0;
+    while ((1ll << l) < d) ++l;
+    return {((1ull << (31 + l)) + d - 1) / d, 31 + l, d};
+}
+
+// A block's 32 columns are S slots of E columns for each of LPB = 32 / (E S) consecutive threads: slot i of thread `sub` starts at
+// column (i LPB + sub) E of the block, E being 8 bf16 (16 bytes), 4 of either type, or one column for rows that allow no more.  Several
+// slots rather than more threads: a block's maximum is then joined in 2 or 3 steps.  Rows whose columns are no multiple of 32 end in a
+// shorter block, where some slots have no columns; with whole blocks the rows do not matter and the blocks are counted through.
+template <typename T, int E, int S>
+struct CkptBlock {
+    using Vec = ColVec<T, E>;
+    using raw_t = typename Vec::type;
+    static constexpr int P = (E + 1) / 2, LPB = kCkptBlock / (E * S);
+    long long at;   // flat index of the thread's first slot
+    int left;       // columns from there to the end of the row or the block; none for a block behind the last
+    __device__ __forceinline__ CkptBlock(long long b, long long blocks, int sub, int C, const RowDivide &nb, bool whole) {
+        if (whole) {
+            at = b * kCkptBlock + sub * E;
+            left = kCkptBlock - sub * E;
+        } else {
+            const long long row = b < (1ll << 31) ? (long long)((unsigned long long)b * nb.mul >> nb.shift) : b / nb.d;
+            const int col = (int)(b - row * nb.d) * kCkptBlock + sub * E;
+            at = row * C + col;
+            left = C - col;
+        }
+        if (b >= blocks) left = 0;
+    }
+    // E divides C: a slot has all its columns or none
+    __device__ __forceinline__ bool ok(int i) const { return i * LPB * E < left; }
+    __device__ __forceinline__ long long slot(int i) const { return at + i * LPB * E; }
+};
+
+// Each thread asks for its columns of U blocks before it uses the first: 64 bytes in flight.
+template <typename T, int E, int S>
+constexpr int ckpt_ahead = 64 / (E * S * (int)sizeof(T)) < 1 ? 1 : 64 / (E * S * (int)sizeof(T)) > 4 ? 4 : 64 / (E * S * (int)sizeof(T));
+
+template <typename T, int E, int S>
+__global__ void __launch_bounds__(256, 4) ckpt8_pack_kernel(long long blocks, int C, RowDivide nb, const T *__restrict__ x, int8_t *__restrict__ codes,
+                                                            uint8_t *__restrict__ scales) {
+    after_predecessor();
+    using B = CkptBlock<T, E, S>;
+    constexpr int P = B::P, LPB = B::LPB, U = ckpt_ahead<T, E, S>;
+    const int sub = threadIdx.x % LPB;
+    const bool whole = C == nb.d * kCkptBlock;
+    // b0: the warp's first block, the same for all its lanes (the shuffles need every lane); a warp's blocks follow one another
+    const long long stride = (long long)gridDim.x * (256 / LPB) * U;
+    for (long long b0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * (32 / LPB) * U; b0 < blocks; b0 += stride) {
+        typename B::raw_t raw[U][S];
 #pragma unroll
-            for (int q = 0; q < EPT / 4; ++q) {
-                const float4 v = __ldg(reinterpret_cast<const float4 *>(p) + q);
-                x[4 * q] = v.x, x[4 * q + 1] = v.y, x[4 * q + 2] = v.z, x[4 * q + 3] = v.w;
+        for (int u = 0; u < U; ++u) {
+            const B p(b0 + u * (32 / LPB) + (threadIdx.x & 31) / LPB, blocks, sub, C, nb, whole);
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+                raw[u][i] = typename B::raw_t{};
+                if (p.ok(i)) raw[u][i] = __ldg(reinterpret_cast<const typename B::raw_t *>(x + p.slot(i)));
             }
-        } else {
-            x[0] = __ldg(p);
         }
-    }
-    __device__ __forceinline__ static void store(float *p, const float (&x)[EPT]) {
-        if constexpr (EPT >= 4) {
 #pragma unroll
-            for (int q = 0; q < EPT / 4; ++q) reinterpret_cast<float4 *>(p)[q] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
-        } else {
-            *p = x[0];
+        for (int u = 0; u < U; ++u) {
+            const long long b = b0 + u * (32 / LPB) + (threadIdx.x & 31) / LPB;
+            const B p(b, blocks, sub, C, nb, whole);
+            float2 v[S][P];
+            unsigned top = 0;
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+                B::Vec::get(raw[u][i], v[i]);
+#pragma unroll
+                for (int q = 0; q < P; ++q) top = max(top, E == 1 ? ckpt_magnitude(v[i][q].x) : max(ckpt_magnitude(v[i][q].x), ckpt_magnitude(v[i][q].y)));
+            }
+#pragma unroll
+            for (int d = 1; d < LPB; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const unsigned s = ckpt_scale_byte(top);
+            const float inv = ckpt_inverse(s);
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+                if (!p.ok(i)) continue;
+                int8_t *to = codes + p.slot(i);
+                if constexpr (E == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(ckpt_code4(&v[i][0].x, inv, s), ckpt_code4(&v[i][2].x, inv, s));
+                else if constexpr (E == 4) *reinterpret_cast<unsigned *>(to) = ckpt_code4(&v[i][0].x, inv, s);
+                else *to = (int8_t)(s == 255u ? 0u : ckpt_code(v[i][0].x, inv));
+            }
+            if (sub == 0 && b < blocks) scales[b] = (uint8_t)s;
         }
-    }
-};
-template <int EPT>
-struct CkptVec<__nv_bfloat16, EPT> {
-    using E = Elem<__nv_bfloat16>;
-    __device__ __forceinline__ static void load(const __nv_bfloat16 *p, float (&x)[EPT]) {
-        if constexpr (EPT == 8) {
-            E::unpack(__ldg(reinterpret_cast<const uint4 *>(p)), x);
-        } else if constexpr (EPT == 4) {
-            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p));
-            x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xffff0000u);
-            x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xffff0000u);
-        } else {
-            x[0] = E::load1(p);
-        }
-    }
-    __device__ __forceinline__ static void store(__nv_bfloat16 *p, const float (&x)[EPT]) {
-        if constexpr (EPT == 8) *reinterpret_cast<uint4 *>(p) = E::pack(x);
-        else if constexpr (EPT == 4) *reinterpret_cast<uint2 *>(p) = make_uint2(E::pack2(x[0], x[1]), E::pack2(x[2], x[3]));
-        else E::store1(p, x[0]);
-    }
-};
-template <int EPT>
-__device__ __forceinline__ void store_codes(int8_t *p, const float (&x)[EPT], float inverse, unsigned s) {
-    if constexpr (EPT == 8) *reinterpret_cast<uint2 *>(p) = make_uint2(ckpt_code4(x, inverse, s), ckpt_code4(x + 4, inverse, s));
-    else if constexpr (EPT == 4) *reinterpret_cast<unsigned *>(p) = ckpt_code4(x, inverse, s);
-    else *p = (int8_t)(s == 255u ? 0u : ckpt_code(x[0], inverse));
-}
-template <int EPT>
-__device__ __forceinline__ void load_codes(const int8_t *p, float scale, float (&x)[EPT]) {
-    if constexpr (EPT == 8) {
-        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p));
-        const unsigned w[2] = {v.x, v.y};
-        ckpt_decode_n<8>(w, scale, x);
-    } else if constexpr (EPT == 4) {
-        const unsigned w[1] = {__ldg(reinterpret_cast<const unsigned *>(p))};
-        ckpt_decode_n<4>(w, scale, x);
-    } else {
-        x[0] = (float)__ldg(reinterpret_cast<const signed char *>(p)) * scale;
     }
 }
 
-// where a thread's columns lie: block b of the array, `at` the flat index of the thread's first column
-struct CkptPlace {
-    long long at;
-    bool some;   // the thread has columns in this block
-};
-template <int EPT>
-__device__ __forceinline__ CkptPlace ckpt_place(long long b, int sub, int C, int nb, bool whole) {
-    if (whole) return {b * kCkptBlock + sub * EPT, true};
-    long long row;
-    int blk;
-    if (b < (1ll << 31)) {   // a 32-bit division is a third of a 64-bit one
-        row = (unsigned)b / (unsigned)nb;
-        blk = (int)((unsigned)b - (unsigned)row * (unsigned)nb);
-    } else {
-        row = b / nb;
-        blk = (int)(b - row * nb);
-    }
-    const int col = blk * kCkptBlock + sub * EPT;
-    return {row * C + col, col < C};   // EPT divides C: a thread has all its columns or none
-}
-
-template <typename T, int EPT>
-__global__ void __launch_bounds__(256) ckpt8_pack_kernel(long long blocks, int C, int nb, const T *__restrict__ x, int8_t *__restrict__ codes,
-                                                         uint8_t *__restrict__ scales) {
+template <typename T, int E, int S>
+__global__ void __launch_bounds__(256, 4) ckpt8_unpack_kernel(long long blocks, int C, RowDivide nb, const int8_t *__restrict__ codes,
+                                                              const uint8_t *__restrict__ scales, T *__restrict__ x) {
     after_predecessor();
-    constexpr int LPB = kCkptBlock / EPT;
-    const long long stride = (long long)gridDim.x * (256 / LPB);
+    using B = CkptBlock<T, E, S>;
+    using W = typename std::conditional<E == 8, uint2, typename std::conditional<E == 4, unsigned, signed char>::type>::type;
+    constexpr int P = B::P, LPB = B::LPB, U = ckpt_ahead<T, E, S>;
     const int sub = threadIdx.x % LPB;
-    const bool whole = C == nb * kCkptBlock;
-    // a warp's blocks all lie before the end or the warp takes this step as a whole: the shuffles need every lane
-    for (long long b0 = (long long)blockIdx.x * (256 / LPB) + (threadIdx.x & ~31) / LPB; b0 < blocks; b0 += stride) {
-        const long long b = b0 + (threadIdx.x & 31) / LPB;
-        CkptPlace p = ckpt_place<EPT>(b, sub, C, nb, whole);
-        p.some = p.some && b < blocks;
-        float v[EPT];
+    const bool whole = C == nb.d * kCkptBlock;
+    const long long stride = (long long)gridDim.x * (256 / LPB) * U;
+    for (long long b0 = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * (32 / LPB) * U + (threadIdx.x & 31) / LPB; b0 < blocks; b0 += stride) {
+        W raw[U][S];
+        unsigned s[U];
 #pragma unroll
-        for (int i = 0; i < EPT; ++i) v[i] = 0.f;
-        if (p.some) CkptVec<T, EPT>::load(x + p.at, v);
-        unsigned top = 0;
+        for (int u = 0; u < U; ++u) {
+            const long long b = b0 + u * (32 / LPB);
+            const B p(b, blocks, sub, C, nb, whole);
+            s[u] = b < blocks ? __ldg(scales + b) : 0u;
 #pragma unroll
-        for (int i = 0; i < EPT; ++i) top = max(top, ckpt_magnitude(v[i]));
+            for (int i = 0; i < S; ++i) {
+                raw[u][i] = W{};
+                if (p.ok(i)) raw[u][i] = __ldg(reinterpret_cast<const W *>(codes + p.slot(i)));
+            }
+        }
 #pragma unroll
-        for (int d = 1; d < LPB; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-        const unsigned s = ckpt_scale_byte(top);
-        if (p.some) store_codes<EPT>(codes + p.at, v, ckpt_inverse(s), s);
-        if (sub == 0 && b < blocks) scales[b] = (uint8_t)s;
+        for (int u = 0; u < U; ++u) {
+            const B p(b0 + u * (32 / LPB), blocks, sub, C, nb, whole);
+            const float scale = ckpt_scale(s[u]);
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+                if (!p.ok(i)) continue;
+                float2 v[P];
+                if constexpr (E == 8) {
+                    const unsigned w[2] = {raw[u][i].x, raw[u][i].y};
+                    ckpt_decode_n<8>(w, scale, &v[0].x);
+                } else if constexpr (E == 4) {
+                    const unsigned w[1] = {raw[u][i]};
+                    ckpt_decode_n<4>(w, scale, &v[0].x);
+                } else {
+                    v[0] = make_float2((float)raw[u][i] * scale, 0.f);
+                }
+                *reinterpret_cast<typename B::raw_t *>(x + p.slot(i)) = B::Vec::put(v);
+            }
+        }
     }
 }
 
-template <typename T, int EPT>
-__global__ void __launch_bounds__(256) ckpt8_unpack_kernel(long long blocks, int C, int nb, const int8_t *__restrict__ codes,
-                                                           const uint8_t *__restrict__ scales, T *__restrict__ x) {
-    after_predecessor();
-    constexpr int LPB = kCkptBlock / EPT;
-    const long long stride = (long long)gridDim.x * (256 / LPB);
-    const int sub = threadIdx.x % LPB;
-    const bool whole = C == nb * kCkptBlock;
-    for (long long b = (long long)blockIdx.x * (256 / LPB) + threadIdx.x / LPB; b < blocks; b += stride) {
-        const CkptPlace p = ckpt_place<EPT>(b, sub, C, nb, whole);
-        if (!p.some) continue;
-        float v[EPT];
-        load_codes<EPT>(codes + p.at, ckpt_scale(__ldg(scales + b)), v);
-        CkptVec<T, EPT>::store(x + p.at, v);
-    }
-}
-
-// columns per thread for these sizes and addresses
-static int ckpt_ept(int32_t C, sar_dtype t, const void *x, const void *codes) {
+// columns per access for these sizes and addresses
+static int ckpt_width(int32_t C, sar_dtype t, const void *x, const void *codes) {
     const size_t es = sar_elem_size(t);
-    for (int ept : {8, 4})
-        if (C % ept == 0 && sar_aligned(x, ept * es < 16 ? ept * es : 16) && sar_aligned(codes, ept)) return ept;
+    for (int e : {8, 4})
+        if (e * es <= 16 && C % e == 0 && sar_aligned(x, e * es) && sar_aligned(codes, e)) return e;
     return 1;
 }
 
 template <typename T, typename Fn>
-static sar_status ckpt_launch(int ept, Fn &&f) {
-    if (ept == 8) return f(Cfg<T, 8, 0, 0>{});
-    if (ept == 4) return f(Cfg<T, 4, 0, 0>{});
-    return f(Cfg<T, 1, 0, 0>{});
+static sar_status ckpt_dispatch(int e, Fn &&f) {
+    if constexpr (sizeof(T) == 2) {
+        if (e == 8) return f(Cfg<T, 8, 1, 0>{});
+    }
+    if (e == 4) return f(Cfg<T, 4, 2, 0>{});
+    return f(Cfg<T, 1, 4, 0>{});
 }
 
 static sar_status ckpt_check(int64_t n, int32_t C, sar_dtype t, const void *x, const void *codes, const void *scales) {
@@ -160,9 +173,10 @@ static sar_status ckpt_check(int64_t n, int32_t C, sar_dtype t, const void *x, c
     return check_elem_align({x}, sar_elem_size(t));
 }
 
-static unsigned ckpt_grid(long long blocks, int ept) {
-    const long long per = 256 / (kCkptBlock / ept), want = (blocks + per - 1) / per;
-    return (unsigned)(want < 148 * 64 ? want : 148 * 64);
+// blocks of 256 threads for so many blocks of columns, per warp and step `per`: as many as run at once walk the array
+static unsigned ckpt_grid(long long blocks, int per) {
+    const long long want = (blocks + 8ll * per - 1) / (8ll * per);
+    return (unsigned)(want < 148 * 4 ? want : 148 * 4);
 }
 
 }  // namespace sar
@@ -175,32 +189,32 @@ sar_status sar_ckpt8_pack(int64_t n, int32_t C, sar_dtype t, const void *x, int8
     SAR_TRY(ckpt_check(n, C, t, x, codes, scales));
     if (n == 0) return SAR_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int nb = (int)ckpt_blocks(C), ept = ckpt_ept(C, t, x, codes);
+    const int nb = (int)ckpt_blocks(C), e = ckpt_width(C, t, x, codes);
     const long long blocks = n * nb;
     auto go = [&](auto cfg) -> sar_status {
         using K = decltype(cfg);
         using T = typename K::type;
-        SAR_LAUNCH("ckpt8_pack", st, launch_if(n * C <= kOverlapElems, ckpt8_pack_kernel<T, K::g>, ckpt_grid(blocks, ept), 256, 0, st, blocks, C, nb,
-                                               static_cast<const T *>(x), codes, scales));
+        SAR_LAUNCH("ckpt8_pack", st, launch_if(n * C <= kOverlapElems, ckpt8_pack_kernel<T, K::g, K::v>, ckpt_grid(blocks, K::g * K::v * ckpt_ahead<T, K::g, K::v>), 256, 0, st,
+                                               blocks, C, row_divide(nb), static_cast<const T *>(x), codes, scales));
         return sar_after_launch();
     };
-    return t == SAR_F32 ? ckpt_launch<float>(ept, go) : ckpt_launch<__nv_bfloat16>(ept, go);
+    return t == SAR_F32 ? ckpt_dispatch<float>(e, go) : ckpt_dispatch<__nv_bfloat16>(e, go);
 }
 
 sar_status sar_ckpt8_unpack(int64_t n, int32_t C, sar_dtype t, const int8_t *codes, const uint8_t *scales, void *x, void *stream) {
     SAR_TRY(ckpt_check(n, C, t, x, codes, scales));
     if (n == 0) return SAR_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int nb = (int)ckpt_blocks(C), ept = ckpt_ept(C, t, x, codes);
+    const int nb = (int)ckpt_blocks(C), e = ckpt_width(C, t, x, codes);
     const long long blocks = n * nb;
     auto go = [&](auto cfg) -> sar_status {
         using K = decltype(cfg);
         using T = typename K::type;
-        SAR_LAUNCH("ckpt8_unpack", st, launch_if(n * C <= kOverlapElems, ckpt8_unpack_kernel<T, K::g>, ckpt_grid(blocks, ept), 256, 0, st, blocks, C, nb,
-                                                 codes, scales, static_cast<T *>(x)));
+        SAR_LAUNCH("ckpt8_unpack", st, launch_if(n * C <= kOverlapElems, ckpt8_unpack_kernel<T, K::g, K::v>, ckpt_grid(blocks, K::g * K::v * ckpt_ahead<T, K::g, K::v>), 256, 0, st,
+                                                 blocks, C, row_divide(nb), codes, scales, static_cast<T *>(x)));
         return sar_after_launch();
     };
-    return t == SAR_F32 ? ckpt_launch<float>(ept, go) : ckpt_launch<__nv_bfloat16>(ept, go);
+    return t == SAR_F32 ? ckpt_dispatch<float>(e, go) : ckpt_dispatch<__nv_bfloat16>(e, go);
 }
 
 }  // extern "C"

@@ -8,8 +8,52 @@
 #pragma once
 
 #include "sar_common.cuh"
+#include "sar_device.cuh"
 
 namespace sar {
+
+// E consecutive columns of a row of type T in one access, as pairs of float32
+template <typename T, int E>
+struct ColVec;
+template <>
+struct ColVec<float, 4> {
+    using type = float4;
+    __device__ __forceinline__ static void get(const float4 &r, float2 (&x)[2]) { x[0] = make_float2(r.x, r.y), x[1] = make_float2(r.z, r.w); }
+    __device__ __forceinline__ static float4 put(const float2 (&x)[2]) { return make_float4(x[0].x, x[0].y, x[1].x, x[1].y); }
+};
+template <>
+struct ColVec<__nv_bfloat16, 8> {
+    using type = uint4;
+    __device__ __forceinline__ static void get(const uint4 &r, float2 (&x)[4]) { Pairs<__nv_bfloat16>::get(r, x); }
+    __device__ __forceinline__ static uint4 put(const float2 (&x)[4]) {
+        using B = Elem<__nv_bfloat16>;
+        return make_uint4(B::pack2(x[0].x, x[0].y), B::pack2(x[1].x, x[1].y), B::pack2(x[2].x, x[2].y), B::pack2(x[3].x, x[3].y));
+    }
+};
+template <>
+struct ColVec<__nv_bfloat16, 4> {
+    using type = uint2;
+    __device__ __forceinline__ static void get(const uint2 &r, float2 (&x)[2]) {
+        x[0] = make_float2(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u));
+        x[1] = make_float2(__uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u));
+    }
+    __device__ __forceinline__ static uint2 put(const float2 (&x)[2]) {
+        using B = Elem<__nv_bfloat16>;
+        return make_uint2(B::pack2(x[0].x, x[0].y), B::pack2(x[1].x, x[1].y));
+    }
+};
+template <>   // one column: the second of the pair is zero throughout
+struct ColVec<float, 1> {
+    using type = float;
+    __device__ __forceinline__ static void get(float r, float2 (&x)[1]) { x[0] = make_float2(r, 0.f); }
+    __device__ __forceinline__ static float put(const float2 (&x)[1]) { return x[0].x; }
+};
+template <>
+struct ColVec<__nv_bfloat16, 1> {
+    using type = unsigned short;
+    __device__ __forceinline__ static void get(unsigned short r, float2 (&x)[1]) { x[0] = make_float2(__uint_as_float((unsigned)r << 16), 0.f); }
+    __device__ __forceinline__ static unsigned short put(const float2 (&x)[1]) { return __bfloat16_as_ushort(__float2bfloat16_rn(x[0].x)); }
+};
 
 constexpr int kCkptBlock = SAR_CKPT8_BLOCK;   // columns that share a scale
 
@@ -45,6 +89,19 @@ template <int N>   // N codes (a multiple of 4, or 1) -> N values
 __device__ __forceinline__ void ckpt_decode_n(const unsigned (&w)[(N + 3) / 4], float scale, float *x) {
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = ckpt_decode(w[i / 4] ^ 0x80808080u, i & 3) * scale;
+}
+
+// 8 codes -> 8 values in bf16, which holds them exactly (two codes in a pass: two packed operations and a conversion)
+__device__ __forceinline__ void ckpt_decode_bf16(const unsigned (&w)[2], float scale, uint32_t (&b)[4]) {
+    const float2 s = make_float2(scale, scale), shift = make_float2(-8388736.f, -8388736.f);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const unsigned flipped = w[q / 2] ^ 0x80808080u;
+        const float2 raw = make_float2(__uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7540u | (2 * q & 3))),
+                                       __uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7540u | ((2 * q + 1) & 3))));
+        const float2 v = __fmul2_rn(__fadd2_rn(raw, shift), s);
+        b[q] = Elem<__nv_bfloat16>::pack2(v.x, v.y);
+    }
 }
 
 static inline int64_t ckpt_blocks(int32_t C) { return ((int64_t)C + kCkptBlock - 1) / kCkptBlock; }

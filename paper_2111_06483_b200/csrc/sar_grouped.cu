@@ -5,6 +5,7 @@
 //                                     that it meets is a partial result, and a second launch adds them up
 // bf16 operands, tensor-core products (tcgen05) with float32 sums in tensor memory, operands staged by tiled copies.
 #include "sar_ckpt8.cuh"
+#include "sar_device.cuh"
 #include "sar_dispatch.cuh"
 #include "sar_tc.cuh"
 
@@ -151,17 +152,19 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
         }
     }
 
+    // all lanes of a warp walk its role's loop and wait; one of them issues
     if (warp == 0) {
-        if (lane == 0) {
-            uint32_t use = 0, set = 0;   // stages and sets of weights used so far
-            int g = g0, held = -1;
-            bool ok = true;
-            for (int t = t0; ok && t < t1; ++t) {
-                while (t >= sh.table.tiles[g + 1]) ++g;
-                if (p.slots && g != held) {
-                    const uint32_t slot = set % p.slots, bar = smem_addr(&sh.w_full[slot]);
-                    ok = set < (uint32_t)p.slots || bar_wait(smem_addr(&sh.w_empty[slot]), (set / p.slots + 1) & 1, failed);
-                    if (!ok) break;
+        RingPlace st, ws;   // in the ring of stages, among the sets of weights
+        uint32_t use = 0, set = 0;   // stages and sets filled so far
+        int g = g0, held = -1;
+        bool ok = true;
+        for (int t = t0; ok && t < t1; ++t) {
+            while (t >= sh.table.tiles[g + 1]) ++g;
+            if (p.slots && g != held) {
+                const uint32_t slot = ws.at, bar = smem_addr(&sh.w_full[slot]);
+                ok = warp_wait(smem_addr(&sh.w_empty[slot]), ws.round ^ 1, failed);
+                if (!ok) break;
+                if (one_lane()) {
                     bar_expect(bar, w_set);
                     for (int k = 0; k < p.steps; ++k) {
                         const uint32_t at = weights + slot * w_set + k * w_step;
@@ -169,14 +172,18 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
                         else
                             for (int c = 0; c < panels; ++c) tile_load_3d(at + c * kPanel, &p.w, n0 + c * 64, k * kStep, g, bar);
                     }
-                    held = g;
-                    ++set;
                 }
-                const int row = sh.table.first[g] + (t - sh.table.tiles[g]) * kTileRows;
-                for (int k = 0; k < p.steps; ++k, ++use) {
-                    const uint32_t s = use % p.stages, bar = smem_addr(&sh.full[s]), at = ring + s * stage_bytes;
-                    ok = use < (uint32_t)p.stages || bar_wait(smem_addr(&sh.empty[s]), (use / p.stages + 1) & 1, failed);
-                    if (!ok) break;
+                __syncwarp();
+                held = g;
+                ++set;
+                ws.next(p.slots);
+            }
+            const int row = sh.table.first[g] + (t - sh.table.tiles[g]) * kTileRows;
+            for (int k = 0; k < p.steps; ++k, ++use, st.next(p.stages)) {
+                const uint32_t s = st.at, bar = smem_addr(&sh.full[s]), at = ring + s * stage_bytes;
+                ok = warp_wait(smem_addr(&sh.empty[s]), st.round ^ 1, failed);
+                if (!ok) break;
+                if (one_lane()) {
                     bar_expect(bar, stage_bytes);
                     tile_load_2d(at, &p.a, k * kStep, row, bar);
                     if (!p.slots) {
@@ -186,58 +193,63 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
                             for (int c = 0; c < panels; ++c) tile_load_3d(b + c * kPanel, &p.w, n0 + c * 64, k * kStep, g, bar);
                     }
                 }
-            }
-            if (!ok) {   // the copies in flight end before the block does
-                for (uint32_t s = 0; s < (uint32_t)p.stages && s < use; ++s) bar_drain(smem_addr(&sh.full[s]), ((use - 1 - s) / p.stages) & 1);
-                for (uint32_t s = 0; s < (uint32_t)p.slots && s < set; ++s) bar_drain(smem_addr(&sh.w_full[s]), ((set - 1 - s) / p.slots) & 1);
+                __syncwarp();
             }
         }
+        if (!ok) {   // the copies in flight end before the block does
+            for (uint32_t s = 0; s < (uint32_t)p.stages && s < use; ++s) bar_drain(smem_addr(&sh.full[s]), ((use - 1 - s) / p.stages) & 1);
+            for (uint32_t s = 0; s < (uint32_t)p.slots && s < set; ++s) bar_drain(smem_addr(&sh.w_full[s]), ((set - 1 - s) / p.slots) & 1);
+        }
     } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t instr = tc_instr((cols + 15) & ~15, false, !WT);
-            uint32_t use = 0, set = 0;
-            int g = g0, held = -1;
-            bool ok = true;
-            for (int t = t0; ok && t < t1; ++t) {
-                const uint32_t i = t - t0, buf = i & 1;
-                while (t >= sh.table.tiles[g + 1]) ++g;
-                if (p.slots && g != held) {
-                    if (held >= 0) tc_commit(smem_addr(&sh.w_empty[(set - 1) % p.slots]));   // all products with the last set
-                    ok = bar_wait(smem_addr(&sh.w_full[set % p.slots]), (set / p.slots) & 1, failed);
-                    if (!ok) break;
-                    held = g;
-                    ++set;
+        const uint32_t instr = tc_instr((cols + 15) & ~15, false, !WT);
+        RingPlace st, ws, acc;
+        uint32_t wset = 0;
+        int g = g0, held = -1;
+        bool ok = true;
+        for (int t = t0; ok && t < t1; ++t, acc.next(2)) {
+            while (t >= sh.table.tiles[g + 1]) ++g;
+            if (p.slots && g != held) {
+                if (held >= 0) {
+                    if (one_lane()) tc_commit(smem_addr(&sh.w_empty[ws.at]));   // all products with the last set
+                    __syncwarp();
+                    ws.next(p.slots);
                 }
-                ok = i < 2 || bar_wait(smem_addr(&sh.acc_empty[buf]), (i / 2 + 1) & 1, failed);
+                ok = warp_wait(smem_addr(&sh.w_full[ws.at]), ws.round, failed);
                 if (!ok) break;
-                tc_after_sync();
-                const uint32_t wset = weights + (p.slots ? (set - 1) % p.slots * w_set : 0);
-                for (int k = 0; k < p.steps; ++k, ++use) {
-                    const uint32_t s = use % p.stages, at = ring + s * stage_bytes;
-                    ok = bar_wait(smem_addr(&sh.full[s]), (use / p.stages) & 1, failed);
-                    if (!ok) break;
-                    tc_after_sync();
-                    const uint32_t b = p.slots ? wset + k * w_step : at + kTileRows * 128;
-                    const int left = (min(kStep, p.K - k * kStep) + 15) / 16;   // copies fill what lies beyond K with zeros
-                    for (int j = 0; j < left; ++j) {
-                        const uint64_t da = tc_operand(at + j * 32, 16, 1024);
-                        const uint64_t db = WT ? tc_operand(b + j * 32, 16, 1024) : tc_operand(b + j * 2048, kPanel, 1024);
-                        tc_mma(tmem + buf * 256, da, db, instr, k > 0 || j > 0);
-                    }
-                    tc_commit(smem_addr(&sh.empty[s]));
-                }
-                if (ok) tc_commit(smem_addr(&sh.acc_full[buf]));
+                wset = weights + ws.at * w_set;
+                held = g;
             }
+            ok = warp_wait(smem_addr(&sh.acc_empty[acc.at]), acc.round ^ 1, failed);
+            if (!ok) break;
+            tc_after_sync();
+            const uint32_t d = tmem + acc.at * 256;
+            for (int k = 0; k < p.steps; ++k, st.next(p.stages)) {
+                const uint32_t at = ring + st.at * stage_bytes, b = p.slots ? wset + k * w_step : at + kTileRows * 128;
+                ok = warp_wait(smem_addr(&sh.full[st.at]), st.round, failed);
+                if (!ok) break;
+                const int left = (min(kStep, p.K - k * kStep) + 15) / 16;   // copies fill what lies beyond K with zeros
+                if (one_lane()) {
+                    const uint64_t da = tc_operand(at, 16, 1024), db = tc_operand(b, WT ? 16 : kPanel, 1024);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (j < left) tc_mma(d, tc_advance(da, j * 32), tc_advance(db, j * (WT ? 32 : 2048)), instr, k > 0 || j > 0);
+                    tc_commit(smem_addr(&sh.empty[st.at]));
+                }
+                __syncwarp();
+            }
+            if (ok && one_lane()) tc_commit(smem_addr(&sh.acc_full[acc.at]));
+            __syncwarp();
         }
     } else {
         const int quad = warp & 3;   // the lanes of tensor memory that this warp may read
         const uint32_t stage = base + (warp - 2) * 2 * kStoreBuf;
         uint32_t stored = 0;
+        RingPlace acc;
         int g = g0;
-        for (int t = t0; t < t1; ++t) {
-            const uint32_t i = t - t0, buf = i & 1;
+        for (int t = t0; t < t1; ++t, acc.next(2)) {
+            const uint32_t buf = acc.at;
             while (t >= sh.table.tiles[g + 1]) ++g;
-            if (!bar_wait(smem_addr(&sh.acc_full[buf]), (i / 2) & 1, failed)) break;
+            if (!warp_wait(smem_addr(&sh.acc_full[buf]), acc.round, failed)) break;
             tc_after_sync();
             const int row = sh.table.first[g] + (t - sh.table.tiles[g]) * kTileRows + quad * 32;
             const int rows = min(32, sh.table.first[g + 1] - row);   // may be <= 0
@@ -247,11 +259,14 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
                 __syncwarp();
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float x[32];
-                    tmem_load32(tmem + buf * 256 + c + h * 32 + ((uint32_t)(quad * 32) << 16), x);
+                    uint32_t x[32];
+                    tmem_ask(tmem + buf * 256 + c + h * 32 + ((uint32_t)(quad * 32) << 16), x);
+                    tmem_wait_load(x);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const float(&v)[8] = *reinterpret_cast<const float(*)[8]>(x + q * 8);
+                        float v[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(x[q * 8 + e]);
                         const uint4 r = Elem<__nv_bfloat16>::pack(v);
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + lane * 128 + (((h * 4 + q) ^ (lane & 7)) << 4)), "r"(r.x),
                                      "r"(r.y), "r"(r.z), "r"(r.w)
@@ -303,7 +318,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
 //
 // The tensor cores add to a float32 sum by cutting off what does not fit: every step of 16 rows takes up to one unit of the last
 // place towards zero, and 16,384 rows in one sum are 2e-5 to 3e-5 off (256 rows 2e-7, 1,024 rows 1e-6, 65,536 rows 8e-5 and
-// more).  So a sum runs over kRunRows rows at most; then four warps add it, rounding to nearest, to sums that lie beside it
+// more).  So a sum runs over kRunRows rows at most; then eight warps add it, rounding to nearest, to sums that lie beside it
 // in tensor memory (128 x 256 sums would take half of the register file).
 //
 // With a checkpoint eight more warps make the first operand: codes times scale, exact in bf16, written where a copy would have put
@@ -317,7 +332,7 @@ struct WeightArgs {
     const int8_t *codes;
     const uint8_t *scales;
     float *part;     // [chunks + G][d_in][d_out]: chunk c's part of group g in record c + g (along the way both only grow)
-    float *sums;     // [chunks + G][2 m_tiles][d_out]: sums of dz's columns, a share of the rows each, or null
+    float *sums;     // [chunks + G][kSumShares m_tiles][d_out]: sums of dz's columns, a share of the rows each, or null
     int *flag;
     int n, G, d_in, d_out, nb;
     int cols;        // of a tile (a multiple of 64 up to 256)
@@ -325,7 +340,8 @@ struct WeightArgs {
     int chunk_rows;  // a multiple of 64
     int stages;
 };
-constexpr int kAdders = 4, kMakers = 8;   // warps
+constexpr int kAdders = 8, kMakers = 8;   // warps
+constexpr int kSumShares = kMakers / 4;    // of a column's sum: a part of every step's rows each
 constexpr int kWeightThreads = 64 + kAdders * 32, kWeightThreads8 = kWeightThreads + kMakers * 32;
 constexpr uint32_t kSumCols = 256;        // where the sums lie in tensor memory, behind the accumulators
 struct WeightShared {
@@ -389,45 +405,45 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     };
 
     if (warp == 0) {
-        if (lane == 0) {
-            uint32_t use = 0;
-            bool ok = true;
-            for (int g = g0; ok && more(g); ++g) {
-                int lo, hi;
-                if (!segment(g, lo, hi)) continue;
-                for (int r = lo; r < hi; r += kStep, ++use) {
-                    const uint32_t s = use % p.stages, bar = smem_addr(&sh.full[s]), at = ring + s * stage_bytes;
-                    ok = use < (uint32_t)p.stages || bar_wait(smem_addr(&sh.empty[s]), (use / p.stages + 1) & 1, failed);
-                    if (!ok) break;
+        RingPlace st;
+        uint32_t use = 0;
+        bool ok = true;
+        for (int g = g0; ok && more(g); ++g) {
+            int lo, hi;
+            if (!segment(g, lo, hi)) continue;
+            for (int r = lo; r < hi; r += kStep, ++use, st.next(p.stages)) {
+                const uint32_t s = st.at, bar = smem_addr(&sh.full[s]), at = ring + s * stage_bytes;
+                ok = warp_wait(smem_addr(&sh.empty[s]), st.round ^ 1, failed);
+                if (!ok) break;
+                if (one_lane()) {
                     bar_expect(bar, ((CK ? 0 : h_panels) + panels) * kPanel);
                     if (!CK)
                         for (int c = 0; c < h_panels; ++c) tile_load_2d(at + c * kPanel, &p.h, m0 + c * 64, r, bar);
                     for (int c = 0; c < panels; ++c) tile_load_2d(at + (2 + c) * kPanel, &p.dz, n0 + c * 64, r, bar);
                 }
+                __syncwarp();
             }
-            if (!ok)
-                for (uint32_t s = 0; s < (uint32_t)p.stages && s < use; ++s) bar_drain(smem_addr(&sh.full[s]), ((use - 1 - s) / p.stages) & 1);
         }
-    } else if (warp == 1) {   // all lanes wait, the first one issues
+        if (!ok)
+            for (uint32_t s = 0; s < (uint32_t)p.stages && s < use; ++s) bar_drain(smem_addr(&sh.full[s]), ((use - 1 - s) / p.stages) & 1);
+    } else if (warp == 1) {
         const uint32_t instr = tc_instr((cols + 15) & ~15, true, true);
-        uint32_t use = 0, run = 0;
+        RingPlace st, acc;
         bool ok = true;
         for (int g = g0; ok && more(g); ++g) {
             int lo, hi;
             if (!segment(g, lo, hi)) continue;
-            for (int r0 = lo; ok && r0 < hi; r0 += kRunRows, ++run) {
-                const uint32_t buf = run % bufs;
-                ok = run < bufs || bar_wait(smem_addr(&sh.acc_empty[buf]), (run / bufs + 1) & 1, failed);
-                ok = __all_sync(0xffffffffu, ok);
+            for (int r0 = lo; ok && r0 < hi; r0 += kRunRows, acc.next(bufs)) {
+                const uint32_t buf = acc.at;
+                ok = warp_wait(smem_addr(&sh.acc_empty[buf]), acc.round ^ 1, failed);
                 if (!ok) break;
                 tc_after_sync();
                 const int r1 = min(hi, r0 + kRunRows);
-                for (int r = r0; r < r1; r += kStep, ++use) {
-                    const uint32_t s = use % p.stages, at = ring + s * stage_bytes;
+                for (int r = r0; r < r1; r += kStep, st.next(p.stages)) {
+                    const uint32_t s = st.at, at = ring + s * stage_bytes;
                     const int rows = min(kStep, hi - r);
-                    ok = bar_wait(smem_addr(&sh.full[s]), (use / p.stages) & 1, failed);
-                    if (CK) ok = ok && bar_wait(smem_addr(&sh.made[s]), (use / p.stages) & 1, failed);
-                    ok = __all_sync(0xffffffffu, ok);
+                    ok = warp_wait(smem_addr(&sh.full[s]), st.round, failed);
+                    if (CK) ok = ok && warp_wait(smem_addr(&sh.made[s]), st.round, failed);
                     if (!ok) break;
                     if (!CK && rows % 16) {
                         clear(at, rows, 0, h_panels, lane, 32);
@@ -435,43 +451,46 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                         async_proxy_fence();
                         __syncwarp();
                     }
-                    tc_after_sync();
-                    if (lane == 0) {
-                        for (int j = 0; j < (rows + 15) / 16; ++j)
-                            tc_mma(tmem + buf * 128, tc_operand(at + j * 2048, kPanel, 1024), tc_operand(at + 2 * kPanel + j * 2048, kPanel, 1024), instr, r > r0 || j > 0);
+                    if (one_lane()) {
+                        const uint64_t da = tc_operand(at, kPanel, 1024), db = tc_operand(at + 2 * kPanel, kPanel, 1024);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (j * 16 < rows) tc_mma(tmem + buf * 128, tc_advance(da, j * 2048), tc_advance(db, j * 2048), instr, r > r0 || j > 0);
                         tc_commit(smem_addr(&sh.empty[s]));
                     }
+                    __syncwarp();
                 }
-                if (ok && lane == 0) tc_commit(smem_addr(&sh.acc_full[buf]));
+                if (ok && one_lane()) tc_commit(smem_addr(&sh.acc_full[buf]));
+                __syncwarp();
             }
         }
     } else if (warp < 2 + kAdders) {
-        const uint32_t quad = warp & 3, lanes = quad * 32 << 16;   // rows m0 + 32 quad + lane of dW
+        const uint32_t quad = warp & 3, part = (warp - 2) / 4, lanes = quad * 32 << 16;   // rows m0 + 32 quad + lane of dW, every other 32 columns
         const int m = m0 + quad * 32 + lane;
-        uint32_t run = 0;
+        RingPlace acc;
         bool ok = true;
         for (int g = g0; ok && more(g); ++g) {
             int lo, hi;
             if (!segment(g, lo, hi)) continue;
             float *out = p.part + ((long long)(chunk + g) * p.d_in + m) * p.d_out + n0;
-            for (int r0 = lo; r0 < hi; r0 += kRunRows, ++run) {
-                const uint32_t buf = run % bufs;
-                ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&sh.acc_full[buf]), (run / bufs) & 1, failed));
+            for (int r0 = lo; r0 < hi; r0 += kRunRows, acc.next(bufs)) {
+                const uint32_t buf = acc.at;
+                ok = warp_wait(smem_addr(&sh.acc_full[buf]), acc.round, failed);
                 if (!ok) break;
                 tc_after_sync();
                 const bool first = r0 == lo, last = r0 + kRunRows >= hi;
-                for (int c = 0; c < cols; c += 32) {
+                for (int c = part * 32; c < cols; c += kAdders / 4 * 32) {
                     uint32_t x[32], y[32];
-                    tmem_ask32(tmem + buf * 128 + c + lanes, x);
-                    if (!first) tmem_ask32(tmem + kSumCols + c + lanes, y);
+                    tmem_ask(tmem + buf * 128 + c + lanes, x);
+                    if (!first) tmem_ask(tmem + kSumCols + c + lanes, y);
                     tmem_wait_load(x);
                     if (!first) {
-                        tmem_tie32(y);
+                        tmem_tie(y);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) + __uint_as_float(y[e]));
                     }
                     if (!last) {
-                        tmem_store32(tmem + kSumCols + c + lanes, x);
+                        tmem_store(tmem + kSumCols + c + lanes, x);
                     } else if (m < p.d_in) {
 #pragma unroll
                         for (int q = 0; q < 8; ++q)
@@ -487,29 +506,35 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     } else if constexpr (CK) {
         const int w = warp - 2 - kAdders, me = w * 32 + lane;
         // the part of h: 8 columns of four rows a step and thread, asked for kAhead steps before they are used
-        constexpr int kAhead = 3;
+        constexpr int kAhead = 3, kRows = kStep / (kMakers * 2);
         const int hc = me & 15, hr = me >> 4;
-        uint2 code[kAhead][4];
-        unsigned scale[kAhead][4];
+        uint2 code[kAhead][kRows];
+        unsigned scale[kAhead][kRows];
         const bool h_cols = m0 + hc * 8 < p.d_in;
-        const auto ask = [&](uint2 (&code)[4], unsigned (&scale)[4], int r, int hi) {
+        const int8_t *codes = p.codes + (m0 + hc * 8);
+        const uint8_t *scales = p.scales + (m0 + hc * 8) / kCkptBlock;
+        const auto ask = [&](uint2 (&code)[kRows], unsigned (&scale)[kRows], int r, int hi) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = r + hr + 16 * i;
+            for (int i = 0; i < kRows; ++i) {
+                const int row = r + hr + 2 * kMakers * i;
                 code[i] = make_uint2(0u, 0u);
                 scale[i] = 0;
                 if (h_cols && row < hi) {
-                    code[i] = __ldg(reinterpret_cast<const uint2 *>(p.codes + (long long)row * p.d_in + m0 + hc * 8));
-                    scale[i] = __ldg(p.scales + (long long)row * p.nb + (m0 + hc * 8) / kCkptBlock);
+                    code[i] = __ldg(reinterpret_cast<const uint2 *>(codes + (long long)row * p.d_in));
+                    scale[i] = __ldg(scales + (long long)row * p.nb);
                 }
             }
         };
-        // the column sums: 8 columns of every fourth row of one half of a step, the steps shared by the blocks of a chunk
+        uint32_t h_at[kRows];   // where they go in a stage
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) h_at[i] = (hc >> 3) * kPanel + (hr + 2 * kMakers * i) * 128 + (((hc & 7) ^ ((hr + 2 * kMakers * i) & 7)) << 4);
+        // The column sums: 8 columns of every fourth row of one share of a step, the steps shared by the blocks of a chunk.
+        // A thread's rows of a step are 4 apart, so that their chunks lie at one of two places of the swizzle.
         const bool want_sums = p.sums != nullptr && (w & 3) < panels;
-        const int half = w >> 2;
-        const uint32_t sum_at = (2 + (w & 3)) * kPanel + (half * 32 + (lane >> 3)) * 128;
-        float cs[8];
-        uint32_t use = 0;
+        const int share = w >> 2, row0 = share * (kStep / kSumShares) + (lane >> 3);
+        const uint32_t sum_at = (2 + (w & 3)) * kPanel + row0 * 128, even = ((lane & 7) ^ (row0 & 7)) << 4, odd = ((lane & 7) ^ ((row0 + 4) & 7)) << 4;
+        float2 cs[4];
+        RingPlace st;
         bool ok = true;
         for (int g = g0; ok && more(g); ++g) {
             int lo, hi;
@@ -517,72 +542,70 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
 #pragma unroll
             for (int d = 0; d < kAhead; ++d) ask(code[d], scale[d], lo + d * kStep, hi);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) cs[e] = 0.f;
-            int step = 0;
+            for (int e = 0; e < 4; ++e) cs[e] = make_float2(0.f, 0.f);
+            int turn = 0;   // the step's number modulo the tiles that share the sums
             for (int r3 = lo; ok && r3 < hi; r3 += kAhead * kStep) {
 #pragma unroll
                 for (int d = 0; d < kAhead; ++d) {   // unrolled: the sets are registers
                     const int r = r3 + d * kStep;
                     if (r >= hi) break;
-                    const uint32_t s = use % p.stages, at = ring + s * stage_bytes;
+                    const uint32_t s = st.at, at = ring + s * stage_bytes;
                     const int rows = min(kStep, hi - r);
-                    ok = __all_sync(0xffffffffu, use < (uint32_t)p.stages || bar_wait(smem_addr(&sh.empty[s]), (use / p.stages + 1) & 1, failed));
+                    ok = warp_wait(smem_addr(&sh.empty[s]), st.round ^ 1, failed);
                     if (!ok) break;
                     if (h_cols) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int row = hr + 16 * i;
+                        for (int i = 0; i < kRows; ++i) {
                             const unsigned word[2] = {code[d][i].x, code[d][i].y};
-                            float v[8];
-                            ckpt_decode_n<8>(word, ckpt_scale(scale[d][i]), v);
-                            const uint4 b = Elem<__nv_bfloat16>::pack(v);
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + (hc >> 3) * kPanel + row * 128 + (((hc & 7) ^ (row & 7)) << 4)),
-                                         "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
-                                         : "memory");
+                            uint32_t b[4];
+                            ckpt_decode_bf16(word, ckpt_scale(scale[d][i]), b);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + h_at[i]), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
                         }
                     }
                     ask(code[d], scale[d], r + kAhead * kStep, hi);
-                    const bool sum = want_sums && step % p.m_tiles == m_tile;
+                    const bool sum = want_sums && turn == m_tile;
+                    if (++turn == p.m_tiles) turn = 0;
                     if (rows % 16 || sum) {
-                        ok = __all_sync(0xffffffffu, bar_wait(smem_addr(&sh.full[s]), (use / p.stages) & 1, failed));
+                        ok = warp_wait(smem_addr(&sh.full[s]), st.round, failed);
                         if (!ok) break;
                     }
                     if (rows % 16) clear(at, rows, 2, 2 + panels, me, kMakers * 32);   // h's rows are zeros already
                     async_proxy_fence();
                     if (sum) {
-                        float cr[8];   // a step's sums first: long sums of single values lose digits
+                        float2 cr[4];   // a step's sums first: long sums of single values lose digits
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) cr[e] = 0.f;
+                        for (int e = 0; e < 4; ++e) cr[e] = make_float2(0.f, 0.f);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int row = half * 32 + (lane >> 3) + 4 * i;
+                        for (int i = 0; i < kStep / kSumShares / 4; ++i) {
+                            if (rows < kStep && row0 + 4 * i >= rows) continue;
                             uint4 v;
-                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at + sum_at + i * 512 + (((lane & 7) ^ (row & 7)) << 4)));
-                            float x[8];
-                            Elem<__nv_bfloat16>::unpack(v, x);
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at + sum_at + i * 512 + (i & 1 ? odd : even)));
+                            float2 x[4];
+                            Pairs<__nv_bfloat16>::get(v, x);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) cr[e] += row < rows ? x[e] : 0.f;
+                            for (int e = 0; e < 4; ++e) cr[e] = __fadd2_rn(cr[e], x[e]);
                         }
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) cs[e] += cr[e];
+                        for (int e = 0; e < 4; ++e) cs[e] = __fadd2_rn(cs[e], cr[e]);
                     }
                     __syncwarp();
                     if (lane == 0) bar_arrive(smem_addr(&sh.made[s]));
-                    ++use;
-                    ++step;
+                    st.next(p.stages);
                 }
             }
             if (ok && want_sums) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    cs[e] += __shfl_xor_sync(0xffffffffu, cs[e], 8);
-                    cs[e] += __shfl_xor_sync(0xffffffffu, cs[e], 16);
-                }
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int d = 8; d < 32; d <<= 1) {
+                        cs[e].x += __shfl_xor_sync(0xffffffffu, cs[e].x, d);
+                        cs[e].y += __shfl_xor_sync(0xffffffffu, cs[e].y, d);
+                    }
                 const int col = (w & 3) * 64 + lane * 8;
                 if (lane < 8 && col < cols) {
-                    float4 *out = reinterpret_cast<float4 *>(p.sums + ((long long)(chunk + g) * 2 * p.m_tiles + m_tile * 2 + half) * p.d_out + n0 + col);
-                    out[0] = make_float4(cs[0], cs[1], cs[2], cs[3]);
-                    out[1] = make_float4(cs[4], cs[5], cs[6], cs[7]);
+                    float4 *out = reinterpret_cast<float4 *>(p.sums + ((long long)(chunk + g) * kSumShares * p.m_tiles + m_tile * kSumShares + share) * p.d_out + n0 + col);
+                    out[0] = make_float4(cs[0].x, cs[0].y, cs[1].x, cs[1].y);
+                    out[1] = make_float4(cs[2].x, cs[2].y, cs[3].x, cs[3].y);
                 }
             }
         }
@@ -595,56 +618,85 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     if (threadIdx.x == 0 && sh.failed && p.flag) *p.flag = 1;
 }
 
-// dW[g] = the sum of group g's records in the order of the chunks, times gamma, plus beta times the sums of dz's columns
-__global__ void __launch_bounds__(256) grouped_weight_reduce_kernel(const int64_t *__restrict__ offsets, int G, long long n, int d_in, int d_out, int chunk_rows,
-                                                                    int shares, const float *__restrict__ part, const float *__restrict__ sums,
+// The records of group g, for every thread of the block: from, from + 1, ... (the group's rows as group_table reads them: the largest
+// offset so far).
+struct Records {
+    long long from;
+    int count;
+};
+__device__ __forceinline__ Records group_records(const int64_t *__restrict__ offsets, int g, long long n, int chunk_rows) {
+    long long lo = 0;
+    if (offsets) {
+        for (int j = threadIdx.x & 31; j <= g; j += 32) lo = max(lo, (long long)__ldg(reinterpret_cast<const long long *>(offsets) + j));
+        for (int d = 16; d > 0; d >>= 1) lo = max(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+    }
+    lo = min(lo, n);
+    const long long hi = offsets ? min(max(lo, (long long)__ldg(reinterpret_cast<const long long *>(offsets) + g + 1)), n) : n;
+    const long long first = lo / chunk_rows;
+    return {first + g, hi > lo ? (int)((hi - 1) / chunk_rows - first) + 1 : 0};
+}
+
+// The column sums of a group's dz: its records' shares in order.  One launch ahead of the next kernel, which needs a sum in every
+// row of dW: added up there they are read d_in times.
+__global__ void __launch_bounds__(512) grouped_sums_reduce_kernel(const int64_t *__restrict__ offsets, long long n, int d_out, int chunk_rows, int shares,
+                                                                  const float *__restrict__ sums, float *__restrict__ total) {
+    after_predecessor();
+    const int g = blockIdx.y;
+    const Records r = group_records(offsets, g, n, chunk_rows);
+    __shared__ float red[16][33];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float acc = 0.f;
+    if (c < d_out) {
+#pragma unroll 4
+        for (int s = w; s < r.count * shares; s += 16) acc += sums[(r.from * shares + s) * d_out + c];
+    }
+    red[w][lane] = acc;
+    __syncthreads();
+    if (w != 0 || c >= d_out) return;
+#pragma unroll
+    for (int k = 1; k < 16; ++k) acc += red[k][lane];
+    total[(long long)g * d_out + c] = acc;
+}
+
+// dW[g] = the sum of group g's records in the order of the chunks, times gamma, plus beta times the sums of dz's columns.
+// 4 outputs a thread, 8 shares of the records.
+__global__ void __launch_bounds__(256) grouped_weight_reduce_kernel(const int64_t *__restrict__ offsets, long long n, int d_in, int d_out, int chunk_rows,
+                                                                    const float *__restrict__ part, const float *__restrict__ total,
                                                                     const float *__restrict__ gamma, const float *__restrict__ beta, float *__restrict__ dw) {
     after_predecessor();
     const int g = blockIdx.y;
-    __shared__ int from, count;
-    __shared__ float4 red[4][64];
-    if (threadIdx.x < 32 && threadIdx.y == 0) {
-        // the group's rows as group_table reads them: the largest offset so far
-        long long lo = 0, hi;
-        for (int j = threadIdx.x; offsets && j <= g; j += 32) lo = max(lo, (long long)offsets[j]);
-        for (int d = 16; d > 0; d >>= 1) lo = max(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-        lo = min(lo, n);
-        hi = offsets ? min(max(lo, (long long)offsets[g + 1]), n) : n;
-        if (threadIdx.x == 0) {
-            from = (int)(lo / chunk_rows);
-            count = hi > lo ? (int)((hi - 1) / chunk_rows) - from + 1 : 0;
-        }
-    }
-    __syncthreads();
-    const long long size = (long long)d_in * d_out, x = (blockIdx.x * 64ll + threadIdx.x) * 4;   // 4 outputs a thread, 4 shares of the records
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f), col = acc;
+    const Records r = group_records(offsets, g, n, chunk_rows);
+    __shared__ float4 red[8][32];
+    const int lane = threadIdx.x & 31, share = threadIdx.x >> 5;
+    const long long size = (long long)d_in * d_out, x = (blockIdx.x * 32ll + lane) * 4;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (x < size) {
-        const int c = (int)(x % d_out);
+        const float *at = part + r.from * size + x;
 #pragma unroll 4
-        for (int s = threadIdx.y; s < count; s += 4) {
-            const float4 v = *reinterpret_cast<const float4 *>(part + (from + s + g) * size + x);
+        for (int s = share; s < r.count; s += 8) {
+            const float4 v = *reinterpret_cast<const float4 *>(at + s * size);
             acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
-            if (sums) {
-                const float4 *u = reinterpret_cast<const float4 *>(sums + (long long)(from + s + g) * shares * d_out + c);
-                for (int i = 0; i < shares; ++i) col.x += u[i * (d_out / 4)].x, col.y += u[i * (d_out / 4)].y, col.z += u[i * (d_out / 4)].z, col.w += u[i * (d_out / 4)].w;
-            }
-        }
-        if (gamma) {
-            const float k = __ldg(gamma + x / d_out);
-            acc.x *= k, acc.y *= k, acc.z *= k, acc.w *= k;
-        }
-        if (sums) {
-            const float k = __ldg(beta + x / d_out);
-            acc.x = fmaf(k, col.x, acc.x), acc.y = fmaf(k, col.y, acc.y), acc.z = fmaf(k, col.z, acc.z), acc.w = fmaf(k, col.w, acc.w);
         }
     }
-    red[threadIdx.y][threadIdx.x] = acc;
+    red[share][lane] = acc;
     __syncthreads();
-    if (threadIdx.y == 0 && x < size) {
-        const float4 b = red[1][threadIdx.x], c = red[2][threadIdx.x], d = red[3][threadIdx.x];
-        *reinterpret_cast<float4 *>(dw + g * size + x) =
-            make_float4((acc.x + b.x) + (c.x + d.x), (acc.y + b.y) + (c.y + d.y), (acc.z + b.z) + (c.z + d.z), (acc.w + b.w) + (c.w + d.w));
+    if (share != 0 || x >= size) return;
+#pragma unroll
+    for (int k = 1; k < 8; ++k) {
+        const float4 v = red[k][lane];
+        acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
     }
+    const int row = (int)(x / d_out), c = (int)(x - (long long)row * d_out);
+    if (gamma) {
+        const float k = __ldg(gamma + row);
+        acc.x *= k, acc.y *= k, acc.z *= k, acc.w *= k;
+    }
+    if (total) {
+        const float k = __ldg(beta + row);
+        const float4 v = *reinterpret_cast<const float4 *>(total + (long long)g * d_out + c);
+        acc.x = fmaf(k, v.x, acc.x), acc.y = fmaf(k, v.y, acc.y), acc.z = fmaf(k, v.z, acc.z), acc.w = fmaf(k, v.w, acc.w);
+    }
+    *reinterpret_cast<float4 *>(dw + g * size + x) = acc;
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
@@ -678,9 +730,9 @@ static sar_status grouped_rows(int64_t n, int32_t groups, int K, int N, const in
     p.N = N;
     p.zero_rest = (flags & SAR_GROUPED_ZERO_REST) != 0;
     p.steps = (K + kStep - 1) / kStep;
-    // Weights stay in shared memory where 64 K of their elements are a slice of at least 128 columns: every row tile
-    // then costs the loads of its rows alone.  Longer contractions take both operands through the ring in slices of 256 columns.
-    const int widest = p.steps <= 4 ? 256 : p.steps <= 8 ? 128 : 256;
+    // Weights stay in shared memory where 128 KB hold a slice of at least 128 columns: every row tile then costs the loads of its
+    // rows alone.  Longer contractions take both operands through the ring in slices of 256 columns.
+    const int widest = p.steps <= 4 ? 256 : p.steps <= 8 ? 16 / p.steps * 64 : 256;
     p.slices = (N + widest - 1) / widest;
     p.cols = round_up_int((N + p.slices - 1) / p.slices, 64);
     p.slices = (N + p.cols - 1) / p.cols;
@@ -716,7 +768,7 @@ static sar_status grouped_rows(int64_t n, int32_t groups, int K, int N, const in
 
 struct WeightPlan {
     int cols, m_tiles, n_tiles, chunks, chunk_rows, stages;
-    size_t smem, part_bytes, sum_bytes;
+    size_t smem, part_bytes, sum_bytes, total_bytes;   // the scratch: records, their column sums, the groups' column sums
 };
 static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out) {
     WeightPlan w;
@@ -737,7 +789,8 @@ static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out) {
     w.stages = w.stages > kStagesMax ? kStagesMax : w.stages;
     w.smem = fixed + w.stages * stage;
     w.part_bytes = sar_round_up((size_t)(w.chunks + groups) * d_in * d_out * 4, 256);
-    w.sum_bytes = sar_round_up((size_t)(w.chunks + groups) * 2 * w.m_tiles * d_out * 4, 256);
+    w.sum_bytes = sar_round_up((size_t)(w.chunks + groups) * kSumShares * w.m_tiles * d_out * 4, 256);
+    w.total_bytes = sar_round_up((size_t)groups * d_out * 4, 256);
     return w;
 }
 
@@ -745,7 +798,7 @@ static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_
                                  const uint8_t *scales, const float *gamma, const float *beta, const void *dz, float *dw, int32_t *flag,
                                  void *workspace, size_t workspace_bytes, cudaStream_t st) {
     const WeightPlan w = weight_plan(n, groups, d_in, d_out);
-    if (!workspace || !sar_aligned(workspace, 16) || workspace_bytes < w.part_bytes + w.sum_bytes) return SAR_ERR_WORKSPACE;
+    if (!workspace || !sar_aligned(workspace, 16) || workspace_bytes < w.part_bytes + w.sum_bytes + w.total_bytes) return SAR_ERR_WORKSPACE;
     WeightArgs p{};
     p.offsets = offsets;
     p.codes = codes;
@@ -777,10 +830,18 @@ static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_
         SAR_LAUNCH("linear_grouped_bwd_weight_ckpt8", st, launch_if(overlap, grouped_weight_kernel<true>, blocks, kWeightThreads8, w.smem, st, p));
     }
     SAR_TRY(sar_after_launch());
+    float *total = nullptr;
+    if (beta) {
+        total = reinterpret_cast<float *>(static_cast<char *>(workspace) + w.part_bytes + w.sum_bytes);
+        SAR_LAUNCH("linear_grouped_sums_reduce", st,
+                   launch(grouped_sums_reduce_kernel, dim3((unsigned)((d_out + 31) / 32), (unsigned)groups), 512, 0, st, offsets, (long long)n, (int)d_out, w.chunk_rows,
+                          kSumShares * w.m_tiles, p.sums, total));
+        SAR_TRY(sar_after_launch());
+    }
     const long long quads = (long long)d_in * d_out / 4;
     SAR_LAUNCH("linear_grouped_bwd_weight_reduce", st,
-               launch(grouped_weight_reduce_kernel, dim3((unsigned)((quads + 63) / 64), (unsigned)groups), dim3(64, 4), 0, st, offsets, (int)groups, (long long)n,
-                      (int)d_in, (int)d_out, w.chunk_rows, 2 * w.m_tiles, p.part, p.sums, gamma, beta, dw));
+               launch(grouped_weight_reduce_kernel, dim3((unsigned)((quads + 31) / 32), (unsigned)groups), 256, 0, st, offsets, (long long)n, (int)d_in, (int)d_out,
+                      w.chunk_rows, p.part, total, gamma, beta, dw));
     return sar_after_launch();
 }
 
@@ -809,7 +870,7 @@ sar_status sar_linear_grouped_bwd_input(int64_t n, int32_t groups, int32_t d_in,
 size_t sar_linear_grouped_workspace_bytes(int64_t n, int32_t groups, int32_t d_in, int32_t d_out) {
     if (n < 1 || n > INT32_MAX || groups < 1 || d_in < 1 || d_out < 1) return 0;
     const WeightPlan w = weight_plan(n, groups, d_in, d_out);
-    return w.part_bytes + w.sum_bytes + 256;
+    return w.part_bytes + w.sum_bytes + w.total_bytes + 256;
 }
 
 static sar_status grouped_zero(int32_t groups, int32_t d_in, int32_t d_out, float *dw, void *stream) {
