@@ -14,6 +14,7 @@ namespace sar {
 constexpr int kTileRows = 128;      // rows of a product's tile: all lanes of tensor memory
 constexpr int kStep = 64;           // contraction per stage: 128 bytes of bf16
 constexpr int kPanel = 64 * 128;    // 64 rows of 128 bytes
+constexpr int kStepMost = 128;      // rows of a stage where they are the contraction
 constexpr int kGroupsMax = SAR_MAX_GROUPS;
 
 sar_status tc_tensor_map(CUtensorMap *map, const void *base, int rank, const uint64_t *dims, const uint32_t *box) {
@@ -99,6 +100,7 @@ struct RowsArgs {
     int steps;       // of 64 along the contraction
     int stages;      // of the ring
     int slots;       // sets of weights in shared memory; 0: they pass through the ring with the rows
+    int store_bufs;  // 2, or 1 where the ring needs the room
     int zero_rest;   // rows of no group are written as zeros
 };
 constexpr int kRowsThreads = 192;
@@ -120,7 +122,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
     const uint32_t w_set = (uint32_t)p.steps * w_step;
     const uint32_t base = (smem_addr(dyn) + (uint32_t)sizeof(RowsShared) + 1023u) & ~1023u;
     const uint32_t stage_bytes = kTileRows * 128 + (p.slots ? 0 : w_step);
-    const uint32_t ring = base + 8 * kStoreBuf, weights = ring + p.stages * stage_bytes;
+    const uint32_t ring = base + 4 * p.store_bufs * kStoreBuf, weights = ring + p.stages * stage_bytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *failed = &sh.failed;
 
@@ -242,7 +244,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
         }
     } else {
         const int quad = warp & 3;   // the lanes of tensor memory that this warp may read
-        const uint32_t stage = base + (warp - 2) * 2 * kStoreBuf;
+        const uint32_t stage = base + (warp - 2) * p.store_bufs * kStoreBuf;
         uint32_t stored = 0;
         RingPlace acc;
         int g = g0;
@@ -254,8 +256,9 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
             const int row = sh.table.first[g] + (t - sh.table.tiles[g]) * kTileRows + quad * 32;
             const int rows = min(32, sh.table.first[g + 1] - row);   // may be <= 0
             for (int c = 0; c < cols; c += 64, ++stored) {
-                const uint32_t at = stage + (stored & 1) * kStoreBuf;
-                store_wait_read<1>();   // lane 0's copy out of this buffer, two ago
+                const uint32_t at = stage + (p.store_bufs == 2 ? (stored & 1) * kStoreBuf : 0);
+                if (p.store_bufs == 2) store_wait_read<1>();   // lane 0's last copy out of this buffer
+                else store_wait_read<0>();
                 __syncwarp();
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -325,23 +328,24 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
 // them.  Its rows stand for gamma v + beta, and  (gamma v + beta)^T dz = gamma (v^T dz) + beta (column sums of dz):  gamma and
 // beta enter in float32 after the product instead of rounding every value, and the column sums are taken from the tiles of dz
 // that are in shared memory anyway.
-constexpr int kRunRows = 512;
+constexpr int kRunRows = 1024;
 struct WeightArgs {
     CUtensorMap h, dz;
     const int64_t *offsets;
     const int8_t *codes;
     const uint8_t *scales;
     float *part;     // [chunks + G][d_in][d_out]: chunk c's part of group g in record c + g (along the way both only grow)
-    float *sums;     // [chunks + G][kSumShares m_tiles][d_out]: sums of dz's columns, a share of the rows each, or null
+    float *sums;     // [chunks + G][2 m_tiles][d_out]: sums of dz's columns, a share of the rows each, or null
     int *flag;
     int n, G, d_in, d_out, nb;
     int cols;        // of a tile (a multiple of 64 up to 256)
     int m_tiles, n_tiles;
     int chunk_rows;  // a multiple of 64
     int stages;
+    int step;        // rows per stage: 64 or 128
+    int h_panels;    // of a stage: 2 with 64 rows, 1 with 128
 };
-constexpr int kAdders = 8, kMakers = 8;   // warps
-constexpr int kSumShares = kMakers / 4;    // of a column's sum: a part of every step's rows each
+constexpr int kAdders = 8, kMakers = 8;   // warps; the adders' work is laid out for 8
 constexpr int kWeightThreads = 64 + kAdders * 32, kWeightThreads8 = kWeightThreads + kMakers * 32;
 constexpr uint32_t kSumCols = 256;        // where the sums lie in tensor memory, behind the accumulators
 struct WeightShared {
@@ -358,14 +362,15 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     WeightShared &sh = *reinterpret_cast<WeightShared *>(dyn);
     const uint32_t ring = (smem_addr(dyn) + (uint32_t)sizeof(WeightShared) + 1023u) & ~1023u;
     const int panels = p.cols / 64;
-    const uint32_t stage_bytes = (2 + panels) * kPanel;
+    const uint32_t panel = p.step * 128, stage_bytes = (p.h_panels + panels) * panel, dz_at = p.h_panels * panel;
     const uint32_t bufs = p.cols <= 128 ? 2 : 1;   // accumulators of 128 columns each, or one of up to 256
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *failed = &sh.failed;
 
     group_table(sh.table, p.offsets, p.G, p.n);
     if (threadIdx.x == 0) {
-        for (int i = 0; i < p.stages; ++i) bar_init(smem_addr(&sh.full[i]), 1), bar_init(smem_addr(&sh.empty[i]), 1), bar_init(smem_addr(&sh.made[i]), kMakers);
+        // a stage is free when its products are done, and the adders have taken their sums of it
+        for (int i = 0; i < p.stages; ++i) bar_init(smem_addr(&sh.full[i]), 1), bar_init(smem_addr(&sh.empty[i]), p.sums ? 1 + kAdders : 1), bar_init(smem_addr(&sh.made[i]), kMakers);
         for (int i = 0; i < 2; ++i) bar_init(smem_addr(&sh.acc_full[i]), 1), bar_init(smem_addr(&sh.acc_empty[i]), kAdders);
         sh.failed = 0;
         bar_init_fence();
@@ -379,7 +384,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     const int tiles = p.m_tiles * p.n_tiles;
     const int chunk = blockIdx.x / tiles, tile = blockIdx.x % tiles, m_tile = tile / p.n_tiles;
     const int m0 = m_tile * 128, n0 = tile % p.n_tiles * p.cols, cols = min(p.cols, p.d_out - n0);
-    const int h_panels = p.d_in - m0 > 64 ? 2 : 1;
+    const int h_panels = p.d_in - m0 > 64 ? 2 : 1;   // with columns
     const int chunk0 = (int)min((long long)p.n, (long long)chunk * p.chunk_rows), chunk1 = (int)min((long long)p.n, (long long)chunk0 + p.chunk_rows);
     int g0 = 0;   // the first group that ends behind the chunk's start
     for (int hi = p.G; g0 < hi;) {
@@ -399,7 +404,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     const auto clear = [&](uint32_t at, int rows, int from, int to, int me, int of) {
         const int rest = 16 - rows % 16;
         for (int i = me; i < rest * 8 * (to - from); i += of) {
-            const uint32_t where = at + (from + i / (rest * 8)) * kPanel + (rows + i / 8 % rest) * 128 + (i % 8) * 16;
+            const uint32_t where = at + (from + i / (rest * 8)) * panel + (rows + i / 8 % rest) * 128 + (i % 8) * 16;
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};\n" ::"r"(where), "r"(0) : "memory");
         }
     };
@@ -411,15 +416,15 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
         for (int g = g0; ok && more(g); ++g) {
             int lo, hi;
             if (!segment(g, lo, hi)) continue;
-            for (int r = lo; r < hi; r += kStep, ++use, st.next(p.stages)) {
+            for (int r = lo; r < hi; r += p.step, ++use, st.next(p.stages)) {
                 const uint32_t s = st.at, bar = smem_addr(&sh.full[s]), at = ring + s * stage_bytes;
                 ok = warp_wait(smem_addr(&sh.empty[s]), st.round ^ 1, failed);
                 if (!ok) break;
                 if (one_lane()) {
-                    bar_expect(bar, ((CK ? 0 : h_panels) + panels) * kPanel);
+                    bar_expect(bar, ((CK ? 0 : h_panels) + panels) * panel);
                     if (!CK)
-                        for (int c = 0; c < h_panels; ++c) tile_load_2d(at + c * kPanel, &p.h, m0 + c * 64, r, bar);
-                    for (int c = 0; c < panels; ++c) tile_load_2d(at + (2 + c) * kPanel, &p.dz, n0 + c * 64, r, bar);
+                        for (int c = 0; c < h_panels; ++c) tile_load_2d(at + c * panel, &p.h, m0 + c * 64, r, bar);
+                    for (int c = 0; c < panels; ++c) tile_load_2d(at + dz_at + c * panel, &p.dz, n0 + c * 64, r, bar);
                 }
                 __syncwarp();
             }
@@ -439,23 +444,28 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                 if (!ok) break;
                 tc_after_sync();
                 const int r1 = min(hi, r0 + kRunRows);
-                for (int r = r0; r < r1; r += kStep, st.next(p.stages)) {
+                for (int r = r0; r < r1; r += p.step, st.next(p.stages)) {
                     const uint32_t s = st.at, at = ring + s * stage_bytes;
-                    const int rows = min(kStep, hi - r);
+                    const int rows = min(p.step, hi - r);
                     ok = warp_wait(smem_addr(&sh.full[s]), st.round, failed);
                     if (CK) ok = ok && warp_wait(smem_addr(&sh.made[s]), st.round, failed);
                     if (!ok) break;
                     if (!CK && rows % 16) {
                         clear(at, rows, 0, h_panels, lane, 32);
-                        clear(at, rows, 2, 2 + panels, lane, 32);
+                        clear(at, rows, p.h_panels, p.h_panels + panels, lane, 32);
                         async_proxy_fence();
                         __syncwarp();
                     }
                     if (one_lane()) {
-                        const uint64_t da = tc_operand(at, kPanel, 1024), db = tc_operand(at + 2 * kPanel, kPanel, 1024);
+                        const uint64_t da = tc_operand(at, panel, 1024), db = tc_operand(at + dz_at, panel, 1024);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
+                        for (int j = 0; j < kStep / 16; ++j)
                             if (j * 16 < rows) tc_mma(tmem + buf * 128, tc_advance(da, j * 2048), tc_advance(db, j * 2048), instr, r > r0 || j > 0);
+                        if (rows > kStep) {
+#pragma unroll
+                            for (int j = kStep / 16; j < kStepMost / 16; ++j)
+                                if (j * 16 < rows) tc_mma(tmem + buf * 128, tc_advance(da, j * 2048), tc_advance(db, j * 2048), instr, true);
+                        }
                         tc_commit(smem_addr(&sh.empty[s]));
                     }
                     __syncwarp();
@@ -467,13 +477,60 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     } else if (warp < 2 + kAdders) {
         const uint32_t quad = warp & 3, part = (warp - 2) / 4, lanes = quad * 32 << 16;   // rows m0 + 32 quad + lane of dW, every other 32 columns
         const int m = m0 + quad * 32 + lane;
-        RingPlace acc;
+        // The column sums of dz: panel quad, 8 columns of every fourth row of one half of a step, the steps shared by the blocks of a
+        // chunk.  A thread's rows are 4 apart, so that their chunks lie at one of two places of the swizzle.
+        const bool want_sums = CK && p.sums && (int)quad < panels;
+        const int half = p.step / 2, row0 = part * half + (lane >> 3);
+        const uint32_t sum_at = dz_at + quad * panel + row0 * 128, even = ((lane & 7) ^ (row0 & 7)) << 4, odd = ((lane & 7) ^ ((row0 + 4) & 7)) << 4;
+        float2 cs[4];
+        RingPlace st, acc;
         bool ok = true;
         for (int g = g0; ok && more(g); ++g) {
             int lo, hi;
             if (!segment(g, lo, hi)) continue;
             float *out = p.part + ((long long)(chunk + g) * p.d_in + m) * p.d_out + n0;
+            int turn = 0;   // the step's number modulo the tiles that share the sums
+#pragma unroll
+            for (int e = 0; e < 4; ++e) cs[e] = make_float2(0.f, 0.f);
             for (int r0 = lo; r0 < hi; r0 += kRunRows, acc.next(bufs)) {
+                if (CK && p.sums) {
+                    const int r1 = min(hi, r0 + kRunRows);
+                    for (int r = r0; r < r1; r += p.step, st.next(p.stages)) {
+                        // also where it is another block's turn: the arrival below belongs to this round of the stage
+                        ok = warp_wait(smem_addr(&sh.full[st.at]), st.round, failed);
+                        if (!ok) break;
+                        if (want_sums && turn == m_tile) {
+                            const uint32_t at = ring + st.at * stage_bytes + sum_at;
+                            float2 cr[4];   // a step's sums first: long sums of single values lose digits
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) cr[e] = make_float2(0.f, 0.f);
+                            for (int i0 = 0; i0 < half / 4; i0 += 8) {   // 8 rows of a thread at a time
+                                uint4 v[8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    v[i] = make_uint4(0u, 0u, 0u, 0u);
+                                    if (row0 + 4 * (i0 + i) < hi - r)
+                                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n"
+                                                     : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w)
+                                                     : "r"(at + (i0 + i) * 512 + (i & 1 ? odd : even)));
+                                }
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    float2 x[4];
+                                    Pairs<__nv_bfloat16>::get(v[i], x);
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) cr[e] = __fadd2_rn(cr[e], x[e]);
+                                }
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) cs[e] = __fadd2_rn(cs[e], cr[e]);
+                            __syncwarp();
+                        }
+                        if (lane == 0) bar_arrive(smem_addr(&sh.empty[st.at]));
+                        if (++turn == p.m_tiles) turn = 0;
+                    }
+                    if (!ok) break;
+                }
                 const uint32_t buf = acc.at;
                 ok = warp_wait(smem_addr(&sh.acc_full[buf]), acc.round, failed);
                 if (!ok) break;
@@ -502,97 +559,6 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                 __syncwarp();
                 if (lane == 0) bar_arrive(smem_addr(&sh.acc_empty[buf]));
             }
-        }
-    } else if constexpr (CK) {
-        const int w = warp - 2 - kAdders, me = w * 32 + lane;
-        // the part of h: 8 columns of four rows a step and thread, asked for kAhead steps before they are used
-        constexpr int kAhead = 3, kRows = kStep / (kMakers * 2);
-        const int hc = me & 15, hr = me >> 4;
-        uint2 code[kAhead][kRows];
-        unsigned scale[kAhead][kRows];
-        const bool h_cols = m0 + hc * 8 < p.d_in;
-        const int8_t *codes = p.codes + (m0 + hc * 8);
-        const uint8_t *scales = p.scales + (m0 + hc * 8) / kCkptBlock;
-        const auto ask = [&](uint2 (&code)[kRows], unsigned (&scale)[kRows], int r, int hi) {
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                const int row = r + hr + 2 * kMakers * i;
-                code[i] = make_uint2(0u, 0u);
-                scale[i] = 0;
-                if (h_cols && row < hi) {
-                    code[i] = __ldg(reinterpret_cast<const uint2 *>(codes + (long long)row * p.d_in));
-                    scale[i] = __ldg(scales + (long long)row * p.nb);
-                }
-            }
-        };
-        uint32_t h_at[kRows];   // where they go in a stage
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) h_at[i] = (hc >> 3) * kPanel + (hr + 2 * kMakers * i) * 128 + (((hc & 7) ^ ((hr + 2 * kMakers * i) & 7)) << 4);
-        // The column sums: 8 columns of every fourth row of one share of a step, the steps shared by the blocks of a chunk.
-        // A thread's rows of a step are 4 apart, so that their chunks lie at one of two places of the swizzle.
-        const bool want_sums = p.sums != nullptr && (w & 3) < panels;
-        const int share = w >> 2, row0 = share * (kStep / kSumShares) + (lane >> 3);
-        const uint32_t sum_at = (2 + (w & 3)) * kPanel + row0 * 128, even = ((lane & 7) ^ (row0 & 7)) << 4, odd = ((lane & 7) ^ ((row0 + 4) & 7)) << 4;
-        float2 cs[4];
-        RingPlace st;
-        bool ok = true;
-        for (int g = g0; ok && more(g); ++g) {
-            int lo, hi;
-            if (!segment(g, lo, hi)) continue;
-#pragma unroll
-            for (int d = 0; d < kAhead; ++d) ask(code[d], scale[d], lo + d * kStep, hi);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) cs[e] = make_float2(0.f, 0.f);
-            int turn = 0;   // the step's number modulo the tiles that share the sums
-            for (int r3 = lo; ok && r3 < hi; r3 += kAhead * kStep) {
-#pragma unroll
-                for (int d = 0; d < kAhead; ++d) {   // unrolled: the sets are registers
-                    const int r = r3 + d * kStep;
-                    if (r >= hi) break;
-                    const uint32_t s = st.at, at = ring + s * stage_bytes;
-                    const int rows = min(kStep, hi - r);
-                    ok = warp_wait(smem_addr(&sh.empty[s]), st.round ^ 1, failed);
-                    if (!ok) break;
-                    if (h_cols) {
-#pragma unroll
-                        for (int i = 0; i < kRows; ++i) {
-                            const unsigned word[2] = {code[d][i].x, code[d][i].y};
-                            uint32_t b[4];
-                            ckpt_decode_bf16(word, ckpt_scale(scale[d][i]), b);
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + h_at[i]), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
-                        }
-                    }
-                    ask(code[d], scale[d], r + kAhead * kStep, hi);
-                    const bool sum = want_sums && turn == m_tile;
-                    if (++turn == p.m_tiles) turn = 0;
-                    if (rows % 16 || sum) {
-                        ok = warp_wait(smem_addr(&sh.full[s]), st.round, failed);
-                        if (!ok) break;
-                    }
-                    if (rows % 16) clear(at, rows, 2, 2 + panels, me, kMakers * 32);   // h's rows are zeros already
-                    async_proxy_fence();
-                    if (sum) {
-                        float2 cr[4];   // a step's sums first: long sums of single values lose digits
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) cr[e] = make_float2(0.f, 0.f);
-#pragma unroll
-                        for (int i = 0; i < kStep / kSumShares / 4; ++i) {
-                            if (rows < kStep && row0 + 4 * i >= rows) continue;
-                            uint4 v;
-                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at + sum_at + i * 512 + (i & 1 ? odd : even)));
-                            float2 x[4];
-                            Pairs<__nv_bfloat16>::get(v, x);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) cr[e] = __fadd2_rn(cr[e], x[e]);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) cs[e] = __fadd2_rn(cs[e], cr[e]);
-                    }
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(smem_addr(&sh.made[s]));
-                    st.next(p.stages);
-                }
-            }
             if (ok && want_sums) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -601,11 +567,73 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                         cs[e].x += __shfl_xor_sync(0xffffffffu, cs[e].x, d);
                         cs[e].y += __shfl_xor_sync(0xffffffffu, cs[e].y, d);
                     }
-                const int col = (w & 3) * 64 + lane * 8;
+                const int col = quad * 64 + lane * 8;
                 if (lane < 8 && col < cols) {
-                    float4 *out = reinterpret_cast<float4 *>(p.sums + ((long long)(chunk + g) * kSumShares * p.m_tiles + m_tile * kSumShares + share) * p.d_out + n0 + col);
-                    out[0] = make_float4(cs[0].x, cs[0].y, cs[1].x, cs[1].y);
-                    out[1] = make_float4(cs[2].x, cs[2].y, cs[3].x, cs[3].y);
+                    float4 *to = reinterpret_cast<float4 *>(p.sums + ((long long)(chunk + g) * 2 * p.m_tiles + m_tile * 2 + part) * p.d_out + n0 + col);
+                    to[0] = make_float4(cs[0].x, cs[0].y, cs[1].x, cs[1].y);
+                    to[1] = make_float4(cs[2].x, cs[2].y, cs[3].x, cs[3].y);
+                }
+            }
+        }
+    } else if constexpr (CK) {
+        const int w = warp - 2 - kAdders, me = w * 32 + lane;
+        // the part of h: 8 columns of four rows a step and thread, asked for kAhead steps before they are used
+        constexpr int kAhead = 3, kRows = 4;
+        const int across = p.h_panels * 8, hc = me & (across - 1), hr = me / across, apart = kMakers * 32 / across;   // apart * kRows = p.step
+        uint2 code[kAhead][kRows];
+        unsigned scale[kAhead][kRows];
+        const bool h_cols = m0 + hc * 8 < p.d_in;
+        const int8_t *codes = p.codes + (m0 + hc * 8);
+        const uint8_t *scales = p.scales + (m0 + hc * 8) / kCkptBlock;
+        const auto ask = [&](uint2 (&code)[kRows], unsigned (&scale)[kRows], int r, int hi) {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const int row = r + hr + apart * i;
+                code[i] = make_uint2(0u, 0u);
+                scale[i] = 0;
+                if (h_cols && row < hi) {
+                    code[i] = __ldg(reinterpret_cast<const uint2 *>(codes + (long long)row * p.d_in));
+                    scale[i] = __ldg(scales + (long long)row * p.nb);
+                }
+            }
+        };
+        // where they go in a stage (apart is a multiple of 8: the rows of a thread have one place in the swizzle)
+        const uint32_t h_at = (hc >> 3) * panel + hr * 128 + (((hc & 7) ^ (hr & 7)) << 4), h_apart = apart * 128;
+        RingPlace st;
+        bool ok = true;
+        for (int g = g0; ok && more(g); ++g) {
+            int lo, hi;
+            if (!segment(g, lo, hi)) continue;
+#pragma unroll
+            for (int d = 0; d < kAhead; ++d) ask(code[d], scale[d], lo + d * p.step, hi);
+            for (int r3 = lo; ok && r3 < hi; r3 += kAhead * p.step) {
+#pragma unroll
+                for (int d = 0; d < kAhead; ++d) {   // unrolled: the sets are registers
+                    const int r = r3 + d * p.step;
+                    if (r >= hi) break;
+                    const uint32_t s = st.at, at = ring + s * stage_bytes;
+                    const int rows = min(p.step, hi - r);
+                    ok = warp_wait(smem_addr(&sh.empty[s]), st.round ^ 1, failed);
+                    if (!ok) break;
+                    if (h_cols) {
+#pragma unroll
+                        for (int i = 0; i < kRows; ++i) {
+                            const unsigned word[2] = {code[d][i].x, code[d][i].y};
+                            uint32_t b[4];
+                            ckpt_decode_bf16(word, ckpt_scale(scale[d][i]), b);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + h_at + i * h_apart), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
+                        }
+                    }
+                    ask(code[d], scale[d], r + kAhead * p.step, hi);
+                    if (rows % 16) {
+                        ok = warp_wait(smem_addr(&sh.full[s]), st.round, failed);
+                        if (!ok) break;
+                        clear(at, rows, p.h_panels, p.h_panels + panels, me, kMakers * 32);   // h's rows are zeros already
+                    }
+                    async_proxy_fence();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_addr(&sh.made[s]));
+                    st.next(p.stages);
                 }
             }
         }
@@ -730,15 +758,19 @@ static sar_status grouped_rows(int64_t n, int32_t groups, int K, int N, const in
     p.N = N;
     p.zero_rest = (flags & SAR_GROUPED_ZERO_REST) != 0;
     p.steps = (K + kStep - 1) / kStep;
-    // Weights stay in shared memory where 128 KB hold a slice of at least 128 columns: every row tile then costs the loads of its
-    // rows alone.  Longer contractions take both operands through the ring in slices of 256 columns.
-    const int widest = p.steps <= 4 ? 256 : p.steps <= 8 ? 16 / p.steps * 64 : 256;
+    // Weights stay in shared memory where 128 KB hold 192 columns of them and more: every row tile then costs the loads of its rows
+    // alone (300,000 rows, 264 x 264: 85 us, through the ring 120).  Longer contractions take both operands through the ring: narrower
+    // slices that stay read the rows again (500,000 rows, 512 x 512: slices of 128 that stay 382 us, of 256 through the ring 236).
+    const int widest = p.steps == 5 ? 192 : 256;
+    const bool stay = p.steps <= 5;
     p.slices = (N + widest - 1) / widest;
     p.cols = round_up_int((N + p.slices - 1) / p.slices, 64);
     p.slices = (N + p.cols - 1) / p.cols;
-    const size_t w_step = (size_t)(p.cols / 64) * kPanel, w_set = p.steps * w_step, fixed = sizeof(RowsShared) + 1024 + 8 * kStoreBuf, row_stage = kTileRows * 128;
+    const size_t w_step = (size_t)(p.cols / 64) * kPanel, w_set = p.steps * w_step, row_stage = kTileRows * 128;
+    p.store_bufs = stay ? 2 : 1;
+    const size_t fixed = sizeof(RowsShared) + 1024 + 4 * p.store_bufs * kStoreBuf;
     size_t smem;
-    if (p.steps <= 8) {
+    if (stay) {
         const size_t room = kSharedMost - fixed;
         p.slots = (int)((room - 3 * row_stage) / w_set);
         p.slots = p.slots > kSlotsMax ? kSlotsMax : p.slots;
@@ -767,7 +799,7 @@ static sar_status grouped_rows(int64_t n, int32_t groups, int K, int N, const in
 }
 
 struct WeightPlan {
-    int cols, m_tiles, n_tiles, chunks, chunk_rows, stages;
+    int cols, m_tiles, n_tiles, chunks, chunk_rows, stages, step, h_panels;
     size_t smem, part_bytes, sum_bytes, total_bytes;   // the scratch: records, their column sums, the groups' column sums
 };
 static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out) {
@@ -784,12 +816,18 @@ static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out) {
     rows = (rows + kStep - 1) / kStep * kStep;
     w.chunk_rows = (int)rows;
     w.chunks = (int)((n + rows - 1) / rows);
-    const size_t fixed = sizeof(WeightShared) + 1024, stage = (size_t)(2 + w.cols / 64) * kPanel;
+    // rows of one panel of h: twice as many a stage, so that a step is worth its waits, where three stages of that fit
+    // (2 million rows, 64 x 64, from a checkpoint: @@)
+    const size_t fixed = sizeof(WeightShared) + 1024;
+    const bool narrow = d_in <= 64 && w.cols <= 192;
+    w.h_panels = narrow ? 1 : 2;
+    w.step = narrow ? kStepMost : kStep;
+    const size_t stage = (size_t)(w.h_panels + w.cols / 64) * w.step * 128;
     w.stages = (int)((kSharedMost - fixed) / stage);
     w.stages = w.stages > kStagesMax ? kStagesMax : w.stages;
     w.smem = fixed + w.stages * stage;
     w.part_bytes = sar_round_up((size_t)(w.chunks + groups) * d_in * d_out * 4, 256);
-    w.sum_bytes = sar_round_up((size_t)(w.chunks + groups) * kSumShares * w.m_tiles * d_out * 4, 256);
+    w.sum_bytes = sar_round_up((size_t)(w.chunks + groups) * 2 * w.m_tiles * d_out * 4, 256);
     w.total_bytes = sar_round_up((size_t)groups * d_out * 4, 256);
     return w;
 }
@@ -816,7 +854,9 @@ static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_
     p.n_tiles = w.n_tiles;
     p.chunk_rows = w.chunk_rows;
     p.stages = w.stages;
-    const uint32_t box[2] = {64, kStep};
+    p.step = w.step;
+    p.h_panels = w.h_panels;
+    const uint32_t box[2] = {64, (uint32_t)w.step};
     const uint64_t h_dims[2] = {(uint64_t)d_in, (uint64_t)n}, z_dims[2] = {(uint64_t)d_out, (uint64_t)n};
     if (h) SAR_TRY(tc_tensor_map(&p.h, h, 2, h_dims, box));
     SAR_TRY(tc_tensor_map(&p.dz, dz, 2, z_dims, box));
@@ -835,7 +875,7 @@ static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_
         total = reinterpret_cast<float *>(static_cast<char *>(workspace) + w.part_bytes + w.sum_bytes);
         SAR_LAUNCH("linear_grouped_sums_reduce", st,
                    launch(grouped_sums_reduce_kernel, dim3((unsigned)((d_out + 31) / 32), (unsigned)groups), 512, 0, st, offsets, (long long)n, (int)d_out, w.chunk_rows,
-                          kSumShares * w.m_tiles, p.sums, total));
+                          2 * w.m_tiles, p.sums, total));
         SAR_TRY(sar_after_launch());
     }
     const long long quads = (long long)d_in * d_out / 4;
