@@ -78,24 +78,25 @@ __global__ void __launch_bounds__(256, 4) ckpt8_pack_kernel(long long blocks, in
             const long long b = b0 + u * (32 / LPB) + (threadIdx.x & 31) / LPB;
             const B p(b, blocks, sub, C, nb, whole);
             float2 v[S][P];
-            unsigned top = 0;
+            float top = 0.f;
 #pragma unroll
             for (int i = 0; i < S; ++i) {
                 B::Vec::get(raw[u][i], v[i]);
 #pragma unroll
-                for (int q = 0; q < P; ++q) top = max(top, E == 1 ? ckpt_magnitude(v[i][q].x) : max(ckpt_magnitude(v[i][q].x), ckpt_magnitude(v[i][q].y)));
+                for (int q = 0; q < P; ++q) top = ckpt_top(top, v[i][q].x, v[i][q].y);
             }
 #pragma unroll
-            for (int d = 1; d < LPB; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+            for (int d = 1; d < LPB; d <<= 1) top = ckpt_top(top, __shfl_xor_sync(0xffffffffu, top, d), 0.f);
             const unsigned s = ckpt_scale_byte(top);
             const float inv = ckpt_inverse(s);
+            const bool cut = ckpt_cut(top, inv);
 #pragma unroll
             for (int i = 0; i < S; ++i) {
                 if (!p.ok(i)) continue;
                 int8_t *to = codes + p.slot(i);
-                if constexpr (E == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(ckpt_code4(&v[i][0].x, inv, s), ckpt_code4(&v[i][2].x, inv, s));
-                else if constexpr (E == 4) *reinterpret_cast<unsigned *>(to) = ckpt_code4(&v[i][0].x, inv, s);
-                else *to = (int8_t)(s == 255u ? 0u : ckpt_code(v[i][0].x, inv));
+                if constexpr (E == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(ckpt_code4(v[i][0], v[i][1], inv, s, cut), ckpt_code4(v[i][2], v[i][3], inv, s, cut));
+                else if constexpr (E == 4) *reinterpret_cast<unsigned *>(to) = ckpt_code4(v[i][0], v[i][1], inv, s, cut);
+                else *to = ckpt_code1(v[i][0].x, inv, s, cut);
             }
             if (sub == 0 && b < blocks) scales[b] = (uint8_t)s;
         }
@@ -134,14 +135,13 @@ __global__ void __launch_bounds__(256, 4) ckpt8_unpack_kernel(long long blocks, 
             for (int i = 0; i < S; ++i) {
                 if (!p.ok(i)) continue;
                 float2 v[P];
-                if constexpr (E == 8) {
-                    const unsigned w[2] = {raw[u][i].x, raw[u][i].y};
-                    ckpt_decode_n<8>(w, scale, &v[0].x);
-                } else if constexpr (E == 4) {
-                    const unsigned w[1] = {raw[u][i]};
-                    ckpt_decode_n<4>(w, scale, &v[0].x);
-                } else {
+                if constexpr (E == 1) {
                     v[0] = make_float2((float)raw[u][i] * scale, 0.f);
+                } else {
+                    unsigned w[2];
+                    memcpy(w, &raw[u][i], E);
+#pragma unroll
+                    for (int q = 0; q < P; ++q) v[q] = ckpt_decode2(w[q / 2] ^ 0x80808080u, 2 * q & 3, make_float2(scale, scale));
                 }
                 *reinterpret_cast<typename B::raw_t *>(x + p.slot(i)) = B::Vec::put(v);
             }

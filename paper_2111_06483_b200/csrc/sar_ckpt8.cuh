@@ -57,49 +57,62 @@ struct ColVec<__nv_bfloat16, 1> {
 
 constexpr int kCkptBlock = SAR_CKPT8_BLOCK;   // columns that share a scale
 
-// |x| as an unsigned key: larger magnitudes have larger keys, and NaN the largest (a maximum of floats would drop it)
-__device__ __forceinline__ unsigned ckpt_magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// the largest magnitude so far and of two more values; NaN where any of them is (a plain maximum would drop it)
+__device__ __forceinline__ float ckpt_top(float top, float a, float b) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(top), "f"(a), "f"(b));
+    return r;
+}
 
-// the scale byte of a block whose largest magnitude has this key: 0 all zero, 255 anything infinite or NaN, else
+// the scale byte of a block whose largest magnitude is `top`: 0 all zero, 255 anything infinite or NaN, else
 // max(E - 6, -126) + 127, which is 1 to 248
-__device__ __forceinline__ unsigned ckpt_scale_byte(unsigned top) {
-    const unsigned e = top >> 23;
-    return top == 0u ? 0u : e == 255u ? 255u : e > 7u ? e - 6u : 1u;
+__device__ __forceinline__ unsigned ckpt_scale_byte(float top) {
+    const unsigned e = __float_as_uint(top) >> 23;   // top has no sign
+    return top == 0.f ? 0u : e == 255u ? 255u : e > 7u ? e - 6u : 1u;
 }
 // 2^(127 - s); 0 for the bytes 0 and 255, whose codes are 0
 __device__ __forceinline__ float ckpt_inverse(unsigned s) { return (s == 0u || s == 255u) ? 0.f : __uint_as_float((254u - s) << 23); }
 // 2^(s - 127): 0 for the byte 0, NaN for 255
 __device__ __forceinline__ float ckpt_scale(unsigned s) { return __uint_as_float(s == 255u ? 0x7fc00000u : s << 23); }
 
-// The code of x in the low byte, to be masked where s is 255.  Added to 1.5 * 2^23 the quotient is rounded to the nearest whole
-// number, ties to even, and its two's complement is the sum's low byte (a conversion instruction runs at a quarter of the rate).
-__device__ __forceinline__ unsigned ckpt_code(float x, float inverse) {
-    return __float_as_uint(fminf(fmaxf(x * inverse, -127.f), 127.f) + 12582912.f);
+// Codes in the low bytes of floats.  Added to 1.5 * 2^23 the quotient x / scale, which is exact, is rounded to the nearest whole number,
+// ties to even, and its two's complement is the sum's low byte.  Only a block whose largest quotient reaches 127.5 can round to
+// 128: one in 200, so a warp looks for that once (`cut`) and clamps there.
+constexpr float kCkptMagic = 12582912.f;
+__device__ __forceinline__ bool ckpt_cut(float top, float inverse) { return __any_sync(0xffffffffu, top * inverse >= 127.5f); }
+__device__ __forceinline__ float ckpt_code(float x, float inverse, bool cut) {
+    const float v = fmaf(x, inverse, kCkptMagic);
+    return cut ? fminf(fmaxf(v, kCkptMagic - 127.f), kCkptMagic + 127.f) : v;
 }
-__device__ __forceinline__ unsigned ckpt_code4(const float *x, float inverse, unsigned s) {
-    const unsigned lo = __byte_perm(ckpt_code(x[0], inverse), ckpt_code(x[1], inverse), 0x0040);
-    const unsigned hi = __byte_perm(ckpt_code(x[2], inverse), ckpt_code(x[3], inverse), 0x0040);
-    return s == 255u ? 0u : __byte_perm(lo, hi, 0x5410);
+__device__ __forceinline__ unsigned ckpt_code4(float2 a, float2 b, float inverse, unsigned s, bool cut) {
+    const float2 i = make_float2(inverse, inverse), m = make_float2(kCkptMagic, kCkptMagic);
+    a = __ffma2_rn(a, i, m);
+    b = __ffma2_rn(b, i, m);
+    if (cut) {
+        const float lo = kCkptMagic - 127.f, hi = kCkptMagic + 127.f;
+        a.x = fminf(fmaxf(a.x, lo), hi), a.y = fminf(fmaxf(a.y, lo), hi), b.x = fminf(fmaxf(b.x, lo), hi), b.y = fminf(fmaxf(b.y, lo), hi);
+    }
+    const unsigned w = __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
+    return s == 255u ? 0u : w;
+}
+__device__ __forceinline__ int8_t ckpt_code1(float x, float inverse, unsigned s, bool cut) {
+    return (int8_t)(s == 255u ? 0u : __float_as_uint(ckpt_code(x, inverse, cut)));
 }
 // code i of a word of four as a float: 2^23 + 128 + code is put together from its bytes, and the subtraction is exact
 __device__ __forceinline__ float ckpt_decode(unsigned flipped /* the word ^ 0x80808080 */, int i) {
     return __uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7540u | i)) - 8388736.f;
 }
-template <int N>   // N codes (a multiple of 4, or 1) -> N values
-__device__ __forceinline__ void ckpt_decode_n(const unsigned (&w)[(N + 3) / 4], float scale, float *x) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = ckpt_decode(w[i / 4] ^ 0x80808080u, i & 3) * scale;
+// codes i and i + 1 of a word times the scale
+__device__ __forceinline__ float2 ckpt_decode2(unsigned flipped, int i, float2 scale) {
+    const float2 raw = make_float2(__uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7540u | i)), __uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7540u | (i + 1))));
+    return __fmul2_rn(__fadd2_rn(raw, make_float2(-8388736.f, -8388736.f)), scale);
 }
-
-// 8 codes -> 8 values in bf16, which holds them exactly (two codes in a pass: two packed operations and a conversion)
+// 8 codes -> 8 values in bf16, which holds them exactly
 __device__ __forceinline__ void ckpt_decode_bf16(const unsigned (&w)[2], float scale, uint32_t (&b)[4]) {
-    const float2 s = make_float2(scale, scale), shift = make_float2(-8388736.f, -8388736.f);
+    const float2 s = make_float2(scale, scale);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const unsigned flipped = w[q / 2] ^ 0x80808080u;
-        const float2 raw = make_float2(__uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7540u | (2 * q & 3))),
-                                       __uint_as_float(__byte_perm(flipped, 0x4B000000u, 0x7540u | ((2 * q + 1) & 3))));
-        const float2 v = __fmul2_rn(__fadd2_rn(raw, shift), s);
+        const float2 v = ckpt_decode2(w[q / 2] ^ 0x80808080u, 2 * q & 3, s);
         b[q] = Elem<__nv_bfloat16>::pack2(v.x, v.y);
     }
 }

@@ -583,19 +583,33 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
         uint2 code[kAhead][kRows];
         unsigned scale[kAhead][kRows];
         const bool h_cols = m0 + hc * 8 < p.d_in;
-        const int8_t *codes = p.codes + (m0 + hc * 8);
-        const uint8_t *scales = p.scales + (m0 + hc * 8) / kCkptBlock;
-        const auto ask = [&](uint2 (&code)[kRows], unsigned (&scale)[kRows], int r, int hi) {
+        const int8_t *codes;     // of the thread's first row kAhead steps on, or where the segment begins
+        const uint8_t *scales;
+        const int code_rows = apart * p.d_in, scale_rows = apart * p.nb;
+        const auto begin = [&](int r) {
+            codes = p.codes + (long long)(r + hr) * p.d_in + m0 + hc * 8;
+            scales = p.scales + (long long)(r + hr) * p.nb + (m0 + hc * 8) / kCkptBlock;
+        };
+        const auto ask = [&](uint2 (&code)[kRows], unsigned (&scale)[kRows], int left) {   // `left` rows to the segment's end
+            if (left >= p.step && h_cols) {
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                const int row = r + hr + apart * i;
-                code[i] = make_uint2(0u, 0u);
-                scale[i] = 0;
-                if (h_cols && row < hi) {
-                    code[i] = __ldg(reinterpret_cast<const uint2 *>(codes + (long long)row * p.d_in));
-                    scale[i] = __ldg(scales + (long long)row * p.nb);
+                for (int i = 0; i < kRows; ++i) {
+                    code[i] = __ldg(reinterpret_cast<const uint2 *>(codes + i * code_rows));
+                    scale[i] = __ldg(scales + i * scale_rows);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    code[i] = make_uint2(0u, 0u);
+                    scale[i] = 0;
+                    if (h_cols && hr + apart * i < left) {
+                        code[i] = __ldg(reinterpret_cast<const uint2 *>(codes + i * code_rows));
+                        scale[i] = __ldg(scales + i * scale_rows);
+                    }
                 }
             }
+            codes += (long long)p.step * p.d_in;
+            scales += p.step * p.nb;
         };
         // where they go in a stage (apart is a multiple of 8: the rows of a thread have one place in the swizzle)
         const uint32_t h_at = (hc >> 3) * panel + hr * 128 + (((hc & 7) ^ (hr & 7)) << 4), h_apart = apart * 128;
@@ -604,8 +618,9 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
         for (int g = g0; ok && more(g); ++g) {
             int lo, hi;
             if (!segment(g, lo, hi)) continue;
+            begin(lo);
 #pragma unroll
-            for (int d = 0; d < kAhead; ++d) ask(code[d], scale[d], lo + d * p.step, hi);
+            for (int d = 0; d < kAhead; ++d) ask(code[d], scale[d], hi - lo - d * p.step);
             for (int r3 = lo; ok && r3 < hi; r3 += kAhead * p.step) {
 #pragma unroll
                 for (int d = 0; d < kAhead; ++d) {   // unrolled: the sets are registers
@@ -624,7 +639,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + h_at + i * h_apart), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
                         }
                     }
-                    ask(code[d], scale[d], r + kAhead * p.step, hi);
+                    ask(code[d], scale[d], hi - r - kAhead * p.step);
                     if (rows % 16) {
                         ok = warp_wait(smem_addr(&sh.full[s]), st.round, failed);
                         if (!ok) break;

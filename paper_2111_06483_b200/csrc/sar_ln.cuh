@@ -83,24 +83,25 @@ struct LnRow {
     __device__ __forceinline__ void put_codes(const LnArgs &a, long long row, bool live, const float2 (&x)[V][P]) const {
 #pragma unroll
         for (int v0 = 0; v0 < V; v0 += SPB) {
-            unsigned top = 0;
+            float top = 0.f;
 #pragma unroll
             for (int v = v0; v < v0 + SPB && v < V; ++v)
 #pragma unroll
                 for (int q = 0; q < P; ++q)
-                    if (ok[v]) top = max(top, E == 1 ? ckpt_magnitude(x[v][q].x) : max(ckpt_magnitude(x[v][q].x), ckpt_magnitude(x[v][q].y)));
+                    if (ok[v]) top = ckpt_top(top, x[v][q].x, E == 1 ? 0.f : x[v][q].y);
 #pragma unroll
-            for (int d = 1; d < LPB; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d, G));
+            for (int d = 1; d < LPB; d <<= 1) top = ckpt_top(top, __shfl_xor_sync(0xffffffffu, top, d, G), 0.f);
             const unsigned s = ckpt_scale_byte(top);
             const float inv = ckpt_inverse(s);
+            const bool cut = ckpt_cut(top, inv);
             if (!live) continue;
 #pragma unroll
             for (int v = v0; v < v0 + SPB && v < V; ++v) {
                 if (!ok[v]) continue;
                 int8_t *p = a.codes + at(row, v);
-                if constexpr (E == 8) *reinterpret_cast<uint2 *>(p) = make_uint2(ckpt_code4(&x[v][0].x, inv, s), ckpt_code4(&x[v][2].x, inv, s));
-                else if constexpr (E == 4) *reinterpret_cast<unsigned *>(p) = ckpt_code4(&x[v][0].x, inv, s);
-                else *p = (int8_t)(s == 255u ? 0u : ckpt_code(x[v][0].x, inv));
+                if constexpr (E == 8) *reinterpret_cast<uint2 *>(p) = make_uint2(ckpt_code4(x[v][0], x[v][1], inv, s, cut), ckpt_code4(x[v][2], x[v][3], inv, s, cut));
+                else if constexpr (E == 4) *reinterpret_cast<unsigned *>(p) = ckpt_code4(x[v][0], x[v][1], inv, s, cut);
+                else *p = ckpt_code1(x[v][0].x, inv, s, cut);
                 if (v == v0 && col(v) % kCkptBlock == 0) a.scales[row * a.nb + col(v) / kCkptBlock] = (uint8_t)s;
             }
         }
@@ -129,7 +130,7 @@ struct LnRow {
 #pragma unroll
             for (int q = 0; q < P; ++q) {
                 const unsigned w = r[v].w[q / 2] ^ 0x80808080u;
-                x[v][q] = E == 1 ? make_float2(ckpt_decode(w, 0) * s.x, 0.f) : __fmul2_rn(make_float2(ckpt_decode(w, 2 * q % 4), ckpt_decode(w, (2 * q + 1) % 4)), s);
+                x[v][q] = E == 1 ? make_float2(ckpt_decode(w, 0) * s.x, 0.f) : ckpt_decode2(w, 2 * q & 3, s);
             }
         }
     }
@@ -350,11 +351,13 @@ __global__ void __launch_bounds__(kThreads) ln_fwd_long_kernel(const LnArgs a) {
             const int c = b * kCkptBlock + lane;
             const float xh = c < a.C ? (ln_load<T>(a.x, o + c) - mean) * rstd : 0.f;
             if constexpr (CK) {
-                unsigned top = ckpt_magnitude(xh);
+                float top = ckpt_top(xh, 0.f, 0.f);
 #pragma unroll
-                for (int d = 16; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+                for (int d = 16; d > 0; d >>= 1) top = ckpt_top(top, __shfl_xor_sync(0xffffffffu, top, d), 0.f);
                 const unsigned s = ckpt_scale_byte(top);
-                if (c < a.C) a.codes[o + c] = (int8_t)(s == 255u ? 0u : ckpt_code(xh, ckpt_inverse(s)));
+                const float inv = ckpt_inverse(s);
+                const bool cut = ckpt_cut(top, inv);
+                if (c < a.C) a.codes[o + c] = ckpt_code1(xh, inv, s, cut);
                 if (lane == 0) a.scales[row * a.nb + b] = (uint8_t)s;
             }
             if (c < a.C) Elem<T>::store1(static_cast<T *>(a.y) + o + c, fmaf(xh, a.gamma ? __ldg(a.gamma + c) : 1.f, a.beta ? __ldg(a.beta + c) : 0.f));
