@@ -1,7 +1,7 @@
 // Checkpoints of node arrays in 8 bits: x[n, C] -> codes and block scales, and back (include/sar.h has the format and the
 // contracts).  Each is one pass over its arrays; nothing is computed that memory would wait for.
 #include "sar_ckpt8.cuh"
-#include "sar_dispatch.cuh"
+#include "sar_ln.cuh"
 
 #include <type_traits>
 
@@ -189,6 +189,14 @@ sar_status sar_ckpt8_pack(int64_t n, int32_t C, sar_dtype t, const void *x, int8
     SAR_TRY(ckpt_check(n, C, t, x, codes, scales));
     if (n == 0) return SAR_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const LnShape s = ln_shape(C, t, kLnCkpt, ln_alignment({x}), ln_alignment({codes}));
+    if (s.shifted && s.E > 0) {
+        LnArgs a = ln_args(n, C);
+        a.x = x;
+        a.codes = codes;
+        a.scales = scales;
+        return (t == SAR_F32 ? ln_checkpoint_f32 : ln_checkpoint_bf16)(s, a, false, st);
+    }
     const int nb = (int)ckpt_blocks(C), e = ckpt_width(C, t, x, codes);
     const long long blocks = n * nb;
     auto go = [&](auto cfg) -> sar_status {
@@ -205,6 +213,14 @@ sar_status sar_ckpt8_unpack(int64_t n, int32_t C, sar_dtype t, const int8_t *cod
     SAR_TRY(ckpt_check(n, C, t, x, codes, scales));
     if (n == 0) return SAR_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const LnShape s = ln_shape(C, t, kLnCkpt, ln_alignment({x}), ln_alignment({codes}));
+    if (s.shifted && s.E > 0) {
+        LnArgs a = ln_args(n, C);
+        a.y = x;
+        a.codes = const_cast<int8_t *>(codes);
+        a.scales = const_cast<uint8_t *>(scales);
+        return (t == SAR_F32 ? ln_checkpoint_f32 : ln_checkpoint_bf16)(s, a, true, st);
+    }
     const int nb = (int)ckpt_blocks(C), e = ckpt_width(C, t, x, codes);
     const long long blocks = n * nb;
     auto go = [&](auto cfg) -> sar_status {

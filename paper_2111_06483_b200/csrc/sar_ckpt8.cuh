@@ -84,16 +84,21 @@ __device__ __forceinline__ float ckpt_code(float x, float inverse, bool cut) {
     const float v = fmaf(x, inverse, kCkptMagic);
     return cut ? fminf(fmaxf(v, kCkptMagic - 127.f), kCkptMagic + 127.f) : v;
 }
-__device__ __forceinline__ unsigned ckpt_code4(float2 a, float2 b, float inverse, unsigned s, bool cut) {
-    const float2 i = make_float2(inverse, inverse), m = make_float2(kCkptMagic, kCkptMagic);
-    a = __ffma2_rn(a, i, m);
-    b = __ffma2_rn(b, i, m);
+// four codes, each with the inverse scale of its own block
+__device__ __forceinline__ unsigned ckpt_codes4(float2 a, float2 b, float2 inv_a, float2 inv_b, bool cut) {
+    const float2 m = make_float2(kCkptMagic, kCkptMagic);
+    a = __ffma2_rn(a, inv_a, m);
+    b = __ffma2_rn(b, inv_b, m);
     if (cut) {
         const float lo = kCkptMagic - 127.f, hi = kCkptMagic + 127.f;
         a.x = fminf(fmaxf(a.x, lo), hi), a.y = fminf(fmaxf(a.y, lo), hi), b.x = fminf(fmaxf(b.x, lo), hi), b.y = fminf(fmaxf(b.y, lo), hi);
     }
-    const unsigned w = __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
-    return s == 255u ? 0u : w;
+    return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
+}
+// four codes of one block
+__device__ __forceinline__ unsigned ckpt_code4(float2 a, float2 b, float inverse, unsigned s, bool cut) {
+    const float2 i = make_float2(inverse, inverse);
+    return s == 255u ? 0u : ckpt_codes4(a, b, i, i, cut);
 }
 __device__ __forceinline__ int8_t ckpt_code1(float x, float inverse, unsigned s, bool cut) {
     return (int8_t)(s == 255u ? 0u : __float_as_uint(ckpt_code(x, inverse, cut)));

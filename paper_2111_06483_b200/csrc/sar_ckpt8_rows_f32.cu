@@ -1,0 +1,15 @@
+#include "sar_ln.cuh"
+
+namespace sar {
+sar_status ln_checkpoint_f32(const LnShape &s, const LnArgs &a, bool unpack, cudaStream_t st) {
+    return ln_dispatch<float, kLnCkpt>(s, [&](auto cfg) -> sar_status {
+        using Row = typename decltype(cfg)::row;
+        if (unpack) {
+            static const unsigned most = ln_resident(ln_unpack_kernel<Row>, 0);
+            return ln_launch("ckpt8_unpack", ln_unpack_kernel<Row>, blocks_for(a.n, Row::G), most, 0, a, st);
+        }
+        static const unsigned most = ln_resident(ln_pack_kernel<Row>, 0);
+        return ln_launch("ckpt8_pack", ln_pack_kernel<Row>, blocks_for(a.n, Row::G), most, 0, a, st);
+    });
+}
+}  // namespace sar

@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
 // them.  Its rows stand for gamma v + beta, and  (gamma v + beta)^T dz = gamma (v^T dz) + beta (column sums of dz):  gamma and
 // beta enter in float32 after the product instead of rounding every value, and the column sums are taken from the tiles of dz
 // that are in shared memory anyway.
-constexpr int kRunRows = 1024;
+constexpr int kRunRows = 512;
 struct WeightArgs {
     CUtensorMap h, dz;
     const int64_t *offsets;

@@ -11,44 +11,9 @@
 
 namespace sar {
 
-// Which kernel, and its lanes and slots, for rows of C columns: E columns move at a time where E divides C and the arrays of type
-// t are aligned to `arrays` bytes, the codes to `codes` bytes.
-static sar_status ln_shape(int32_t C, sar_dtype t, bool backward, size_t arrays, size_t codes, LnShape *s) {
+static sar_status ln_check(int32_t C, sar_dtype t) {
     if (t != SAR_F32 && t != SAR_BF16) return SAR_ERR_INVALID_ARG;
-    if (C > (1 << 20)) return SAR_ERR_UNSUPPORTED;
-    const auto may = [&](int e) { return C % e == 0 && arrays >= e * sar_elem_size(t) && codes >= (size_t)e; };
-    *s = {0, 32, 0};
-    if (C > kLnRowCols) return SAR_OK;
-#define SAR_LN_FIT(EE, GG, VV) \
-    if (s->E == 0 && GG * VV * EE >= C) *s = {EE, GG, VV};
-    if (t == SAR_BF16 && may(8)) {
-        SAR_LN_8(SAR_LN_FIT)
-    } else if (may(4)) {
-        SAR_LN_4(SAR_LN_FIT)
-    } else if (backward) {
-        SAR_LN_1B(SAR_LN_FIT)
-    } else {
-        SAR_LN_1(SAR_LN_FIT)
-    }
-#undef SAR_LN_FIT
-    return SAR_OK;
-}
-
-// the largest power of two up to 16 that divides all addresses
-static size_t ln_alignment(std::initializer_list<const void *> ps) {
-    size_t a = 16;
-    for (const void *p : ps)
-        while (a > 1 && p && !sar_aligned(p, a)) a /= 2;
-    return a;
-}
-
-static LnArgs ln_args(int64_t n, int32_t C) {
-    LnArgs a{};
-    a.n = n;
-    a.C = C;
-    a.inv_c = 1.f / (float)C;
-    a.nb = (int)ckpt_blocks(C);
-    return a;
+    return C > (1 << 20) ? SAR_ERR_UNSUPPORTED : SAR_OK;
 }
 
 static sar_status ln_zero(int32_t C, float *dgamma, float *dbeta, cudaStream_t st) {
@@ -71,8 +36,8 @@ size_t sar_ln_workspace_bytes(int32_t C) {
 static sar_status ln_fwd_entry(int64_t n, int32_t C, sar_dtype t, const void *x, const float *gamma, const float *beta, float eps, void *y,
                                float *mean, float *rstd, int8_t *codes, uint8_t *scales, bool ckpt, void *stream) {
     if (n < 0 || C < 1 || !(eps >= 0.f) || (n > 0 && (!x || !y || (ckpt && (!rstd || !codes || !scales))))) return SAR_ERR_INVALID_ARG;
-    LnShape s;
-    SAR_TRY(ln_shape(C, t, false, ln_alignment({x, y}), ln_alignment({codes}), &s));
+    SAR_TRY(ln_check(C, t));
+    const LnShape s = ln_shape(C, t, kLnFwd, ln_alignment({x, y}), ln_alignment({codes}));
     SAR_TRY(check_elem_align({mean, rstd, gamma, beta}, 4));
     SAR_TRY(check_elem_align({x, y}, sar_elem_size(t)));
     if (n == 0) return SAR_OK;
@@ -104,8 +69,8 @@ static sar_status ln_bwd_entry(int64_t n, int32_t C, sar_dtype t, const void *x,
                                bool ckpt, const float *rstd, const float *gamma, const void *gy, void *gx, float *dgamma, float *dbeta,
                                void *workspace, size_t workspace_bytes, void *stream) {
     if (n < 0 || C < 1 || (n > 0 && (!rstd || !gy || !gx || (ckpt ? !codes || !scales : !x || !mean)))) return SAR_ERR_INVALID_ARG;
-    LnShape s;
-    SAR_TRY(ln_shape(C, t, true, ln_alignment({x, gy, gx}), ln_alignment({codes}), &s));
+    SAR_TRY(ln_check(C, t));
+    const LnShape s = ln_shape(C, t, kLnBwd, ln_alignment({x, gy, gx}), ln_alignment({codes}));
     SAR_TRY(check_elem_align({mean, rstd, gamma, dgamma, dbeta}, 4));
     SAR_TRY(check_elem_align({x, gy, gx}, sar_elem_size(t)));
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -10,7 +10,9 @@ namespace sar {
 
 constexpr int kSms = 148;
 constexpr int kLnBlocks = kSms * 8;   // largest grid (grids depend on the sizes alone: a fixed summation order)
-constexpr int kLnRowCols = 1024;      // longest row that a warp holds in registers
+// the sums of a block's weight gradients in shared memory: a copy for each warp where that is at most kLnSmem
+constexpr size_t kLnSmem = 32 * 1024;
+__host__ __device__ constexpr int ln_copies(int C) { return (size_t)kWarpsPerBlock * 2 * C * 4 <= kLnSmem ? kWarpsPerBlock : 1; }
 
 struct LnArgs {
     long long n;
@@ -27,10 +29,6 @@ struct LnArgs {
     float *partial;               // [blocks][2][C] or null (no weight gradients asked for)
 };
 
-// A row across the G lanes of a group: slot v of lane gl holds E columns from (v G + gl) E on, E being 16 bytes (8 bf16, 4
-// float32), 8 bytes (4 bf16) or one column, whatever C and the addresses allow.  Few lanes with many columns each, 16 where C
-// allows it, rather than many lanes with few: a warp then has up to 8 rows in hand and joins their sums in 2 to 4 steps
-// instead of 5.  (A million rows of 256 bf16, forward, 16 lanes of 16 columns against 32 of 8: see the table in sar_ln.cu.)
 template <int G>
 __device__ __forceinline__ float ln_sum(float x) {
 #pragma unroll
@@ -39,9 +37,17 @@ __device__ __forceinline__ float ln_sum(float x) {
 }
 __device__ __forceinline__ float2 ln_splat(float x) { return make_float2(x, x); }
 
-template <typename T, int E, int G, int V>
+// A row across the G lanes of a group, each with V slots of E columns: 16 bytes (8 bf16, 4 float32), or one column where the
+// arrays are not aligned to that.  Few lanes with many columns each, 16 of bf16 and 8 of float32 where that covers the row,
+// rather than many lanes with few: a warp then has up to 8 rows in hand and joins their sums in 2 to 4 steps instead of 5
+// (a million rows of 256 bf16, forward: 32 lanes of 8 columns 208 us, 16 of 16 171).
+//
+// LnRow: E divides C (or is 1).  Slot v of lane gl holds the columns from (v G + gl) E on, all or none of them.
+template <typename T_, int E_, int G_, int V_>
 struct LnRow {
-    static constexpr int P = (E + 1) / 2;   // pairs per slot
+    using T = T_;
+    static constexpr int E = E_, G = G_, V = V_, P = (E + 1) / 2;   // pairs per slot
+    static constexpr bool kShifted = false;
     using Raw = ColVec<T, E>;
     using raw_t = typename Raw::type;
     struct Packed {   // a slot of a checkpoint
@@ -50,9 +56,22 @@ struct LnRow {
     };
     int gl, C;
     bool ok[V];
-    __device__ __forceinline__ LnRow(const LnArgs &a, int gl_) : gl(gl_), C(a.C) {
+    __device__ __forceinline__ LnRow(const LnArgs &a, int gl_, long long) : gl(gl_), C(a.C) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) ok[v] = col(v) < C;   // E divides C: a slot has all its columns or none
+        for (int v = 0; v < V; ++v) ok[v] = col(v) < C;
+    }
+    __device__ __forceinline__ bool has(int v, int e) const { return ok[v]; }
+    // what a slot holds where it has no column: zeros
+    __device__ __forceinline__ void clean(int v, float2 (&x)[P]) const {
+        if constexpr (E == 1) x[0].y = 0.f;
+        if (!ok[v]) {
+#pragma unroll
+            for (int q = 0; q < P; ++q) x[q] = make_float2(0.f, 0.f);
+        }
+    }
+    __device__ __forceinline__ void get(const raw_t (&r)[V], float2 (&x)[V][P]) const {
+#pragma unroll
+        for (int v = 0; v < V; ++v) Raw::get(r[v], x[v]);
     }
     __device__ __forceinline__ int col(int v) const { return (v * G + gl) * E; }
     __device__ __forceinline__ long long at(long long row, int v) const { return row * C + col(v); }
@@ -136,49 +155,239 @@ struct LnRow {
     }
 };
 
+// LnShiftedRow: any C, arrays aligned to 16 bytes.  A row then starts anywhere within a vector, m columns behind its start; rows E
+// apart start at the same place, and a group's rows are a multiple of 8 apart.  So slot v of lane gl holds, for all the group's
+// rows, the columns from (v G + gl) E - m on, which are whole vectors of the array; those at the row's ends hold columns of
+// the rows beside it as well, which count as zeros and are written column by column.
+template <typename T_, int E_, int G_, int V_>
+struct LnShiftedRow {
+    using T = T_;
+    static constexpr int E = E_, G = G_, V = V_, P = E / 2;
+    static constexpr bool kShifted = true;
+    static constexpr int L = kCkptBlock / E;   // lanes whose slots make a checkpoint's block, but for the m columns before it
+    static_assert(G % L == 0, "a block's lanes are one group's");
+    static constexpr unsigned kAll = (1u << E) - 1u;
+    using Raw = ColVec<T, E>;
+    using raw_t = typename Raw::type;
+    struct Packed {
+        unsigned w[E / 4];
+        unsigned s, before;   // the scale bytes of the slot's block and, for its first m columns, of the block before
+    };
+    int gl, C, m;
+    long long total;          // the array's values
+    unsigned mask[V];         // the slot's columns that are the row's
+    bool head;                // the slots begin m columns before a block
+    __device__ __forceinline__ LnShiftedRow(const LnArgs &a, int gl_, long long first_row) : gl(gl_), C(a.C), total(a.n * a.C) {
+        m = (int)(first_row * C % E);
+        head = m > 0 && gl % L == 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            mask[v] = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) mask[v] |= (unsigned)(col(v) + e >= 0 && col(v) + e < C) << e;
+        }
+    }
+    __device__ __forceinline__ int col(int v) const { return (v * G + gl) * E - m; }
+    __device__ __forceinline__ long long at(long long row, int v) const { return row * C + col(v); }
+    __device__ __forceinline__ bool has(int v, int e) const { return mask[v] >> e & 1u; }
+    // the vector reaches past the array's end
+    __device__ __forceinline__ bool beyond(long long row, int v) const { return at(row, v) + E > total; }
+    __device__ __forceinline__ void clean(int v, float2 (&x)[P]) const {
+        if (mask[v] == kAll) return;
+#pragma unroll
+        for (int q = 0; q < P; ++q) x[q] = make_float2(has(v, 2 * q) ? x[q].x : 0.f, has(v, 2 * q + 1) ? x[q].y : 0.f);
+    }
+    __device__ __forceinline__ void get(const raw_t (&r)[V], float2 (&x)[V][P]) const {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            Raw::get(r[v], x[v]);
+            clean(v, x[v]);
+        }
+    }
+    __device__ __forceinline__ void ask(const void *base, long long row, bool live, raw_t (&r)[V]) const {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            r[v] = raw_t{};
+            if (!live || mask[v] == 0u) continue;
+            const T *p = static_cast<const T *>(base) + at(row, v);
+            if (!beyond(row, v)) {
+                r[v] = *reinterpret_cast<const raw_t *>(p);
+            } else {
+                float2 x[P];
+#pragma unroll
+                for (int q = 0; q < P; ++q) x[q] = make_float2(has(v, 2 * q) ? (float)p[2 * q] : 0.f, has(v, 2 * q + 1) ? (float)p[2 * q + 1] : 0.f);
+                r[v] = Raw::put(x);
+            }
+        }
+    }
+    __device__ __forceinline__ void put(void *base, long long row, const float2 (&x)[V][P]) const {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (mask[v] == 0u) continue;
+            T *p = static_cast<T *>(base) + at(row, v);
+            if (mask[v] == kAll) {
+                *reinterpret_cast<raw_t *>(p) = Raw::put(x[v]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (has(v, e)) Elem<T>::store1(p + e, e & 1 ? x[v][e / 2].y : x[v][e / 2].x);
+            }
+        }
+    }
+    __device__ __forceinline__ void cols(const float *p, float fill, float2 (&c)[V][P]) const {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int q = 0; q < P; ++q)
+                c[v][q] = make_float2(p && has(v, 2 * q) ? __ldg(p + col(v) + 2 * q) : fill, p && has(v, 2 * q + 1) ? __ldg(p + col(v) + 2 * q + 1) : fill);
+    }
+    // what the group's lane before the first of this lane's block holds in slot v: the block before
+    template <typename X>
+    __device__ __forceinline__ X before(const X (&x)[V], int v) const {
+        const int first = gl & ~(L - 1);
+        const X here = __shfl_sync(0xffffffffu, x[v], (first - L) & (G - 1), G), back = __shfl_sync(0xffffffffu, x[v > 0 ? v - 1 : 0], G - 1, G);
+        return first > 0 ? here : v > 0 ? back : X(0);
+    }
+    __device__ __forceinline__ void put_codes(const LnArgs &a, long long row, bool live, const float2 (&x)[V][P]) const {
+        float top[V], front[V], inv[V];   // front: of the m columns that belong to the block before
+        unsigned s[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            top[v] = front[v] = 0.f;
+            if (head) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float y = e & 1 ? x[v][e / 2].y : x[v][e / 2].x;
+                    front[v] = ckpt_top(front[v], e < m ? y : 0.f, 0.f);
+                    top[v] = ckpt_top(top[v], e < m ? 0.f : y, 0.f);
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < P; ++q) top[v] = ckpt_top(top[v], x[v][q].x, x[v][q].y);
+            }
+#pragma unroll
+            for (int d = 1; d < L; d <<= 1) top[v] = ckpt_top(top[v], __shfl_xor_sync(0xffffffffu, top[v], d, G), 0.f);
+        }
+        bool cut = false, bad = false;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int first = gl & ~(L - 1);
+            const float next = __shfl_sync(0xffffffffu, front[v], (first + L) & (G - 1), G), after = __shfl_sync(0xffffffffu, front[v + 1 < V ? v + 1 : v], 0, G);
+            top[v] = ckpt_top(top[v], first + L < G ? next : v + 1 < V ? after : 0.f, 0.f);
+            s[v] = ckpt_scale_byte(top[v]);
+            inv[v] = ckpt_inverse(s[v]);
+            cut = cut || top[v] * inv[v] >= 127.5f;
+            bad = bad || s[v] == 255u;
+        }
+        cut = __any_sync(0xffffffffu, cut);
+        bad = __any_sync(0xffffffffu, bad);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float inv_before = before(inv, v);
+            const unsigned s_before = before(s, v);
+            if (!live || mask[v] == 0u) continue;
+            unsigned w[E / 4];
+#pragma unroll
+            for (int q = 0; q < P; q += 2) {
+                float2 y[2] = {x[v][q], x[v][q + 1]}, i[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const bool fx = head && 2 * (q + h) < m, fy = head && 2 * (q + h) + 1 < m;
+                    i[h] = make_float2(fx ? inv_before : inv[v], fy ? inv_before : inv[v]);
+                    if (bad) y[h] = make_float2((fx ? s_before : s[v]) == 255u ? 0.f : y[h].x, (fy ? s_before : s[v]) == 255u ? 0.f : y[h].y);
+                }
+                w[q / 2] = ckpt_codes4(y[0], y[1], i[0], i[1], cut);
+            }
+            int8_t *p = a.codes + at(row, v);
+            if (mask[v] == kAll) {
+                if constexpr (E == 8) *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+                else *reinterpret_cast<unsigned *>(p) = w[0];
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (has(v, e)) p[e] = (int8_t)(w[e / 4] >> (e % 4 * 8));
+            }
+            const int block = (v * G + gl) / L;
+            if (gl % L == 0 && block < a.nb) a.scales[row * a.nb + block] = (uint8_t)s[v];
+        }
+    }
+    __device__ __forceinline__ void ask(const LnArgs &a, long long row, bool live, Packed (&r)[V]) const {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            r[v] = Packed{};
+            if (!live || mask[v] == 0u) continue;
+            const int8_t *p = a.codes + at(row, v);
+            if (!beyond(row, v)) {
+                if constexpr (E == 8) {
+                    const uint2 c = __ldg(reinterpret_cast<const uint2 *>(p));
+                    r[v].w[0] = c.x, r[v].w[1] = c.y;
+                } else {
+                    r[v].w[0] = __ldg(reinterpret_cast<const unsigned *>(p));
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (has(v, e)) r[v].w[e / 4] |= (unsigned)(unsigned char)p[e] << (e % 4 * 8);
+            }
+            const int block = (v * G + gl) / L;
+            if (block < a.nb) r[v].s = __ldg(a.scales + row * a.nb + block);
+            if (head && block > 0) r[v].before = __ldg(a.scales + row * a.nb + block - 1);
+        }
+    }
+    __device__ __forceinline__ void decode(const Packed (&r)[V], float2 (&x)[V][P]) const {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float here = ckpt_scale(r[v].s), front = head ? ckpt_scale(r[v].before) : here;
+#pragma unroll
+            for (int q = 0; q < P; ++q)
+                x[v][q] = ckpt_decode2(r[v].w[q / 2] ^ 0x80808080u, 2 * q & 3, make_float2(2 * q < m ? front : here, 2 * q + 1 < m ? front : here));
+            clean(v, x[v]);
+        }
+    }
+};
+
 // Blocks that an SM is to hold at least, which bounds the registers, for N columns a lane.  A million rows of 256 columns, us:
 // bf16 forward 106 registers 190, 80 (three blocks) 171; backward 138 344, 128 (two) 252, from the checkpoint 140 429, 128 245;
 // float32 forward with the checkpoint 84 472, 78 (three) 397; backward from it 102 483, 80 (three) 392.
-constexpr int ln_blocks(int N, int E, bool bwd, bool ck) {
-    return N > 16 ? 1 : E == 8 ? (bwd || ck ? 2 : 3) : E == 4 ? (N > 8 ? 1 : bwd && !ck ? 2 : 3) : N > 8 ? 1 : bwd && N > 4 ? 2 : 3;
+template <typename Row>
+constexpr int ln_blocks(bool bwd, bool ck) {
+    constexpr int N = Row::E * Row::V;
+    if (Row::kShifted) return N > 16 ? 1 : 2;
+    return N > 16 ? 1 : Row::E == 8 ? (bwd || ck ? 2 : 3) : Row::E == 4 ? (N > 8 ? 1 : bwd && !ck ? 2 : 3) : N > 8 ? 1 : bwd && N > 4 ? 2 : 3;
 }
 
 // Rows are walked one ahead: a group asks for its next row before it works on the one it has (two sets of registers in turn),
 // so that loads are in flight all the time.
-template <typename T, int E, int G, int V, bool CK>
-__global__ void __launch_bounds__(kThreads, ln_blocks(E * V, E, false, CK)) ln_fwd_kernel(const LnArgs a) {
+template <typename Row, bool CK>
+__global__ void __launch_bounds__(kThreads, ln_blocks<Row>(false, CK)) ln_fwd_kernel(const LnArgs a) {
     after_predecessor();
-    using Row = LnRow<T, E, G, V>;
-    constexpr int P = Row::P;
+    constexpr int G = Row::G, V = Row::V, P = Row::P;
     const LaneId<G> id;
-    const Row r(a, id.gl);
+    const long long stride = (long long)gridDim.x * kWarpsPerBlock * (32 / G);
+    long long base = ((long long)blockIdx.x * kWarpsPerBlock + id.warp) * (32 / G);   // the warp's first row: the shuffles need all its lanes
+    const Row r(a, id.gl, base + id.gid);
     float2 ga[V][P], be[V][P];
     r.cols(a.gamma, 1.f, ga);
     r.cols(a.beta, 0.f, be);
-    const long long stride = (long long)gridDim.x * kWarpsPerBlock * (32 / G);
-    long long base = ((long long)blockIdx.x * kWarpsPerBlock + id.warp) * (32 / G);   // the warp's first row: the shuffles need all its lanes
     const auto ask = [&](long long base, typename Row::raw_t(&raw)[V]) { r.ask(a.x, base + id.gid, base + id.gid < a.n, raw); };
     const auto work = [&](long long base, const typename Row::raw_t(&raw)[V]) {
         const long long row = base + id.gid;
         const bool live = row < a.n;
         float2 x[V][P], sum = make_float2(0.f, 0.f);
+        r.get(raw, x);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            Row::Raw::get(raw[v], x[v]);
+        for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int q = 0; q < P; ++q) sum = __fadd2_rn(sum, x[v][q]);   // a slot without columns holds zeros
-        }
+            for (int q = 0; q < P; ++q) sum = __fadd2_rn(sum, x[v][q]);   // what is no column is zero
         const float mean = ln_sum<G>(sum.x + sum.y) * a.inv_c;
-        const float2 shift = make_float2(-mean, E == 1 ? 0.f : -mean);
         float2 dev = make_float2(0.f, 0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            if (!r.ok[v]) continue;
 #pragma unroll
-            for (int q = 0; q < P; ++q) {
-                x[v][q] = __fadd2_rn(x[v][q], shift);
-                dev = __ffma2_rn(x[v][q], x[v][q], dev);
-            }
+            for (int q = 0; q < P; ++q) x[v][q] = __fadd2_rn(x[v][q], ln_splat(-mean));
+            r.clean(v, x[v]);
+#pragma unroll
+            for (int q = 0; q < P; ++q) dev = __ffma2_rn(x[v][q], x[v][q], dev);
         }
         const float rstd = __frsqrt_rn(fmaf(ln_sum<G>(dev.x + dev.y), a.inv_c, a.eps));
 #pragma unroll
@@ -208,22 +417,21 @@ __global__ void __launch_bounds__(kThreads, ln_blocks(E * V, E, false, CK)) ln_f
     }
 }
 
-template <typename T, int E, int G, int V, bool CK>
-__global__ void __launch_bounds__(kThreads, ln_blocks(E * V, E, true, CK)) ln_bwd_kernel(const LnArgs a) {
+template <typename Row, bool CK>
+__global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_kernel(const LnArgs a) {
     after_predecessor();
-    using Row = LnRow<T, E, G, V>;
-    constexpr int P = Row::P;
-    extern __shared__ float smem[];   // [2][C]
+    constexpr int G = Row::G, V = Row::V, P = Row::P;
+    extern __shared__ float smem[];   // [copies][2][C]
     const LaneId<G> id;
-    const Row r(a, id.gl);
+    const long long stride = (long long)gridDim.x * kWarpsPerBlock * (32 / G);
+    long long base = ((long long)blockIdx.x * kWarpsPerBlock + id.warp) * (32 / G);
+    const Row r(a, id.gl, base + id.gid);
     float2 ga[V][P], s0[V][P], s1[V][P];
     r.cols(a.gamma, 1.f, ga);
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int q = 0; q < P; ++q) s0[v][q] = s1[v][q] = make_float2(0.f, 0.f);
-    const long long stride = (long long)gridDim.x * kWarpsPerBlock * (32 / G);
-    long long base = ((long long)blockIdx.x * kWarpsPerBlock + id.warp) * (32 / G);
     struct Asked {
         typename Row::raw_t x[CK ? 1 : V], g[V];
         typename Row::Packed c[CK ? V : 1];
@@ -243,22 +451,22 @@ __global__ void __launch_bounds__(kThreads, ln_blocks(E * V, E, true, CK)) ln_bw
         float2 x[V][P], g[V][P], along2 = make_float2(0.f, 0.f), level2 = along2;
         const float2 rs = ln_splat(in.rs);
         if constexpr (CK) r.decode(in.c, x);
+        else r.get(in.x, x);
+        r.get(in.g, g);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if constexpr (!CK) {
-                const float2 shift = make_float2(-in.mu, E == 1 ? 0.f : -in.mu);
-                Row::Raw::get(in.x[v], x[v]);
 #pragma unroll
-                for (int q = 0; q < P; ++q) x[v][q] = __fmul2_rn(__fadd2_rn(x[v][q], shift), rs);   // xhat; where there is no column, g is zero
+                for (int q = 0; q < P; ++q) x[v][q] = __fmul2_rn(__fadd2_rn(x[v][q], ln_splat(-in.mu)), rs);   // xhat
+                r.clean(v, x[v]);
             }
-            Row::Raw::get(in.g[v], g[v]);
 #pragma unroll
             for (int q = 0; q < P; ++q) {
                 s0[v][q] = __fadd2_rn(s0[v][q], g[v][q]);
-                if (CK || r.ok[v]) s1[v][q] = __ffma2_rn(g[v][q], x[v][q], s1[v][q]);
+                s1[v][q] = __ffma2_rn(g[v][q], x[v][q], s1[v][q]);
                 g[v][q] = __fmul2_rn(g[v][q], ga[v][q]);
                 level2 = __fadd2_rn(level2, g[v][q]);
-                if (CK || r.ok[v]) along2 = __ffma2_rn(g[v][q], x[v][q], along2);   // not 0 * xhat: a row of infinite mean would spoil it
+                along2 = __ffma2_rn(g[v][q], x[v][q], along2);
             }
         }
         const float level = ln_sum<G>(level2.x + level2.y) * a.inv_c;
@@ -281,35 +489,99 @@ __global__ void __launch_bounds__(kThreads, ln_blocks(E * V, E, true, CK)) ln_bw
         work(base + stride, two);
     }
     if (!a.partial) return;
-    // the groups of a warp first, then the warps one after the other
+    // The groups of a warp, then the warps, which have a copy each where they fit (one after the other otherwise).  Rows that start at
+    // different places of a vector have different columns in a lane: their groups add to shared memory in turn.
+    if constexpr (!Row::kShifted) {
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+        for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int q = 0; q < P; ++q) {
+            for (int q = 0; q < P; ++q) {
 #pragma unroll
-            for (int d = 16; d >= G; d >>= 1) {
-                s0[v][q].x += __shfl_xor_sync(0xffffffffu, s0[v][q].x, d);
-                s0[v][q].y += __shfl_xor_sync(0xffffffffu, s0[v][q].y, d);
-                s1[v][q].x += __shfl_xor_sync(0xffffffffu, s1[v][q].x, d);
-                s1[v][q].y += __shfl_xor_sync(0xffffffffu, s1[v][q].y, d);
-            }
-        }
-    for (int w = 0; w < kWarpsPerBlock; ++w) {
-        if (id.warp == w && id.gid == 0) {
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (r.ok[v]) {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const int c = r.col(v) + e;
-                        smem[c] = (w ? smem[c] : 0.f) + (e & 1 ? s1[v][e / 2].y : s1[v][e / 2].x);
-                        smem[a.C + c] = (w ? smem[a.C + c] : 0.f) + (e & 1 ? s0[v][e / 2].y : s0[v][e / 2].x);
-                    }
+                for (int d = 16; d >= G; d >>= 1) {
+                    s0[v][q].x += __shfl_xor_sync(0xffffffffu, s0[v][q].x, d);
+                    s0[v][q].y += __shfl_xor_sync(0xffffffffu, s0[v][q].y, d);
+                    s1[v][q].x += __shfl_xor_sync(0xffffffffu, s1[v][q].x, d);
+                    s1[v][q].y += __shfl_xor_sync(0xffffffffu, s1[v][q].y, d);
                 }
+            }
+    }
+    const int copies = ln_copies(a.C);
+    float *mine = smem + (copies > 1 ? id.warp * 2 * a.C : 0);
+    for (int w = 0; w < kWarpsPerBlock / copies; ++w) {
+        if (copies > 1 || id.warp == w) {
+            for (int t = 0; t < (Row::kShifted ? 32 / G : 1); ++t) {
+                if (id.gid == t) {
+                    const bool begin = w == 0 && t == 0;
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+#pragma unroll
+                        for (int e = 0; e < Row::E; ++e)
+                            if (r.has(v, e)) {
+                                float *p = mine + r.col(v) + e;
+                                p[0] = (begin ? 0.f : p[0]) + (e & 1 ? s1[v][e / 2].y : s1[v][e / 2].x);
+                                p[a.C] = (begin ? 0.f : p[a.C]) + (e & 1 ? s0[v][e / 2].y : s0[v][e / 2].x);
+                            }
+                }
+                __syncwarp();
+            }
         }
         __syncthreads();
     }
-    for (int c = threadIdx.x; c < 2 * a.C; c += kThreads) a.partial[(size_t)blockIdx.x * 2 * a.C + c] = smem[c];
+    for (int c = threadIdx.x; c < 2 * a.C; c += kThreads) {
+        float acc = smem[c];
+        for (int k = 1; k < copies; ++k) acc += smem[k * 2 * a.C + c];
+        a.partial[(size_t)blockIdx.x * 2 * a.C + c] = acc;
+    }
+}
+
+// ---- checkpoints of rows that are no whole number of vectors ------------------------------------------------------------------
+template <typename Row>
+__global__ void __launch_bounds__(kThreads, 2) ln_pack_kernel(const LnArgs a) {
+    after_predecessor();
+    constexpr int G = Row::G, V = Row::V, P = Row::P;
+    const LaneId<G> id;
+    const long long stride = (long long)gridDim.x * kWarpsPerBlock * (32 / G);
+    long long base = ((long long)blockIdx.x * kWarpsPerBlock + id.warp) * (32 / G);
+    const Row r(a, id.gl, base + id.gid);
+    const auto ask = [&](long long base, typename Row::raw_t(&raw)[V]) { r.ask(a.x, base + id.gid, base + id.gid < a.n, raw); };
+    const auto work = [&](long long base, const typename Row::raw_t(&raw)[V]) {
+        float2 x[V][P];
+        r.get(raw, x);
+        r.put_codes(a, base + id.gid, base + id.gid < a.n, x);
+    };
+    typename Row::raw_t one[V], two[V];
+    if (base < a.n) ask(base, one);
+    for (; base < a.n; base += 2 * stride) {
+        ask(base + stride, two);
+        work(base, one);
+        if (base + stride >= a.n) break;
+        ask(base + 2 * stride, one);
+        work(base + stride, two);
+    }
+}
+
+template <typename Row>
+__global__ void __launch_bounds__(kThreads, 2) ln_unpack_kernel(const LnArgs a) {
+    after_predecessor();
+    constexpr int G = Row::G, V = Row::V, P = Row::P;
+    const LaneId<G> id;
+    const long long stride = (long long)gridDim.x * kWarpsPerBlock * (32 / G);
+    long long row = ((long long)blockIdx.x * kWarpsPerBlock + id.warp) * (32 / G) + id.gid;
+    const Row r(a, id.gl, row);
+    const auto work = [&](long long row, const typename Row::Packed(&raw)[V]) {
+        float2 x[V][P];
+        r.decode(raw, x);
+        r.put(a.y, row, x);
+    };
+    typename Row::Packed one[V], two[V];
+    r.ask(a, row, row < a.n, one);
+    for (; row < a.n; row += 2 * stride) {
+        r.ask(a, row + stride, row + stride < a.n, two);
+        work(row, one);
+        if (row + stride >= a.n) break;
+        r.ask(a, row + 2 * stride, row + 2 * stride < a.n, one);
+        work(row + stride, two);
+    }
 }
 
 // ---- rows longer than the registers of a warp: a block takes a row and reads it again for every pass (from L1 or L2) ----------
@@ -411,92 +683,164 @@ __global__ void __launch_bounds__(kThreads) ln_long_sums_kernel(const LnArgs a, 
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------
-// How rows of C columns are spread over lanes: E columns a slot, V slots in G lanes; E = 0: longer than a warp's registers.
+// How rows of C columns are spread over lanes: E columns a slot, V slots in G lanes, shifted or not; E = 0: longer than a warp's
+// registers.
 struct LnShape {
     int E, G, V;
+    bool shifted;
 };
-template <typename T, int E, int G, int V>
-struct LnCfg {
-    using type = T;
-    static constexpr int e = E, g = G, v = V;
-};
-// Every (G, V) of a width E in ascending G V E: the first that covers C is taken.  16 columns a lane of bf16 and 8 of float32 or
-// single ones where that covers the row, more only where 32 lanes do not.
+// Every (E, G, V) of a kind of row in ascending E G V: the first that covers the row is taken.
 #define SAR_LN_8(X) X(8, 4, 1) X(8, 4, 2) X(8, 4, 3) X(8, 8, 2) X(8, 8, 3) X(8, 16, 2) X(8, 16, 3) X(8, 32, 2) X(8, 32, 3) X(8, 32, 4)
 #define SAR_LN_4(X) X(4, 4, 1) X(4, 4, 2) X(4, 8, 2) X(4, 8, 3) X(4, 16, 2) X(4, 16, 3) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6) X(4, 32, 8)
-#define SAR_LN_1(X) X(1, 4, 1) X(1, 4, 4) X(1, 4, 8) X(1, 8, 6) X(1, 8, 8) X(1, 16, 6) X(1, 16, 8) X(1, 32, 6) X(1, 32, 8) X(1, 32, 12) X(1, 32, 16) X(1, 32, 24) X(1, 32, 32)
+#define SAR_LN_8S(X) X(8, 16, 2) X(8, 32, 2) X(8, 32, 3) X(8, 32, 4)
+#define SAR_LN_4S(X) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6) X(4, 32, 8)
+// ... and narrow shifted rows, for checkpoints alone
+#define SAR_LN_8N(X) X(8, 4, 1) X(8, 4, 2) X(8, 8, 2)
+#define SAR_LN_4N(X) X(4, 8, 1) X(4, 8, 2) X(4, 16, 2)
+#define SAR_LN_1(X) X(1, 4, 1) X(1, 4, 4) X(1, 4, 8) X(1, 8, 6) X(1, 8, 8) X(1, 16, 6) X(1, 16, 8) X(1, 32, 8) X(1, 32, 32)
 // ... and of single columns in the backward pass, which carries two sums for each of them
-#define SAR_LN_1B(X) X(1, 4, 1) X(1, 4, 4) X(1, 8, 4) X(1, 16, 3) X(1, 16, 4) X(1, 32, 3) X(1, 32, 4) X(1, 32, 6) X(1, 32, 8) X(1, 32, 12) X(1, 32, 16) X(1, 32, 24) X(1, 32, 32)
+#define SAR_LN_1B(X) X(1, 4, 1) X(1, 4, 4) X(1, 8, 4) X(1, 16, 3) X(1, 16, 4) X(1, 32, 3) X(1, 32, 4) X(1, 32, 8) X(1, 32, 32)
+// Columns from which rows that are no whole vectors are taken shifted.  64 million values, us, one column a lane and slot against
+// shifted: 95 bf16 forward 93 / 96, with checkpoint 187 / 205, backward 157 / 162; 191 bf16 111 / 97, 265 / 203, 191 / 159; 191
+// float32 123 / 113, 289 / 275, 169 / 156.  Checkpoints: 47 bf16 packed 173 / 141, unpacked 117 / 99.
+constexpr int kLnShiftedFrom = 128, kCkptShiftedFrom = 16;
 
-// blocks of a kernel that run at once: each walks its rows (a constant of the kernel and the device; 48 KB of shared memory and less)
+template <typename R>
+struct LnCfg {
+    using row = R;
+};
+// Calls f(LnCfg<row>{}) with the shape's kind of row.
+enum LnPass { kLnFwd, kLnBwd, kLnCkpt };   // kLnCkpt: packing and unpacking of shifted rows alone
+template <typename T, LnPass PASS, typename Fn>
+static inline sar_status ln_dispatch(const LnShape &s, Fn &&f) {
+#define SAR_LN_CASE(EE, GG, VV) \
+    if (!s.shifted && s.E == EE && s.G == GG && s.V == VV) return f(LnCfg<LnRow<T, EE, GG, VV>>{});
+#define SAR_LN_SHIFTED(EE, GG, VV) \
+    if (s.shifted && s.E == EE && s.G == GG && s.V == VV) return f(LnCfg<LnShiftedRow<T, EE, GG, VV>>{});
+    if constexpr (sizeof(T) == 2) {
+        SAR_LN_8S(SAR_LN_SHIFTED)
+    } else {
+        SAR_LN_4S(SAR_LN_SHIFTED)
+    }
+    if constexpr (PASS == kLnCkpt) {
+        if constexpr (sizeof(T) == 2) {
+            SAR_LN_8N(SAR_LN_SHIFTED)
+        } else {
+            SAR_LN_4N(SAR_LN_SHIFTED)
+        }
+    } else {
+        if constexpr (sizeof(T) == 2) {
+            SAR_LN_8(SAR_LN_CASE)
+        }
+        SAR_LN_4(SAR_LN_CASE)
+        if constexpr (PASS == kLnBwd) {
+            SAR_LN_1B(SAR_LN_CASE)
+        } else {
+            SAR_LN_1(SAR_LN_CASE)
+        }
+    }
+#undef SAR_LN_CASE
+#undef SAR_LN_SHIFTED
+    return SAR_ERR_UNSUPPORTED;
+}
+
+// The shape for rows of C columns of type t in arrays aligned to `arrays` bytes and codes aligned to `codes`: as many columns at a
+// time as divide C and are aligned; rows that allow one at a time are taken shifted where they are wide and the arrays aligned.
+static inline LnShape ln_shape(int32_t C, sar_dtype t, LnPass pass, size_t arrays, size_t codes) {
+    LnShape s{0, 32, 0, false};
+    const int E = t == SAR_BF16 ? 8 : 4;
+    const auto may = [&](int e) { return C % e == 0 && arrays >= e * sar_elem_size(t) && codes >= (size_t)e; };
+    int need = C;
+#define SAR_LN_FIT(EE, GG, VV) \
+    if (s.E == 0 && EE * GG * VV >= need) s.E = EE, s.G = GG, s.V = VV;
+    if (E == 8 && may(8)) {
+        SAR_LN_8(SAR_LN_FIT)
+    } else if (may(4)) {
+        SAR_LN_4(SAR_LN_FIT)
+    } else if (C >= (pass == kLnCkpt ? kCkptShiftedFrom : kLnShiftedFrom) && arrays >= 16 && codes >= (size_t)E) {
+        s.shifted = true;
+        need = C + E - 1;   // wherever in a vector the row starts
+        if (E == 8) {
+            if (pass == kLnCkpt) {
+                SAR_LN_8N(SAR_LN_FIT)
+            }
+            SAR_LN_8S(SAR_LN_FIT)
+        } else {
+            if (pass == kLnCkpt) {
+                SAR_LN_4N(SAR_LN_FIT)
+            }
+            SAR_LN_4S(SAR_LN_FIT)
+        }
+    } else if (pass == kLnBwd) {
+        SAR_LN_1B(SAR_LN_FIT)
+    } else {
+        SAR_LN_1(SAR_LN_FIT)
+    }
+#undef SAR_LN_FIT
+    return s;
+}
+
+// the largest power of two up to 16 that divides all addresses
+static inline size_t ln_alignment(std::initializer_list<const void *> ps) {
+    size_t a = 16;
+    for (const void *p : ps)
+        while (a > 1 && p && !sar_aligned(p, a)) a /= 2;
+    return a;
+}
+
+static inline LnArgs ln_args(int64_t n, int32_t C) {
+    LnArgs a{};
+    a.n = n;
+    a.C = C;
+    a.inv_c = 1.f / (float)C;
+    a.nb = (int)ckpt_blocks(C);
+    return a;
+}
+
+// blocks of a kernel that run at once: each walks its rows (a constant of the kernel and the device)
 template <typename K>
 static unsigned ln_resident(K kernel, size_t smem) {
     int per_sm = 0;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kThreads, smem) != cudaSuccess) (void)cudaGetLastError();
     return (unsigned)(kSms * (per_sm < 1 ? 1 : per_sm > kLnBlocks / kSms ? kLnBlocks / kSms : per_sm));
 }
-
-template <typename T, bool BWD, typename Fn>
-static inline sar_status ln_dispatch(const LnShape &s, Fn &&f) {
-#define SAR_LN_CASE(EE, GG, VV) \
-    if (s.E == EE && s.G == GG && s.V == VV) return f(LnCfg<T, EE, GG, VV>{});
-    if constexpr (sizeof(T) == 2) {
-        SAR_LN_8(SAR_LN_CASE)
-    }
-    SAR_LN_4(SAR_LN_CASE)
-    if constexpr (BWD) {
-        SAR_LN_1B(SAR_LN_CASE)
-    } else {
-        SAR_LN_1(SAR_LN_CASE)
-    }
-#undef SAR_LN_CASE
-    return SAR_ERR_UNSUPPORTED;
+template <typename K>
+static sar_status ln_launch(const char *name, K kernel, unsigned want, unsigned most, size_t smem, const LnArgs &a, cudaStream_t st) {
+    SAR_LAUNCH(name, st, launch_if(a.n * a.C <= kOverlapElems, kernel, want < 1 ? 1 : want < most ? want : most, kThreads, smem, st, a));
+    return sar_after_launch();
 }
 
 template <typename T, bool CK>
 static sar_status ln_forward_of(const LnShape &s, const LnArgs &a, cudaStream_t st) {
-    const bool overlap = a.n * a.C <= kOverlapElems;
     const char *name = CK ? "ln_fwd_ckpt8" : "ln_fwd";
-    if (s.E == 0) {
-        const unsigned blocks = (unsigned)(a.n < kLnBlocks ? a.n : kLnBlocks);
-        SAR_LAUNCH(name, st, launch_if(overlap, ln_fwd_long_kernel<T, CK>, blocks, kThreads, 0, st, a));
-        return sar_after_launch();
-    }
-    return ln_dispatch<T, false>(s, [&](auto cfg) -> sar_status {
-        using K = decltype(cfg);
-        static const unsigned most = ln_resident(ln_fwd_kernel<T, K::e, K::g, K::v, CK>, 0);
-        const unsigned want = blocks_for(a.n, K::g), blocks = want < most ? want : most;
-        SAR_LAUNCH(name, st, launch_if(overlap, ln_fwd_kernel<T, K::e, K::g, K::v, CK>, blocks, kThreads, 0, st, a));
-        return sar_after_launch();
+    if (s.E == 0) return ln_launch(name, ln_fwd_long_kernel<T, CK>, (unsigned)(a.n < kLnBlocks ? a.n : kLnBlocks), kLnBlocks, 0, a, st);
+    return ln_dispatch<T, kLnFwd>(s, [&](auto cfg) -> sar_status {
+        using Row = typename decltype(cfg)::row;
+        static const unsigned most = ln_resident(ln_fwd_kernel<Row, CK>, 0);
+        return ln_launch(name, ln_fwd_kernel<Row, CK>, blocks_for(a.n, Row::G), most, 0, a, st);
     });
 }
 
 // the row pass and the records of the weights' sums (a.partial); *records: how many
 template <typename T, bool CK>
 static sar_status ln_backward_of(const LnShape &s, const LnArgs &a, unsigned *records, cudaStream_t st) {
-    const bool overlap = a.n * a.C <= kOverlapElems;
     const char *name = CK ? "ln_bwd_ckpt8" : "ln_bwd";
     if (s.E == 0) {
         // the sums first: gx may be written over gy or x
-        const int slices = (int)((a.n + 63) / 64 < 148 ? (a.n + 63) / 64 : 148);
+        const int slices = (int)((a.n + 63) / 64 < kSms ? (a.n + 63) / 64 : kSms);
         if (a.partial) {
-            SAR_LAUNCH("ln_bwd_sums", st, launch_if(overlap, ln_long_sums_kernel<T, CK>, (unsigned)(((long long)slices * a.C + kThreads - 1) / kThreads), kThreads, 0, st, a, slices));
+            SAR_LAUNCH("ln_bwd_sums", st, launch_if(a.n * a.C <= kOverlapElems, ln_long_sums_kernel<T, CK>, (unsigned)(((long long)slices * a.C + kThreads - 1) / kThreads), kThreads, 0, st, a, slices));
             SAR_TRY(sar_after_launch());
         }
         *records = (unsigned)slices;
-        const unsigned blocks = (unsigned)(a.n < kLnBlocks ? a.n : kLnBlocks);
-        SAR_LAUNCH(name, st, launch_if(overlap, ln_bwd_long_kernel<T, CK>, blocks, kThreads, 0, st, a));
-        return sar_after_launch();
+        return ln_launch(name, ln_bwd_long_kernel<T, CK>, (unsigned)(a.n < kLnBlocks ? a.n : kLnBlocks), kLnBlocks, 0, a, st);
     }
-    return ln_dispatch<T, true>(s, [&](auto cfg) -> sar_status {
-        using K = decltype(cfg);
-        // a few rows per lane group before a block pays for its record
-        const unsigned want = blocks_for((a.n + 3) / 4, K::g);
-        static const unsigned most = ln_resident(ln_bwd_kernel<T, K::e, K::g, K::v, CK>, 2 * kLnRowCols * sizeof(float));
-        const unsigned blocks = want < 1 ? 1 : want < most ? want : most;
-        *records = blocks;
-        SAR_LAUNCH(name, st, launch_if(overlap, ln_bwd_kernel<T, K::e, K::g, K::v, CK>, blocks, kThreads, a.partial ? (size_t)2 * a.C * 4 : 0, st, a));
-        return sar_after_launch();
+    return ln_dispatch<T, kLnBwd>(s, [&](auto cfg) -> sar_status {
+        using Row = typename decltype(cfg)::row;
+        static const unsigned most = ln_resident(ln_bwd_kernel<Row, CK>, kLnSmem);
+        const unsigned want = blocks_for((a.n + 3) / 4, Row::G);   // a few rows per lane group before a block pays for its record
+        *records = want < 1 ? 1 : want < most ? want : most;
+        return ln_launch(name, ln_bwd_kernel<Row, CK>, want, most, a.partial ? (size_t)ln_copies(a.C) * 2 * a.C * 4 : 0, a, st);
     });
 }
 
@@ -505,5 +849,8 @@ sar_status ln_forward_f32(const LnShape &s, const LnArgs &a, bool ckpt, cudaStre
 sar_status ln_forward_bf16(const LnShape &s, const LnArgs &a, bool ckpt, cudaStream_t st);
 sar_status ln_backward_f32(const LnShape &s, const LnArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
 sar_status ln_backward_bf16(const LnShape &s, const LnArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
+// checkpoints of rows of a shifted shape: x -> codes and scales, and back to y
+sar_status ln_checkpoint_f32(const LnShape &s, const LnArgs &a, bool unpack, cudaStream_t st);
+sar_status ln_checkpoint_bf16(const LnShape &s, const LnArgs &a, bool unpack, cudaStream_t st);
 
 }  // namespace sar
