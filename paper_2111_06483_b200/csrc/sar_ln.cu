@@ -70,7 +70,7 @@ static sar_status ln_bwd_entry(int64_t n, int32_t C, sar_dtype t, const void *x,
                                void *workspace, size_t workspace_bytes, void *stream) {
     if (n < 0 || C < 1 || (n > 0 && (!rstd || !gy || !gx || (ckpt ? !codes || !scales : !x || !mean)))) return SAR_ERR_INVALID_ARG;
     SAR_TRY(ln_check(C, t));
-    const LnShape s = ln_shape(C, t, kLnBwd, ln_alignment({x, gy, gx}), ln_alignment({codes}));
+    const LnShape s = ln_shape(C, t, ckpt ? kLnBwd8 : kLnBwd, ln_alignment({x, gy, gx}), ln_alignment({codes}));
     SAR_TRY(check_elem_align({mean, rstd, gamma, dgamma, dbeta}, 4));
     SAR_TRY(check_elem_align({x, gy, gx}, sar_elem_size(t)));
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -534,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_ker
     }
 }
 
-// ---- checkpoints of rows that are no whole number of vectors ------------------------------------------------------------------
+// ---- checkpoints of rows whose last block is short ------------------------------------------------------------------
 template <typename Row>
 __global__ void __launch_bounds__(kThreads, 2) ln_pack_kernel(const LnArgs a) {
     after_predecessor();
@@ -694,7 +694,7 @@ struct LnShape {
 #define SAR_LN_4(X) X(4, 4, 1) X(4, 4, 2) X(4, 8, 2) X(4, 8, 3) X(4, 16, 2) X(4, 16, 3) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6) X(4, 32, 8)
 #define SAR_LN_8S(X) X(8, 16, 2) X(8, 32, 2) X(8, 32, 3) X(8, 32, 4)
 #define SAR_LN_4S(X) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6) X(4, 32, 8)
-// ... and narrow shifted rows, for checkpoints alone
+// ... and narrow shifted rows, for what reads checkpoints or only packs
 #define SAR_LN_8N(X) X(8, 4, 1) X(8, 4, 2) X(8, 8, 2)
 #define SAR_LN_4N(X) X(4, 8, 1) X(4, 8, 2) X(4, 16, 2)
 #define SAR_LN_1(X) X(1, 4, 1) X(1, 4, 4) X(1, 4, 8) X(1, 8, 6) X(1, 8, 8) X(1, 16, 6) X(1, 16, 8) X(1, 32, 8) X(1, 32, 32)
@@ -702,7 +702,8 @@ struct LnShape {
 #define SAR_LN_1B(X) X(1, 4, 1) X(1, 4, 4) X(1, 8, 4) X(1, 16, 3) X(1, 16, 4) X(1, 32, 3) X(1, 32, 4) X(1, 32, 8) X(1, 32, 32)
 // Columns from which rows that are no whole vectors are taken shifted.  64 million values, us, one column a lane and slot against
 // shifted: 95 bf16 forward 93 / 96, with checkpoint 187 / 205, backward 157 / 162; 191 bf16 111 / 97, 265 / 203, 191 / 159; 191
-// float32 123 / 113, 289 / 275, 169 / 156.  Checkpoints: 47 bf16 packed 173 / 141, unpacked 117 / 99.
+// float32 123 / 113, 289 / 275, 169 / 156.  Checkpoints: 47 bf16 packed 173 / 141, unpacked 117 / 99, backward from
+// one 228 / 180; 47 float32 191 / 189.
 constexpr int kLnShiftedFrom = 128, kCkptShiftedFrom = 16;
 
 template <typename R>
@@ -710,7 +711,7 @@ struct LnCfg {
     using row = R;
 };
 // Calls f(LnCfg<row>{}) with the shape's kind of row.
-enum LnPass { kLnFwd, kLnBwd, kLnCkpt };   // kLnCkpt: packing and unpacking of shifted rows alone
+enum LnPass { kLnFwd, kLnBwd, kLnBwd8, kLnCkpt };   // kLnBwd8: from a checkpoint; kLnCkpt: packing and unpacking
 template <typename T, LnPass PASS, typename Fn>
 static inline sar_status ln_dispatch(const LnShape &s, Fn &&f) {
 #define SAR_LN_CASE(EE, GG, VV) \
@@ -722,22 +723,21 @@ static inline sar_status ln_dispatch(const LnShape &s, Fn &&f) {
     } else {
         SAR_LN_4S(SAR_LN_SHIFTED)
     }
-    if constexpr (PASS == kLnCkpt) {
+    if constexpr (PASS == kLnCkpt || PASS == kLnBwd8) {
         if constexpr (sizeof(T) == 2) {
             SAR_LN_8N(SAR_LN_SHIFTED)
         } else {
             SAR_LN_4N(SAR_LN_SHIFTED)
         }
+    }
+    if constexpr (sizeof(T) == 2) {
+        SAR_LN_8(SAR_LN_CASE)
+    }
+    SAR_LN_4(SAR_LN_CASE)
+    if constexpr (PASS == kLnBwd || PASS == kLnBwd8) {
+        SAR_LN_1B(SAR_LN_CASE)
     } else {
-        if constexpr (sizeof(T) == 2) {
-            SAR_LN_8(SAR_LN_CASE)
-        }
-        SAR_LN_4(SAR_LN_CASE)
-        if constexpr (PASS == kLnBwd) {
-            SAR_LN_1B(SAR_LN_CASE)
-        } else {
-            SAR_LN_1(SAR_LN_CASE)
-        }
+        SAR_LN_1(SAR_LN_CASE)
     }
 #undef SAR_LN_CASE
 #undef SAR_LN_SHIFTED
@@ -749,6 +749,7 @@ static inline sar_status ln_dispatch(const LnShape &s, Fn &&f) {
 static inline LnShape ln_shape(int32_t C, sar_dtype t, LnPass pass, size_t arrays, size_t codes) {
     LnShape s{0, 32, 0, false};
     const int E = t == SAR_BF16 ? 8 : 4;
+    const bool from_ckpt = pass == kLnCkpt || pass == kLnBwd8;
     const auto may = [&](int e) { return C % e == 0 && arrays >= e * sar_elem_size(t) && codes >= (size_t)e; };
     int need = C;
 #define SAR_LN_FIT(EE, GG, VV) \
@@ -757,21 +758,21 @@ static inline LnShape ln_shape(int32_t C, sar_dtype t, LnPass pass, size_t array
         SAR_LN_8(SAR_LN_FIT)
     } else if (may(4)) {
         SAR_LN_4(SAR_LN_FIT)
-    } else if (C >= (pass == kLnCkpt ? kCkptShiftedFrom : kLnShiftedFrom) && arrays >= 16 && codes >= (size_t)E) {
+    } else if (C >= (from_ckpt ? kCkptShiftedFrom : kLnShiftedFrom) && arrays >= 16 && codes >= (size_t)E) {
         s.shifted = true;
         need = C + E - 1;   // wherever in a vector the row starts
         if (E == 8) {
-            if (pass == kLnCkpt) {
+            if (from_ckpt) {
                 SAR_LN_8N(SAR_LN_FIT)
             }
             SAR_LN_8S(SAR_LN_FIT)
         } else {
-            if (pass == kLnCkpt) {
+            if (from_ckpt) {
                 SAR_LN_4N(SAR_LN_FIT)
             }
             SAR_LN_4S(SAR_LN_FIT)
         }
-    } else if (pass == kLnBwd) {
+    } else if (pass == kLnBwd || pass == kLnBwd8) {
         SAR_LN_1B(SAR_LN_FIT)
     } else {
         SAR_LN_1(SAR_LN_FIT)
@@ -835,7 +836,7 @@ static sar_status ln_backward_of(const LnShape &s, const LnArgs &a, unsigned *re
         *records = (unsigned)slices;
         return ln_launch(name, ln_bwd_long_kernel<T, CK>, (unsigned)(a.n < kLnBlocks ? a.n : kLnBlocks), kLnBlocks, 0, a, st);
     }
-    return ln_dispatch<T, kLnBwd>(s, [&](auto cfg) -> sar_status {
+    return ln_dispatch<T, CK ? kLnBwd8 : kLnBwd>(s, [&](auto cfg) -> sar_status {
         using Row = typename decltype(cfg)::row;
         static const unsigned most = ln_resident(ln_bwd_kernel<Row, CK>, kLnSmem);
         const unsigned want = blocks_for((a.n + 3) / 4, Row::G);   // a few rows per lane group before a block pays for its record
@@ -849,7 +850,7 @@ sar_status ln_forward_f32(const LnShape &s, const LnArgs &a, bool ckpt, cudaStre
 sar_status ln_forward_bf16(const LnShape &s, const LnArgs &a, bool ckpt, cudaStream_t st);
 sar_status ln_backward_f32(const LnShape &s, const LnArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
 sar_status ln_backward_bf16(const LnShape &s, const LnArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
-// checkpoints of rows of a shifted shape: x -> codes and scales, and back to y
+// checkpoints row by row: x -> codes and scales, and back to y
 sar_status ln_checkpoint_f32(const LnShape &s, const LnArgs &a, bool unpack, cudaStream_t st);
 sar_status ln_checkpoint_bf16(const LnShape &s, const LnArgs &a, bool unpack, cudaStream_t st);
 
