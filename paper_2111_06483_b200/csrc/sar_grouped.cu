@@ -347,6 +347,7 @@ struct WeightArgs {
 };
 constexpr int kAdders = 8, kMakers = 8;   // warps; the adders' work is laid out for 8
 constexpr int kWeightThreads = 64 + kAdders * 32, kWeightThreads8 = kWeightThreads + kMakers * 32;
+constexpr uint32_t kTurnBuf = 32 * 64;    // an adder's 32 rows of 16 sums on their way out
 constexpr uint32_t kSumCols = 256;        // where the sums lie in tensor memory, behind the accumulators
 struct WeightShared {
     alignas(8) uint64_t full[kStagesMax], empty[kStagesMax], made[kStagesMax], acc_full[2], acc_empty[2];
@@ -360,7 +361,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     after_predecessor();
     extern __shared__ uint8_t dyn[];
     WeightShared &sh = *reinterpret_cast<WeightShared *>(dyn);
-    const uint32_t ring = (smem_addr(dyn) + (uint32_t)sizeof(WeightShared) + 1023u) & ~1023u;
+    const uint32_t turns = (smem_addr(dyn) + (uint32_t)sizeof(WeightShared) + 1023u) & ~1023u, ring = turns + kAdders * kTurnBuf;
     const int panels = p.cols / 64;
     const uint32_t panel = p.step * 128, stage_bytes = (p.h_panels + panels) * panel, dz_at = p.h_panels * panel;
     const uint32_t bufs = p.cols <= 128 ? 2 : 1;   // accumulators of 128 columns each, or one of up to 256
@@ -476,7 +477,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
         }
     } else if (warp < 2 + kAdders) {
         const uint32_t quad = warp & 3, part = (warp - 2) / 4, lanes = quad * 32 << 16;   // rows m0 + 32 quad + lane of dW, every other 32 columns
-        const int m = m0 + quad * 32 + lane;
+        const uint32_t turn_buf = turns + (warp - 2) * kTurnBuf;
         // The column sums of dz: panel quad, 8 columns of every fourth row of one half of a step, the steps shared by the blocks of a
         // chunk.  A thread's rows are 4 apart, so that their chunks lie at one of two places of the swizzle.
         const bool want_sums = CK && p.sums && (int)quad < panels;
@@ -488,7 +489,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
         for (int g = g0; ok && more(g); ++g) {
             int lo, hi;
             if (!segment(g, lo, hi)) continue;
-            float *out = p.part + ((long long)(chunk + g) * p.d_in + m) * p.d_out + n0;
+            float *out = p.part + ((long long)(chunk + g) * p.d_in + m0 + quad * 32) * p.d_out + n0;   // the warp's first row
             int turn = 0;   // the step's number modulo the tiles that share the sums
 #pragma unroll
             for (int e = 0; e < 4; ++e) cs[e] = make_float2(0.f, 0.f);
@@ -548,10 +549,27 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                     }
                     if (!last) {
                         tmem_store(tmem + kSumCols + c + lanes, x);
-                    } else if (m < p.d_in) {
+                    } else {
+                        // A thread has a row of 32 sums.  Written so, a store touches 32 lines (128 x 256 sums: 10,000 cycles); turned in
+                        // shared memory, where chunk q of row l lies at q ^ (l >> 1 & 3), it writes 64 bytes of 8 rows.
 #pragma unroll
-                        for (int q = 0; q < 8; ++q)
-                            if (c + q * 4 < cols) *reinterpret_cast<uint4 *>(out + c + q * 4) = make_uint4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+                        for (int f = 0; f < 2; ++f) {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(turn_buf + lane * 64 + ((q ^ (lane >> 1 & 3)) << 4)), "r"(x[f * 16 + q * 4]),
+                                             "r"(x[f * 16 + q * 4 + 1]), "r"(x[f * 16 + q * 4 + 2]), "r"(x[f * 16 + q * 4 + 3])
+                                             : "memory");
+                            __syncwarp();
+                            const int q = lane & 3, col = c + f * 16 + q * 4;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int r = i * 8 + (lane >> 2);
+                                uint4 v;
+                                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(turn_buf + r * 64 + ((q ^ (r >> 1 & 3)) << 4)) : "memory");
+                                if (m0 + (int)quad * 32 + r < p.d_in && col < cols) *reinterpret_cast<uint4 *>(out + (long long)r * p.d_out + col) = v;
+                            }
+                            __syncwarp();
+                        }
                     }
                 }
                 tmem_wait_store();
@@ -701,34 +719,39 @@ __global__ void __launch_bounds__(512) grouped_sums_reduce_kernel(const int64_t 
     total[(long long)g * d_out + c] = acc;
 }
 
-// dW[g] = the sum of group g's records in the order of the chunks, times gamma, plus beta times the sums of dz's columns.
-// 4 outputs a thread, 8 shares of the records.
+// dW[g] = the sum of group g's records, times gamma, plus beta times the sums of dz's columns.  4 outputs a thread; SHARES warps share
+// the records of the same outputs where there are too few outputs to fill the device (the order is fixed either way).
+template <int SHARES>
 __global__ void __launch_bounds__(256) grouped_weight_reduce_kernel(const int64_t *__restrict__ offsets, long long n, int d_in, int d_out, int chunk_rows,
                                                                     const float *__restrict__ part, const float *__restrict__ total,
                                                                     const float *__restrict__ gamma, const float *__restrict__ beta, float *__restrict__ dw) {
     after_predecessor();
+    constexpr int kAcross = 256 / SHARES;
     const int g = blockIdx.y;
     const Records r = group_records(offsets, g, n, chunk_rows);
-    __shared__ float4 red[8][32];
-    const int lane = threadIdx.x & 31, share = threadIdx.x >> 5;
-    const long long size = (long long)d_in * d_out, x = (blockIdx.x * 32ll + lane) * 4;
+    __shared__ float4 red[SHARES][kAcross];
+    const int lane = threadIdx.x % kAcross, share = threadIdx.x / kAcross;
+    const long long size = (long long)d_in * d_out, x = (blockIdx.x * (long long)kAcross + lane) * 4;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (x < size) {
         const float *at = part + r.from * size + x;
-#pragma unroll 4
-        for (int s = share; s < r.count; s += 8) {
+#pragma unroll 8
+        for (int s = share; s < r.count; s += SHARES) {
             const float4 v = *reinterpret_cast<const float4 *>(at + s * size);
             acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
         }
     }
-    red[share][lane] = acc;
-    __syncthreads();
-    if (share != 0 || x >= size) return;
+    if constexpr (SHARES > 1) {
+        red[share][lane] = acc;
+        __syncthreads();
+        if (share != 0) return;
 #pragma unroll
-    for (int k = 1; k < 8; ++k) {
-        const float4 v = red[k][lane];
-        acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
+        for (int k = 1; k < SHARES; ++k) {
+            const float4 v = red[k][lane];
+            acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
+        }
     }
+    if (x >= size) return;
     const int row = (int)(x / d_out), c = (int)(x - (long long)row * d_out);
     if (gamma) {
         const float k = __ldg(gamma + row);
@@ -817,7 +840,7 @@ struct WeightPlan {
     int cols, m_tiles, n_tiles, chunks, chunk_rows, stages, step, h_panels;
     size_t smem, part_bytes, sum_bytes, total_bytes;   // the scratch: records, their column sums, the groups' column sums
 };
-static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out) {
+static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out, bool ckpt) {
     WeightPlan w;
     w.n_tiles = (d_out + 255) / 256;
     w.cols = round_up_int((d_out + w.n_tiles - 1) / w.n_tiles, 64);
@@ -825,18 +848,17 @@ static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out) {
     w.m_tiles = (d_in + 127) / 128;
     const int tiles = w.m_tiles * w.n_tiles;
     long long chunks = kSms / tiles;
-    if (chunks > n / 256) chunks = n / 256;   // rows below which a chunk is not worth its record
+    if (chunks > (n + kStep - 1) / kStep) chunks = (n + kStep - 1) / kStep;   // short chunks cost a record each, but small calls wait for steps: 2,000 rows, 256 x 256, chunks of 64, 128, 256 rows and more 29, 35, 42 us
     if (chunks < 1) chunks = 1;
     long long rows = (n + chunks - 1) / chunks;
     rows = (rows + kStep - 1) / kStep * kStep;
     w.chunk_rows = (int)rows;
     w.chunks = (int)((n + rows - 1) / rows);
-    // rows of one panel of h: twice as many a stage, so that a step is worth its waits, where three stages of that fit
-    // (2 million rows, 64 x 64, from a checkpoint: @@)
-    const size_t fixed = sizeof(WeightShared) + 1024;
-    const bool narrow = d_in <= 64 && w.cols <= 192;
-    w.h_panels = narrow ? 1 : 2;
-    w.step = narrow ? kStepMost : kStep;
+    // Twice as many rows a stage, so that a step is worth its waits, where three stages of that fit (2 million rows, 64 x 64: 99 -> 85 us,
+    // from a checkpoint 144 -> 86).  The makers' shares of a stage are 64 rows of two panels of h or 128 of one.
+    const size_t fixed = sizeof(WeightShared) + 1024 + kAdders * kTurnBuf;
+    w.h_panels = d_in <= 64 && w.cols <= 192 ? 1 : 2;
+    w.step = w.h_panels == 1 || (!ckpt && w.cols <= 128) ? kStepMost : kStep;
     const size_t stage = (size_t)(w.h_panels + w.cols / 64) * w.step * 128;
     w.stages = (int)((kSharedMost - fixed) / stage);
     w.stages = w.stages > kStagesMax ? kStagesMax : w.stages;
@@ -850,7 +872,7 @@ static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out) {
 static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, const int64_t *offsets, const void *h, const int8_t *codes,
                                  const uint8_t *scales, const float *gamma, const float *beta, const void *dz, float *dw, int32_t *flag,
                                  void *workspace, size_t workspace_bytes, cudaStream_t st) {
-    const WeightPlan w = weight_plan(n, groups, d_in, d_out);
+    const WeightPlan w = weight_plan(n, groups, d_in, d_out, !h);
     if (!workspace || !sar_aligned(workspace, 16) || workspace_bytes < w.part_bytes + w.sum_bytes + w.total_bytes) return SAR_ERR_WORKSPACE;
     WeightArgs p{};
     p.offsets = offsets;
@@ -894,8 +916,11 @@ static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_
         SAR_TRY(sar_after_launch());
     }
     const long long quads = (long long)d_in * d_out / 4;
+    const bool many = quads * groups >= 32 * 1024;
+    auto reduce = many ? grouped_weight_reduce_kernel<1> : grouped_weight_reduce_kernel<8>;
+    const int across = many ? 256 : 32;
     SAR_LAUNCH("linear_grouped_bwd_weight_reduce", st,
-               launch(grouped_weight_reduce_kernel, dim3((unsigned)((quads + 31) / 32), (unsigned)groups), 256, 0, st, offsets, (long long)n, (int)d_in, (int)d_out,
+               launch(reduce, dim3((unsigned)((quads + across - 1) / across), (unsigned)groups), 256, 0, st, offsets, (long long)n, (int)d_in, (int)d_out,
                       w.chunk_rows, p.part, total, gamma, beta, dw));
     return sar_after_launch();
 }
@@ -924,7 +949,7 @@ sar_status sar_linear_grouped_bwd_input(int64_t n, int32_t groups, int32_t d_in,
 
 size_t sar_linear_grouped_workspace_bytes(int64_t n, int32_t groups, int32_t d_in, int32_t d_out) {
     if (n < 1 || n > INT32_MAX || groups < 1 || d_in < 1 || d_out < 1) return 0;
-    const WeightPlan w = weight_plan(n, groups, d_in, d_out);
+    const WeightPlan w = weight_plan(n, groups, d_in, d_out, false);   // the scratch is the same either way
     return w.part_bytes + w.sum_bytes + w.total_bytes + 256;
 }
 

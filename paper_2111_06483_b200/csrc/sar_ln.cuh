@@ -346,14 +346,18 @@ struct LnShiftedRow {
     }
 };
 
-// Blocks that an SM is to hold at least, which bounds the registers, for N columns a lane.  A million rows of 256 columns, us:
-// bf16 forward 106 registers 190, 80 (three blocks) 171; backward 138 344, 128 (two) 252, from the checkpoint 140 429, 128 245;
-// float32 forward with the checkpoint 84 472, 78 (three) 397; backward from it 102 483, 80 (three) 392.
+// Blocks that an SM is to hold at least, which bounds the registers, for N columns a lane.  64 million values in rows of 256, us, as the
+// compiler likes and so: bf16 forward 106 registers 48, 80 (three blocks) 43; backward 138 86, 128 (two) 63, from the checkpoint 140
+// 107, 128 61; float32 forward with the checkpoint 84 118, 78 (three) 99.  Wider rows: two where the pass carries no sums (1,024
+// bf16 with the checkpoint 100, two blocks 79), one where it does (backward 87, two blocks 172: the sums leave the registers).
 template <typename Row>
 constexpr int ln_blocks(bool bwd, bool ck) {
-    constexpr int N = Row::E * Row::V;
-    if (Row::kShifted) return N > 16 ? 1 : 2;
-    return N > 16 ? 1 : Row::E == 8 ? (bwd || ck ? 2 : 3) : Row::E == 4 ? (N > 8 ? 1 : bwd && !ck ? 2 : 3) : N > 8 ? 1 : bwd && N > 4 ? 2 : 3;
+    constexpr int N = Row::E * Row::V, E = Row::E;
+    if (E == 1) return N > 8 ? 1 : bwd && N > 4 ? 2 : 3;
+    if (bwd) return N <= 8 && ck && E == 4 && !Row::kShifted ? 3 : N <= (Row::kShifted && E == 4 ? 12 : 16) ? 2 : 1;
+    if (Row::kShifted) return N <= 24 ? 2 : 1;
+    if (E == 8) return N <= 16 && !ck ? 3 : 2;
+    return N <= 8 ? 3 : N >= 32 && !ck ? 1 : 2;
 }
 
 // Rows are walked one ahead: a group asks for its next row before it works on the one it has (two sets of registers in turn),
