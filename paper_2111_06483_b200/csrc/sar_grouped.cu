@@ -42,7 +42,7 @@ sar_status tc_tensor_map(CUtensorMap *map, const void *base, int rank, const uin
     return r == CUDA_SUCCESS ? SAR_OK : SAR_ERR_CUDA;
 }
 
-// First row of every group, and what precedes each group in tiles, by the block's first warp.  Offsets that lead backwards or out
+// First row of every group, and what precedes each group in tiles, by the block's first warp (the others see it after a barrier).  Offsets that lead backwards or out
 // of the array are brought to the last one seen and to the array's ends: whatever they hold, every access stays in bounds.
 struct GroupTable {
     int first[kGroupsMax + 1];   // first[g] .. first[g + 1]: g's rows
@@ -79,7 +79,6 @@ __device__ __forceinline__ void group_table(GroupTable &t, const int64_t *__rest
             tiles = __shfl_sync(0xffffffffu, k, 31);
         }
     }
-    __syncthreads();
 }
 
 // ---- rows: z = h W[g], dh = dz W[g]^T ----------------------------------------------------------------------------------------
@@ -126,15 +125,18 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *failed = &sh.failed;
 
+    // the table, tensor memory, the barriers and the maps, each by a warp of its own
     group_table(sh.table, p.offsets, p.G, p.n);
-    if (threadIdx.x == 0) {
+    if (warp == 1) tmem_alloc(smem_addr(&sh.tmem));
+    if (threadIdx.x == 64) {
         for (int i = 0; i < p.stages; ++i) bar_init(smem_addr(&sh.full[i]), 1), bar_init(smem_addr(&sh.empty[i]), 1);
         for (int i = 0; i < kSlotsMax; ++i) bar_init(smem_addr(&sh.w_full[i]), 1), bar_init(smem_addr(&sh.w_empty[i]), 1);
         for (int i = 0; i < 2; ++i) bar_init(smem_addr(&sh.acc_full[i]), 1), bar_init(smem_addr(&sh.acc_empty[i]), 4);
         sh.failed = 0;
         bar_init_fence();
     }
-    if (warp == 1) tmem_alloc(smem_addr(&sh.tmem));
+    if (threadIdx.x == 96) map_prefetch(&p.a), map_prefetch(&p.w), map_prefetch(&p.d);
+    __syncwarp();
     tc_before_sync();
     __syncthreads();
     tc_after_sync();
@@ -369,14 +371,19 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     volatile int *failed = &sh.failed;
 
     group_table(sh.table, p.offsets, p.G, p.n);
-    if (threadIdx.x == 0) {
+    if (warp == 1) tmem_alloc(smem_addr(&sh.tmem));
+    if (threadIdx.x == 64) {
         // a stage is free when its products are done, and the adders have taken their sums of it
         for (int i = 0; i < p.stages; ++i) bar_init(smem_addr(&sh.full[i]), 1), bar_init(smem_addr(&sh.empty[i]), p.sums ? 1 + kAdders : 1), bar_init(smem_addr(&sh.made[i]), kMakers);
         for (int i = 0; i < 2; ++i) bar_init(smem_addr(&sh.acc_full[i]), 1), bar_init(smem_addr(&sh.acc_empty[i]), kAdders);
         sh.failed = 0;
         bar_init_fence();
     }
-    if (warp == 1) tmem_alloc(smem_addr(&sh.tmem));
+    if (threadIdx.x == 96) {
+        if (!CK) map_prefetch(&p.h);
+        map_prefetch(&p.dz);
+    }
+    __syncwarp();
     tc_before_sync();
     __syncthreads();
     tc_after_sync();
@@ -697,8 +704,8 @@ __device__ __forceinline__ Records group_records(const int64_t *__restrict__ off
     return {first + g, hi > lo ? (int)((hi - 1) / chunk_rows - first) + 1 : 0};
 }
 
-// The column sums of a group's dz: its records' shares in order.  One launch ahead of the next kernel, which needs a sum in every
-// row of dW: added up there they are read d_in times.
+// The column sums of a group's dz: its records' shares in order.  One launch ahead of the next kernel where that has many outputs: it
+// needs the sums in every row of dW, and added up there they would be read d_in times.
 __global__ void __launch_bounds__(512) grouped_sums_reduce_kernel(const int64_t *__restrict__ offsets, long long n, int d_out, int chunk_rows, int shares,
                                                                   const float *__restrict__ sums, float *__restrict__ total) {
     after_predecessor();
@@ -722,45 +729,48 @@ __global__ void __launch_bounds__(512) grouped_sums_reduce_kernel(const int64_t 
 // dW[g] = the sum of group g's records, times gamma, plus beta times the sums of dz's columns.  4 outputs a thread; SHARES warps share
 // the records of the same outputs where there are too few outputs to fill the device (the order is fixed either way).
 template <int SHARES>
-__global__ void __launch_bounds__(256) grouped_weight_reduce_kernel(const int64_t *__restrict__ offsets, long long n, int d_in, int d_out, int chunk_rows,
-                                                                    const float *__restrict__ part, const float *__restrict__ total,
+__global__ void __launch_bounds__(SHARES == 32 ? 1024 : 256) grouped_weight_reduce_kernel(const int64_t *__restrict__ offsets, long long n, int d_in, int d_out, int chunk_rows,
+                                                                    const float *__restrict__ part, const float *__restrict__ sums, int sum_shares,
                                                                     const float *__restrict__ gamma, const float *__restrict__ beta, float *__restrict__ dw) {
     after_predecessor();
-    constexpr int kAcross = 256 / SHARES;
+    constexpr int kAcross = SHARES == 1 ? 256 : 32;
     const int g = blockIdx.y;
     const Records r = group_records(offsets, g, n, chunk_rows);
-    __shared__ float4 red[SHARES][kAcross];
+    __shared__ float4 red[SHARES][kAcross], red_col[SHARES][kAcross];
     const int lane = threadIdx.x % kAcross, share = threadIdx.x / kAcross;
     const long long size = (long long)d_in * d_out, x = (blockIdx.x * (long long)kAcross + lane) * 4;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int row = (int)(x / d_out), c = (int)(x - (long long)row * d_out);
+    const auto add = [](float4 &a, const float4 &b) { a.x += b.x, a.y += b.y, a.z += b.z, a.w += b.w; };
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f), col = acc;
     if (x < size) {
         const float *at = part + r.from * size + x;
 #pragma unroll 8
-        for (int s = share; s < r.count; s += SHARES) {
-            const float4 v = *reinterpret_cast<const float4 *>(at + s * size);
-            acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
+        for (int s = share; s < r.count; s += SHARES) add(acc, *reinterpret_cast<const float4 *>(at + s * size));
+        if (sums) {
+            if constexpr (SHARES > 1) {   // few outputs: the records' column sums are added up here as well
+#pragma unroll 4
+                for (int s = share; s < r.count * sum_shares; s += SHARES) add(col, *reinterpret_cast<const float4 *>(sums + (r.from * sum_shares + s) * d_out + c));
+            } else {
+                col = *reinterpret_cast<const float4 *>(sums + (long long)g * d_out + c);   // of grouped_sums_reduce_kernel
+            }
         }
     }
     if constexpr (SHARES > 1) {
         red[share][lane] = acc;
+        red_col[share][lane] = col;
         __syncthreads();
         if (share != 0) return;
 #pragma unroll
-        for (int k = 1; k < SHARES; ++k) {
-            const float4 v = red[k][lane];
-            acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
-        }
+        for (int k = 1; k < SHARES; ++k) add(acc, red[k][lane]), add(col, red_col[k][lane]);
     }
     if (x >= size) return;
-    const int row = (int)(x / d_out), c = (int)(x - (long long)row * d_out);
     if (gamma) {
         const float k = __ldg(gamma + row);
         acc.x *= k, acc.y *= k, acc.z *= k, acc.w *= k;
     }
-    if (total) {
+    if (sums) {
         const float k = __ldg(beta + row);
-        const float4 v = *reinterpret_cast<const float4 *>(total + (long long)g * d_out + c);
-        acc.x = fmaf(k, v.x, acc.x), acc.y = fmaf(k, v.y, acc.y), acc.z = fmaf(k, v.z, acc.z), acc.w = fmaf(k, v.w, acc.w);
+        acc.x = fmaf(k, col.x, acc.x), acc.y = fmaf(k, col.y, acc.y), acc.z = fmaf(k, col.z, acc.z), acc.w = fmaf(k, col.w, acc.w);
     }
     *reinterpret_cast<float4 *>(dw + g * size + x) = acc;
 }
@@ -907,21 +917,23 @@ static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_
         SAR_LAUNCH("linear_grouped_bwd_weight_ckpt8", st, launch_if(overlap, grouped_weight_kernel<true>, blocks, kWeightThreads8, w.smem, st, p));
     }
     SAR_TRY(sar_after_launch());
-    float *total = nullptr;
-    if (beta) {
-        total = reinterpret_cast<float *>(static_cast<char *>(workspace) + w.part_bytes + w.sum_bytes);
+    const long long quads = (long long)d_in * d_out / 4;
+    const bool many = quads * groups >= 32 * 1024;   // outputs enough to fill the device with a thread for four
+    const float *sums = p.sums;
+    if (sums && many) {
+        float *total = reinterpret_cast<float *>(static_cast<char *>(workspace) + w.part_bytes + w.sum_bytes);
         SAR_LAUNCH("linear_grouped_sums_reduce", st,
                    launch(grouped_sums_reduce_kernel, dim3((unsigned)((d_out + 31) / 32), (unsigned)groups), 512, 0, st, offsets, (long long)n, (int)d_out, w.chunk_rows,
-                          2 * w.m_tiles, p.sums, total));
+                          2 * w.m_tiles, sums, total));
         SAR_TRY(sar_after_launch());
+        sums = total;
     }
-    const long long quads = (long long)d_in * d_out / 4;
-    const bool many = quads * groups >= 32 * 1024;
-    auto reduce = many ? grouped_weight_reduce_kernel<1> : grouped_weight_reduce_kernel<8>;
+    const bool few = quads * groups < 4 * 1024;
+    auto reduce = many ? grouped_weight_reduce_kernel<1> : few ? grouped_weight_reduce_kernel<32> : grouped_weight_reduce_kernel<8>;
     const int across = many ? 256 : 32;
     SAR_LAUNCH("linear_grouped_bwd_weight_reduce", st,
-               launch(reduce, dim3((unsigned)((quads + across - 1) / across), (unsigned)groups), 256, 0, st, offsets, (long long)n, (int)d_in, (int)d_out,
-                      w.chunk_rows, p.part, total, gamma, beta, dw));
+               launch(reduce, dim3((unsigned)((quads + across - 1) / across), (unsigned)groups), few ? 1024 : 256, 0, st, offsets, (long long)n, (int)d_in, (int)d_out,
+                      w.chunk_rows, p.part, sums, 2 * w.m_tiles, gamma, beta, dw));
     return sar_after_launch();
 }
 

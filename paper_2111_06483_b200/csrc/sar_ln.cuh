@@ -10,9 +10,13 @@ namespace sar {
 
 constexpr int kSms = 148;
 constexpr int kLnBlocks = kSms * 8;   // largest grid (grids depend on the sizes alone: a fixed summation order)
-// the sums of a block's weight gradients in shared memory: a copy for each warp where that is at most kLnSmem
+// the sums of a block's weight gradients in shared memory: as many copies as fit, a copy for each warp at most
 constexpr size_t kLnSmem = 32 * 1024;
-__host__ __device__ constexpr int ln_copies(int C) { return (size_t)kWarpsPerBlock * 2 * C * 4 <= kLnSmem ? kWarpsPerBlock : 1; }
+__host__ __device__ constexpr int ln_copies(int C) {
+    int k = kWarpsPerBlock;
+    while (k > 1 && (size_t)k * 2 * C * 4 > kLnSmem) k /= 2;
+    return k;
+}
 
 struct LnArgs {
     long long n;
@@ -510,9 +514,9 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_ker
             }
     }
     const int copies = ln_copies(a.C);
-    float *mine = smem + (copies > 1 ? id.warp * 2 * a.C : 0);
+    float *mine = smem + id.warp % copies * 2 * a.C;
     for (int w = 0; w < kWarpsPerBlock / copies; ++w) {
-        if (copies > 1 || id.warp == w) {
+        if (id.warp / copies == w) {
             for (int t = 0; t < (Row::kShifted ? 32 / G : 1); ++t) {
                 if (id.gid == t) {
                     const bool begin = w == 0 && t == 0;
@@ -843,7 +847,7 @@ static sar_status ln_backward_of(const LnShape &s, const LnArgs &a, unsigned *re
     return ln_dispatch<T, CK ? kLnBwd8 : kLnBwd>(s, [&](auto cfg) -> sar_status {
         using Row = typename decltype(cfg)::row;
         static const unsigned most = ln_resident(ln_bwd_kernel<Row, CK>, kLnSmem);
-        const unsigned want = blocks_for((a.n + 3) / 4, Row::G);   // a few rows per lane group before a block pays for its record
+        const unsigned want = blocks_for((a.n + 1) / 2, Row::G);   // two rows per lane group, which it asks for at once, before a block pays for its record
         *records = want < 1 ? 1 : want < most ? want : most;
         return ln_launch(name, ln_bwd_kernel<Row, CK>, want, most, a.partial ? (size_t)ln_copies(a.C) * 2 * a.C * 4 : 0, a, st);
     });
