@@ -597,8 +597,8 @@ SAR_API sar_status sar_bn_bwd_apply_act(int64_t n, int32_t C, sar_dtype t, const
  *                     anything infinite or NaN.  Every value comes back within 2^(s - 127), a 64th of top at most; the bytes
  *                     are the same on every path and device.
  *   sar_ckpt8_unpack  the values that the checkpoint stands for (exact in float32; in bf16 as well).
- * x and codes as they may be: rows whose columns are a multiple of 8 (or 4) with x aligned to 16 bytes and codes to 8 (or 4)
- * move several columns at a time.  n = 0 is allowed.  Errors: SAR_ERR_INVALID_ARG, SAR_ERR_UNSUPPORTED (C > 2^20),
+ * Arrays aligned to 16 bytes (codes to 8) move 16 bytes at a time whatever C; others work as well, column by column.
+ * n = 0 is allowed.  Errors: SAR_ERR_INVALID_ARG, SAR_ERR_UNSUPPORTED (C > 2^20),
  * SAR_ERR_ALIGNMENT (x not aligned to its type).
  * ------------------------------------------------------------------------------------------- */
 #define SAR_CKPT8_BLOCK 32
@@ -618,6 +618,8 @@ SAR_API sar_status sar_ckpt8_unpack(int64_t n, int32_t C, sar_dtype t, const int
  *   sar_ln_bwd_ckpt8   sar_ln_bwd with xhat = what the checkpoint stands for (gx may be gy).
  * Scratch of the backward calls where dgamma or dbeta is asked for: sar_ln_workspace_bytes(C).  Sums over the rows are formed in
  * a fixed order (no atomics), block partials are added in float64.  n = 0 is allowed (dgamma, dbeta are written as zeros).
+ * Arrays aligned to 16 bytes (codes to 8) move 16 bytes at a time whatever C; others work as well, column by column; rows of
+ * more than about 1,000 columns are read again for each of the row's sums.
  * Errors: SAR_ERR_INVALID_ARG (NULL arrays, eps < 0 or NaN), SAR_ERR_UNSUPPORTED (C > 2^20), SAR_ERR_ALIGNMENT (arrays not
  * aligned to their type), SAR_ERR_WORKSPACE.
  * ------------------------------------------------------------------------------------------- */
@@ -650,7 +652,7 @@ SAR_API sar_status sar_ln_bwd_ckpt8(int64_t n, int32_t C, sar_dtype t, const int
  * written as zeros with flags = SAR_GROUPED_ZERO_REST.  flag (DEVICE int, may be NULL) is set to 1 if a wait inside the kernel
  * ran out of its bound (seconds), which leaves results unwritten; the library's tests check that it stays 0.
  * Arrays are 16-byte aligned (codes 8), t must be SAR_BF16, d_in and d_out multiples of 8 up to 2^20, groups <= SAR_MAX_GROUPS,
- * n < 2^31 - 128 (SAR_ERR_UNSUPPORTED otherwise).  Scratch of the weight calls: sar_linear_grouped_workspace_bytes.  n = 0 is
+ * n < 2^31 - 2048 (SAR_ERR_UNSUPPORTED otherwise).  Scratch of the weight calls: sar_linear_grouped_workspace_bytes.  n = 0 is
  * allowed (dw is then written as zeros).
  * ------------------------------------------------------------------------------------------- */
 #define SAR_MAX_GROUPS 1024

@@ -345,7 +345,7 @@ struct WeightArgs {
     int chunk_rows;  // a multiple of 64
     int stages;
     int step;        // rows per stage: 64 or 128
-    int h_panels;    // of a stage: 2 with 64 rows, 1 with 128
+    int h_panels;    // of a stage: 2, or 1 where h has no more
 };
 constexpr int kAdders = 8, kMakers = 8;   // warps; the adders' work is laid out for 8
 constexpr int kWeightThreads = 64 + kAdders * 32, kWeightThreads8 = kWeightThreads + kMakers * 32;
@@ -782,7 +782,7 @@ constexpr size_t kSharedMost = 227 * 1024;
 static sar_status grouped_check(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, sar_dtype t, const int64_t *offsets, std::initializer_list<const void *> ps) {
     if (n < 0 || groups < 1 || d_in < 1 || d_out < 1 || (!offsets && groups > 1)) return SAR_ERR_INVALID_ARG;
     if (t != SAR_BF16) return t == SAR_F32 ? SAR_ERR_UNSUPPORTED : SAR_ERR_INVALID_ARG;
-    if (n > INT32_MAX - kTileRows || groups > kGroupsMax || d_in % 8 || d_out % 8 || d_in > (1 << 20) || d_out > (1 << 20)) return SAR_ERR_UNSUPPORTED;
+    if (n > INT32_MAX - 2048 || groups > kGroupsMax || d_in % 8 || d_out % 8 || d_in > (1 << 20) || d_out > (1 << 20)) return SAR_ERR_UNSUPPORTED;
     if (offsets && !sar_aligned(offsets, 8)) return SAR_ERR_ALIGNMENT;
     for (const void *p : ps)
         if (!p) return SAR_ERR_INVALID_ARG;

@@ -52,6 +52,26 @@ def test_pack_and_unpack(n, c, dt):
     check(x, p.codes, p.scales)
 
 
+@pytest.mark.parametrize("c", [2, 3, 5, 7, 9, 15, 17, 23, 36, 50, 57, 63, 95, 121, 122, 127, 166, 249, 250, 333, 505, 506, 761, 1017, 1018, 1021, 1022, 1023, 1025, 1030, 1036, 1100])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 2, 9, 5001])
+def test_rows_that_are_no_whole_vectors(n, c, dt):
+    """Every place within a vector that a row can start at, the last vectors of the array, and one column more or less than a kernel's
+    lanes cover; many rows a lane group.  The bytes behind the codes and the values stay as they were."""
+    from paper_2111_06483_b200 import binding as B
+    x = rows(min(n, 203), c, dt, 1000 * n + c).repeat(-(-n // 203), 1)[:n].contiguous().cuda()
+    codes = torch.full((n * c + 16,), 99, dtype=torch.int8, device="cuda")
+    scales = torch.full((n * ((c + 31) // 32) + 16,), 77, dtype=torch.uint8, device="cuda")
+    own, s = codes[:n * c].view(n, c), scales[:-16].view(n, -1)
+    B.sar_ckpt8_pack(x, own, s)
+    assert (codes[n * c:] == 99).all() and (scales[-16:] == 77).all()
+    want_codes, want_scales = oracle.ckpt8_pack(x.float().cpu().numpy())
+    assert np.array_equal(s.cpu().numpy(), want_scales) and np.array_equal(own.cpu().numpy(), want_codes)
+    back = torch.full((n * c + 16,), 7.0, dtype=DT[dt], device="cuda")
+    B.sar_ckpt8_unpack(own, s, back[:n * c].view(n, c))
+    assert (back[n * c:] == 7).all() and same(back[:n * c].view(n, c).double().cpu().numpy(), oracle.ckpt8_unpack(want_codes, want_scales))
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("skip_x,skip_codes", [(1, 0), (0, 1), (4, 4), (2, 0)])
 def test_addresses_that_are_not_aligned(dt, skip_x, skip_codes):

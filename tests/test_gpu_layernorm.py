@@ -167,6 +167,44 @@ def test_many_rows(c, dt):
         within(np64(dbeta), want[2], tol[2], "dbeta")
 
 
+@pytest.mark.parametrize("c", [127, 129, 166, 249, 250, 253, 254, 333, 505, 506, 761, 762, 1017, 1018, 1021, 1022, 1023])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 9, 4003])
+def test_rows_that_are_no_whole_vectors(n, c, dt):
+    """Rows that start anywhere within a vector, to one column more or less than a kernel's lanes cover, all four passes."""
+    test_forward(n, c, dt, 1.0)
+    test_forward_with_the_checkpoint_of_its_rows(n, c, dt, 1.0)
+    test_backward(n, c, dt, 1.0)
+    test_backward_from_the_checkpoint(n, c, dt)
+
+
+@pytest.mark.parametrize("c", [5, 47, 127, 333, 1021])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_what_lies_before_and_behind_stays(c, dt):
+    """y, gx, codes and scales are written to the last value and not a byte further, and infinities behind x and gy reach nothing."""
+    from paper_2111_06483_b200 import api, binding as B
+    n = 37
+    x, gy, gamma, beta = problem(n, c, dt, 1.0, c)
+    want_y, (ck, rstd) = api.ln_forward(x, 1e-5, gamma, beta, checkpoint=True)
+    want_gx, dgamma, dbeta = api.ln_backward(None, gy, (ck, rstd), gamma)
+
+    def room(like, fill):
+        t = torch.full((like.numel() + 32,), fill, dtype=like.dtype, device="cuda")
+        t[16:-16] = like.reshape(-1)
+        return t, t[16:-16].view(like.shape)
+
+    (_, xs), (_, gs) = room(x, float("inf")), room(gy, float("nan"))
+    (ry, y), (rc, codes), (rs, scales) = room(torch.zeros_like(x), 3.0), room(torch.zeros_like(ck.codes), 99), room(torch.zeros_like(ck.scales), 77)
+    B.sar_ln_fwd_ckpt8(xs, gamma, beta, 1e-5, y, rstd, codes, scales)
+    assert torch.equal(y, want_y) and torch.equal(codes, ck.codes) and torch.equal(scales, ck.scales)
+    (rg, gx), ws = room(torch.zeros_like(x), 3.0), torch.empty(B.sar_ln_workspace_bytes(c), dtype=torch.uint8, device="cuda")
+    dg, db = torch.empty_like(dgamma), torch.empty_like(dbeta)
+    B.sar_ln_bwd_ckpt8(codes, scales, rstd, gamma, gs, gx, dg, db, ws)
+    assert torch.equal(gx, want_gx) and torch.equal(dg, dgamma) and torch.equal(db, dbeta)
+    for r, v in ((ry, 3), (rg, 3), (rc, 99), (rs, 77)):
+        assert (r[:16] == v).all() and (r[-16:] == v).all()
+
+
 def test_gradient_against_differences():
     """The loss sum(y * gy) in float64 on the oracle's forward pass, moved along random directions: what the backward pass says
     of its slope.  A central difference of step 1e-4 on values of order 1 is off by 1e-8 and the float32 gradient by 1e-5."""
@@ -230,10 +268,11 @@ def test_rows_with_infinities_and_nan_spoil_no_other_row(c):
     assert torch.equal(gx[good], gx0[good]) and gx[~good].isnan().all()
 
 
+@pytest.mark.parametrize("c", [64, 300, 1000])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-def test_addresses_that_are_not_aligned(dt):
+def test_addresses_that_are_not_aligned(c, dt):
     from paper_2111_06483_b200 import api, binding as B
-    n, c = 65, 64
+    n = 65
     x, gy, gamma, beta = problem(n, c, dt, 1.0, 3)
     want, tol = forward_bounds(np64(x), np64(gamma), np64(beta), 1e-5)
     room = torch.full((n * c + 2,), 9.0, dtype=DT[dt], device="cuda")
@@ -242,11 +281,11 @@ def test_addresses_that_are_not_aligned(dt):
     B.sar_ln_fwd(x, gamma, beta, 1e-5, off, mean, rstd)
     within(np64(off), want[0], tol[0] + half(dt, np.abs(want[0]) + tol[0]), "y")
     codes = torch.zeros(n * c + 1, dtype=torch.int8, device="cuda")[1:].view(n, c)
-    scales = torch.empty(n, 2, dtype=torch.uint8, device="cuda")
+    scales = torch.empty(n, (c + 31) // 32, dtype=torch.uint8, device="cuda")
     B.sar_ln_fwd_ckpt8(x, gamma, beta, 1e-5, off, rstd, codes, scales)
     B.sar_ln_bwd_ckpt8(codes, scales, rstd, gamma, gy, off, None, None, None)
     gx = oracle.ln_backward(oracle.ckpt8_unpack(codes.cpu().numpy(), scales.cpu().numpy()), np64(rstd), np64(gy), np64(gamma))[0]
-    within(np64(off), gx, 64 * U * (np.abs(gx) + np64(rstd)[:, None] * 10) + half(dt, gx), "gx")
+    within(np64(off), gx, (links(c) + 48) * U * (np.abs(gx) + np64(rstd)[:, None] * 30) + half(dt, gx), "gx")   # |xhat| and |gy gamma| below 5 or so each
     assert room[0] == 9 and room[-1] == 9
 
 
