@@ -90,18 +90,17 @@ __global__ void __launch_bounds__(256, 4) ckpt8_pack_kernel(long long blocks, in
             }
 #pragma unroll
             for (int d = 1; d < LPB; d <<= 1) top = ckpt_top(top, __shfl_xor_sync(0xffffffffu, top, d), 0.f);
-            const unsigned s = ckpt_scale_byte(top);
-            const float inv = ckpt_inverse(s);
-            const bool cut = ckpt_cut(top, inv);
+            const float inv = ckpt_inverse(top);
+            const bool bad = ckpt_bad(top), cut = __any_sync(0xffffffffu, ckpt_cut(top, inv));
 #pragma unroll
             for (int i = 0; i < S; ++i) {
                 if (!p.ok(i)) continue;
                 int8_t *to = codes + p.slot(i);
-                if constexpr (E == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(ckpt_code4(v[i][0], v[i][1], inv, s, cut), ckpt_code4(v[i][2], v[i][3], inv, s, cut));
-                else if constexpr (E == 4) *reinterpret_cast<unsigned *>(to) = ckpt_code4(v[i][0], v[i][1], inv, s, cut);
-                else *to = ckpt_code1(v[i][0].x, inv, s, cut);
+                if constexpr (E == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(ckpt_code4(v[i][0], v[i][1], inv, bad, cut), ckpt_code4(v[i][2], v[i][3], inv, bad, cut));
+                else if constexpr (E == 4) *reinterpret_cast<unsigned *>(to) = ckpt_code4(v[i][0], v[i][1], inv, bad, cut);
+                else *to = ckpt_code1(v[i][0].x, inv, bad, cut);
             }
-            if (sub == 0 && b < blocks) scales[b] = (uint8_t)s;
+            if (sub == 0 && b < blocks) scales[b] = (uint8_t)ckpt_scale_byte(top);
         }
     }
 }

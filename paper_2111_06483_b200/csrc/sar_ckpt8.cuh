@@ -70,16 +70,17 @@ __device__ __forceinline__ unsigned ckpt_scale_byte(float top) {
     const unsigned e = __float_as_uint(top) >> 23;   // top has no sign
     return top == 0.f ? 0u : e == 255u ? 255u : e > 7u ? e - 6u : 1u;
 }
-// 2^(127 - s); 0 for the bytes 0 and 255, whose codes are 0
-__device__ __forceinline__ float ckpt_inverse(unsigned s) { return (s == 0u || s == 255u) ? 0.f : __uint_as_float((254u - s) << 23); }
+// 2^(127 - s) of the byte for `top`; some power of two where that is 0 (zeros have code 0 with any) or 255 (codes are masked)
+__device__ __forceinline__ float ckpt_inverse(float top) { return __uint_as_float((260u - max(__float_as_uint(top) >> 23, 7u)) << 23); }
+__device__ __forceinline__ bool ckpt_bad(float top) { return __float_as_uint(top) >= 0x7f800000u; }   // infinite or NaN: byte 255
 // 2^(s - 127): 0 for the byte 0, NaN for 255
 __device__ __forceinline__ float ckpt_scale(unsigned s) { return __uint_as_float(s == 255u ? 0x7fc00000u : s << 23); }
 
 // Codes in the low bytes of floats.  Added to 1.5 * 2^23 the quotient x / scale, which is exact, is rounded to the nearest whole number,
 // ties to even, and its two's complement is the sum's low byte.  Only a block whose largest quotient reaches 127.5 can round to
-// 128: one in 200, so a warp looks for that once (`cut`) and clamps there.
+// 128: one in 200, so a warp votes on that (`cut`) and clamps there.
 constexpr float kCkptMagic = 12582912.f;
-__device__ __forceinline__ bool ckpt_cut(float top, float inverse) { return __any_sync(0xffffffffu, top * inverse >= 127.5f); }
+__device__ __forceinline__ bool ckpt_cut(float top, float inverse) { return !(top * inverse < 127.5f); }   // for a warp's vote
 __device__ __forceinline__ float ckpt_code(float x, float inverse, bool cut) {
     const float v = fmaf(x, inverse, kCkptMagic);
     return cut ? fminf(fmaxf(v, kCkptMagic - 127.f), kCkptMagic + 127.f) : v;
@@ -96,12 +97,13 @@ __device__ __forceinline__ unsigned ckpt_codes4(float2 a, float2 b, float2 inv_a
     return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
 }
 // four codes of one block
-__device__ __forceinline__ unsigned ckpt_code4(float2 a, float2 b, float inverse, unsigned s, bool cut) {
+__device__ __forceinline__ unsigned ckpt_code4(float2 a, float2 b, float inverse, bool bad, bool cut) {
     const float2 i = make_float2(inverse, inverse);
-    return s == 255u ? 0u : ckpt_codes4(a, b, i, i, cut);
+    const unsigned w = ckpt_codes4(a, b, i, i, cut);
+    return bad ? 0u : w;
 }
-__device__ __forceinline__ int8_t ckpt_code1(float x, float inverse, unsigned s, bool cut) {
-    return (int8_t)(s == 255u ? 0u : __float_as_uint(ckpt_code(x, inverse, cut)));
+__device__ __forceinline__ int8_t ckpt_code1(float x, float inverse, bool bad, bool cut) {
+    return (int8_t)(bad ? 0u : __float_as_uint(ckpt_code(x, inverse, cut)));
 }
 // code i of a word of four as a float: 2^23 + 128 + code is put together from its bytes, and the subtraction is exact
 __device__ __forceinline__ float ckpt_decode(unsigned flipped /* the word ^ 0x80808080 */, int i) {

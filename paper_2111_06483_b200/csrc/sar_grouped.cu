@@ -815,7 +815,7 @@ static sar_status grouped_rows(int64_t n, int32_t groups, int K, int N, const in
     p.cols = round_up_int((N + p.slices - 1) / p.slices, 64);
     p.slices = (N + p.cols - 1) / p.cols;
     const size_t w_step = (size_t)(p.cols / 64) * kPanel, w_set = p.steps * w_step, row_stage = kTileRows * 128;
-    p.store_bufs = stay ? 2 : 1;
+    p.store_bufs = stay && p.steps * p.cols < 4 * 256 ? 2 : 1;   // where the weights take 128 KB a second buffer costs a stage of four
     const size_t fixed = sizeof(RowsShared) + 1024 + 4 * p.store_bufs * kStoreBuf;
     size_t smem;
     if (stay) {

@@ -104,28 +104,34 @@ struct LnRow {
     // The checkpoint: 32 columns are the slots of LPB consecutive lanes, SPB slots each (the whole group where it is narrower).
     static constexpr int SPB = G * E >= 32 ? 1 : 32 / (G * E), LPB = 32 / E < G ? 32 / E : G;
     __device__ __forceinline__ void put_codes(const LnArgs &a, long long row, bool live, const float2 (&x)[V][P]) const {
+        constexpr int B = (V + SPB - 1) / SPB;   // blocks that the lane has a part of
+        float top[B];
+        bool cut = false;
 #pragma unroll
-        for (int v0 = 0; v0 < V; v0 += SPB) {
-            float top = 0.f;
+        for (int b = 0; b < B; ++b) {
+            top[b] = 0.f;
 #pragma unroll
-            for (int v = v0; v < v0 + SPB && v < V; ++v)
+            for (int v = b * SPB; v < (b + 1) * SPB && v < V; ++v)
 #pragma unroll
-                for (int q = 0; q < P; ++q)
-                    if (ok[v]) top = ckpt_top(top, x[v][q].x, E == 1 ? 0.f : x[v][q].y);
+                for (int q = 0; q < P; ++q) top[b] = ckpt_top(top[b], x[v][q].x, x[v][q].y);   // what is no column is zero
 #pragma unroll
-            for (int d = 1; d < LPB; d <<= 1) top = ckpt_top(top, __shfl_xor_sync(0xffffffffu, top, d, G), 0.f);
-            const unsigned s = ckpt_scale_byte(top);
-            const float inv = ckpt_inverse(s);
-            const bool cut = ckpt_cut(top, inv);
-            if (!live) continue;
+            for (int d = 1; d < LPB; d <<= 1) top[b] = ckpt_top(top[b], __shfl_xor_sync(0xffffffffu, top[b], d, G), 0.f);
+            cut = cut || ckpt_cut(top[b], ckpt_inverse(top[b]));
+        }
+        cut = __any_sync(0xffffffffu, cut);
+        if (!live) return;
 #pragma unroll
-            for (int v = v0; v < v0 + SPB && v < V; ++v) {
+        for (int b = 0; b < B; ++b) {
+            const float inv = ckpt_inverse(top[b]);
+            const bool bad = ckpt_bad(top[b]);
+#pragma unroll
+            for (int v = b * SPB; v < (b + 1) * SPB && v < V; ++v) {
                 if (!ok[v]) continue;
                 int8_t *p = a.codes + at(row, v);
-                if constexpr (E == 8) *reinterpret_cast<uint2 *>(p) = make_uint2(ckpt_code4(x[v][0], x[v][1], inv, s, cut), ckpt_code4(x[v][2], x[v][3], inv, s, cut));
-                else if constexpr (E == 4) *reinterpret_cast<unsigned *>(p) = ckpt_code4(x[v][0], x[v][1], inv, s, cut);
-                else *p = ckpt_code1(x[v][0].x, inv, s, cut);
-                if (v == v0 && col(v) % kCkptBlock == 0) a.scales[row * a.nb + col(v) / kCkptBlock] = (uint8_t)s;
+                if constexpr (E == 8) *reinterpret_cast<uint2 *>(p) = make_uint2(ckpt_code4(x[v][0], x[v][1], inv, bad, cut), ckpt_code4(x[v][2], x[v][3], inv, bad, cut));
+                else if constexpr (E == 4) *reinterpret_cast<unsigned *>(p) = ckpt_code4(x[v][0], x[v][1], inv, bad, cut);
+                else *p = ckpt_code1(x[v][0].x, inv, bad, cut);
+                if (v == b * SPB && col(v) % kCkptBlock == 0) a.scales[row * a.nb + col(v) / kCkptBlock] = (uint8_t)ckpt_scale_byte(top[b]);
             }
         }
     }
@@ -254,7 +260,6 @@ struct LnShiftedRow {
     }
     __device__ __forceinline__ void put_codes(const LnArgs &a, long long row, bool live, const float2 (&x)[V][P]) const {
         float top[V], front[V], inv[V];   // front: of the m columns that belong to the block before
-        unsigned s[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             top[v] = front[v] = 0.f;
@@ -278,17 +283,16 @@ struct LnShiftedRow {
             const int first = gl & ~(L - 1);
             const float next = __shfl_sync(0xffffffffu, front[v], (first + L) & (G - 1), G), after = __shfl_sync(0xffffffffu, front[v + 1 < V ? v + 1 : v], 0, G);
             top[v] = ckpt_top(top[v], first + L < G ? next : v + 1 < V ? after : 0.f, 0.f);
-            s[v] = ckpt_scale_byte(top[v]);
-            inv[v] = ckpt_inverse(s[v]);
-            cut = cut || top[v] * inv[v] >= 127.5f;
-            bad = bad || s[v] == 255u;
+            inv[v] = ckpt_inverse(top[v]);
+            cut = cut || ckpt_cut(top[v], inv[v]);
+            bad = bad || ckpt_bad(top[v]);
         }
         cut = __any_sync(0xffffffffu, cut);
         bad = __any_sync(0xffffffffu, bad);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float inv_before = before(inv, v);
-            const unsigned s_before = before(s, v);
+            const float top_before = before(top, v);
             if (!live || mask[v] == 0u) continue;
             unsigned w[E / 4];
 #pragma unroll
@@ -298,7 +302,7 @@ struct LnShiftedRow {
                 for (int h = 0; h < 2; ++h) {
                     const bool fx = head && 2 * (q + h) < m, fy = head && 2 * (q + h) + 1 < m;
                     i[h] = make_float2(fx ? inv_before : inv[v], fy ? inv_before : inv[v]);
-                    if (bad) y[h] = make_float2((fx ? s_before : s[v]) == 255u ? 0.f : y[h].x, (fy ? s_before : s[v]) == 255u ? 0.f : y[h].y);
+                    if (bad) y[h] = make_float2(ckpt_bad(fx ? top_before : top[v]) ? 0.f : y[h].x, ckpt_bad(fy ? top_before : top[v]) ? 0.f : y[h].y);
                 }
                 w[q / 2] = ckpt_codes4(y[0], y[1], i[0], i[1], cut);
             }
@@ -312,7 +316,7 @@ struct LnShiftedRow {
                     if (has(v, e)) p[e] = (int8_t)(w[e / 4] >> (e % 4 * 8));
             }
             const int block = (v * G + gl) / L;
-            if (gl % L == 0 && block < a.nb) a.scales[row * a.nb + block] = (uint8_t)s[v];
+            if (gl % L == 0 && block < a.nb) a.scales[row * a.nb + block] = (uint8_t)ckpt_scale_byte(top[v]);
         }
     }
     __device__ __forceinline__ void ask(const LnArgs &a, long long row, bool live, Packed (&r)[V]) const {
@@ -634,11 +638,10 @@ __global__ void __launch_bounds__(kThreads) ln_fwd_long_kernel(const LnArgs a) {
                 float top = ckpt_top(xh, 0.f, 0.f);
 #pragma unroll
                 for (int d = 16; d > 0; d >>= 1) top = ckpt_top(top, __shfl_xor_sync(0xffffffffu, top, d), 0.f);
-                const unsigned s = ckpt_scale_byte(top);
-                const float inv = ckpt_inverse(s);
-                const bool cut = ckpt_cut(top, inv);
-                if (c < a.C) a.codes[o + c] = ckpt_code1(xh, inv, s, cut);
-                if (lane == 0) a.scales[row * a.nb + b] = (uint8_t)s;
+                const float inv = ckpt_inverse(top);
+                const bool cut = __any_sync(0xffffffffu, ckpt_cut(top, inv));
+                if (c < a.C) a.codes[o + c] = ckpt_code1(xh, inv, ckpt_bad(top), cut);
+                if (lane == 0) a.scales[row * a.nb + b] = (uint8_t)ckpt_scale_byte(top);
             }
             if (c < a.C) Elem<T>::store1(static_cast<T *>(a.y) + o + c, fmaf(xh, a.gamma ? __ldg(a.gamma + c) : 1.f, a.beta ? __ldg(a.beta + c) : 0.f));
         }
@@ -706,8 +709,6 @@ struct LnShape {
 #define SAR_LN_8N(X) X(8, 4, 1) X(8, 4, 2) X(8, 8, 2)
 #define SAR_LN_4N(X) X(4, 8, 1) X(4, 8, 2) X(4, 16, 2)
 #define SAR_LN_1(X) X(1, 4, 1) X(1, 4, 4) X(1, 4, 8) X(1, 8, 6) X(1, 8, 8) X(1, 16, 6) X(1, 16, 8) X(1, 32, 8) X(1, 32, 32)
-// ... and of single columns in the backward pass, which carries two sums for each of them
-#define SAR_LN_1B(X) X(1, 4, 1) X(1, 4, 4) X(1, 8, 4) X(1, 16, 3) X(1, 16, 4) X(1, 32, 3) X(1, 32, 4) X(1, 32, 8) X(1, 32, 32)
 // Columns from which rows that are no whole vectors are taken shifted.  64 million values, us, one column a lane and slot against
 // shifted: 95 bf16 forward 93 / 96, with checkpoint 187 / 205, backward 157 / 162; 191 bf16 111 / 97, 265 / 203, 191 / 159; 191
 // float32 123 / 113, 289 / 275, 169 / 156.  Checkpoints: 47 bf16 packed 173 / 141, unpacked 117 / 99, backward from
@@ -742,11 +743,7 @@ static inline sar_status ln_dispatch(const LnShape &s, Fn &&f) {
         SAR_LN_8(SAR_LN_CASE)
     }
     SAR_LN_4(SAR_LN_CASE)
-    if constexpr (PASS == kLnBwd || PASS == kLnBwd8) {
-        SAR_LN_1B(SAR_LN_CASE)
-    } else {
-        SAR_LN_1(SAR_LN_CASE)
-    }
+    SAR_LN_1(SAR_LN_CASE)
 #undef SAR_LN_CASE
 #undef SAR_LN_SHIFTED
     return SAR_ERR_UNSUPPORTED;
@@ -780,8 +777,6 @@ static inline LnShape ln_shape(int32_t C, sar_dtype t, LnPass pass, size_t array
             }
             SAR_LN_4S(SAR_LN_FIT)
         }
-    } else if (pass == kLnBwd || pass == kLnBwd8) {
-        SAR_LN_1B(SAR_LN_FIT)
     } else {
         SAR_LN_1(SAR_LN_FIT)
     }
