@@ -517,10 +517,14 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_ker
                 }
             }
     }
-    const int copies = ln_copies(a.C);
-    float *mine = smem + id.warp % copies * 2 * a.C;
-    for (int w = 0; w < kWarpsPerBlock / copies; ++w) {
-        if (id.warp / copies == w) {
+    // The warp's number once more, from a source the compiler does not see through: kept from the start it pushes a value that the
+    // rows need out of the registers (250,000 rows of 1,024 float32 from the checkpoint 625 us, so 492; 552 and 500 without one).
+    unsigned warp;
+    asm volatile("shr.u32 %0, %1, 5;" : "=r"(warp) : "r"(threadIdx.x));
+    const unsigned copies = ln_copies(a.C), turns = kWarpsPerBlock / copies;
+    float *mine = smem + warp / turns * 2 * a.C;
+    for (unsigned w = 0; w < turns; ++w) {
+        if (warp % turns == w) {
             for (int t = 0; t < (Row::kShifted ? 32 / G : 1); ++t) {
                 if (id.gid == t) {
                     const bool begin = w == 0 && t == 0;
@@ -541,7 +545,7 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_ker
     }
     for (int c = threadIdx.x; c < 2 * a.C; c += kThreads) {
         float acc = smem[c];
-        for (int k = 1; k < copies; ++k) acc += smem[k * 2 * a.C + c];
+        for (unsigned k = 1; k < copies; ++k) acc += smem[k * 2 * a.C + c];
         a.partial[(size_t)blockIdx.x * 2 * a.C + c] = acc;
     }
 }
