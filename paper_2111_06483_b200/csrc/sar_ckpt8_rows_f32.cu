@@ -6,10 +6,10 @@ sar_status ln_checkpoint_f32(const LnShape &s, const LnArgs &a, bool unpack, cud
         using Row = typename decltype(cfg)::row;
         if (unpack) {
             static const unsigned most = ln_resident(ln_unpack_kernel<Row>, 0);
-            return ln_launch("ckpt8_unpack", ln_unpack_kernel<Row>, blocks_for(a.n, Row::G), most, 0, a, st);
+            return ln_launch("ckpt8_unpack", ln_unpack_kernel<Row>, ln_grid<Row::G>(a.n), most, 0, a, st);
         }
         static const unsigned most = ln_resident(ln_pack_kernel<Row>, 0);
-        return ln_launch("ckpt8_pack", ln_pack_kernel<Row>, blocks_for(a.n, Row::G), most, 0, a, st);
+        return ln_launch("ckpt8_pack", ln_pack_kernel<Row>, ln_grid<Row::G>(a.n), most, 0, a, st);
     });
 }
 }  // namespace sar

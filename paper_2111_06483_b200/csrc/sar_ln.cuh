@@ -33,18 +33,62 @@ struct LnArgs {
     float *partial;               // [blocks][2][C] or null (no weight gradients asked for)
 };
 
+// Where a thread stands: lane gl of group gid of its warp, whose first row is the block's row `first`; a group is the whole block
+// where G is 256.
 template <int G>
-__device__ __forceinline__ float ln_sum(float x) {
+struct LnLane {
+    static constexpr int kRows = kThreads / G;   // rows that a block has in hand
+    static constexpr bool kBlock = G > 32;
+    static_assert(!kBlock || G == kThreads, "a group is lanes of a warp or the block");
+    int gl, gid, first;
+    __device__ __forceinline__ LnLane() {
+        gl = threadIdx.x & (G - 1);
+        gid = kBlock ? 0 : (threadIdx.x & 31) / G;
+        first = kBlock ? 0 : (threadIdx.x >> 5) * (32 / G);
+    }
+};
+template <int G>
+static inline unsigned ln_grid(long long rows) { return (unsigned)((rows + LnLane<G>::kRows - 1) / LnLane<G>::kRows); }
+
+// Sums over a group's lanes.  A block's go by way of red[which]: two of them in turn, so that a sum costs one barrier.
+struct LnRed {
+    float2 red[2][kWarpsPerBlock];
+};
+template <int G>
+__device__ __forceinline__ float2 ln_sum2(float2 x, LnRed &r, int which) {
+    constexpr int W = G < 32 ? G : 32;
 #pragma unroll
-    for (int d = G / 2; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d, G);
+    for (int d = W / 2; d > 0; d >>= 1) x.x += __shfl_xor_sync(0xffffffffu, x.x, d, W);
+#pragma unroll
+    for (int d = W / 2; d > 0; d >>= 1) x.y += __shfl_xor_sync(0xffffffffu, x.y, d, W);
+    if constexpr (G > 32) {
+        if ((threadIdx.x & 31) == 0) r.red[which][threadIdx.x >> 5] = x;
+        __syncthreads();
+        x = r.red[which][0];
+#pragma unroll
+        for (int w = 1; w < kWarpsPerBlock; ++w) x = __fadd2_rn(x, r.red[which][w]);
+    }
     return x;
+}
+template <int G>
+__device__ __forceinline__ float ln_sum(float x, LnRed &r, int which) {
+    constexpr int W = G < 32 ? G : 32;
+    if constexpr (G > 32) {
+        return ln_sum2<G>(make_float2(x, 0.f), r, which).x;
+    } else {
+#pragma unroll
+        for (int d = W / 2; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d, W);
+        return x;
+    }
 }
 __device__ __forceinline__ float2 ln_splat(float x) { return make_float2(x, x); }
 
 // A row across the G lanes of a group, each with V slots of E columns: 16 bytes (8 bf16, 4 float32), or one column where the
 // arrays are not aligned to that.  Few lanes with many columns each, 16 of bf16 and 8 of float32 where that covers the row,
 // rather than many lanes with few: a warp then has up to 8 rows in hand and joins their sums in 2 to 4 steps instead of 5
-// (a million rows of 256 bf16, forward: 32 lanes of 8 columns 208 us, 16 of 16 171).
+// (a million rows of 256 bf16, forward: 32 lanes of 8 columns 208 us, 16 of 16 171).  Above 1,024 columns the group is the block:
+// a row still stays in registers and is read once (120,000 rows of 2,048 bf16, us, a block that reads its row again for every
+// pass against this: forward 564 / 210, with the checkpoint 1091 / 260, backward 945 / 274, from the checkpoint 1261 / 273).
 //
 // LnRow: E divides C (or is 1).  Slot v of lane gl holds the columns from (v G + gl) E on, all or none of them.
 template <typename T_, int E_, int G_, int V_>
@@ -115,7 +159,7 @@ struct LnRow {
 #pragma unroll
                 for (int q = 0; q < P; ++q) top[b] = ckpt_top(top[b], x[v][q].x, x[v][q].y);   // what is no column is zero
 #pragma unroll
-            for (int d = 1; d < LPB; d <<= 1) top[b] = ckpt_top(top[b], __shfl_xor_sync(0xffffffffu, top[b], d, G), 0.f);
+            for (int d = 1; d < LPB; d <<= 1) top[b] = ckpt_top(top[b], __shfl_xor_sync(0xffffffffu, top[b], d, G < 32 ? G : 32), 0.f);
             cut = cut || ckpt_cut(top[b], ckpt_inverse(top[b]));
         }
         cut = __any_sync(0xffffffffu, cut);
@@ -358,10 +402,14 @@ struct LnShiftedRow {
 // compiler likes and so: bf16 forward 106 registers 48, 80 (three blocks) 43; backward 138 86, 128 (two) 63, from the checkpoint 140
 // 107, 128 61; float32 forward with the checkpoint 84 118, 78 (three) 99.  Wider rows: two where the pass carries no sums (1,024
 // bf16 with the checkpoint 100, two blocks 79), one where it does (backward 87, two blocks 172: the sums leave the registers).
+// Rows of a block wait at a barrier for every sum, so other blocks have to fill in: 120,000 rows of 2,048 bf16 backward two blocks
+// 354, three 274, from the checkpoint 446, 315, four 273; 60,000 of 4,096 forward two 207, three 176, four 185, backward one 408,
+// two 255, three 442.
 template <typename Row>
 constexpr int ln_blocks(bool bwd, bool ck) {
     constexpr int N = Row::E * Row::V, E = Row::E;
-    if (E == 1) return N > 8 ? 1 : bwd && N > 4 ? 2 : 3;
+    if (Row::G > 32) return bwd ? (N <= 4 ? (E == 1 ? 3 : 4) : N <= 8 ? (E == 8 ? 4 : E == 4 ? 3 : 2) : N <= 16 ? 2 : 1) : N <= 8 ? 4 : N <= 16 && E != 4 ? 3 : 2;
+    if (E == 1) return bwd && N > 4 ? 2 : 3;
     if (bwd) return N <= 8 && ck && E == 4 && !Row::kShifted ? 3 : N <= (Row::kShifted && E == 4 ? 12 : 16) ? 2 : 1;
     if (Row::kShifted) return N <= 24 ? 2 : 1;
     if (E == 8) return N <= 16 && !ck ? 3 : 2;
@@ -374,9 +422,10 @@ template <typename Row, bool CK>
 __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(false, CK)) ln_fwd_kernel(const LnArgs a) {
     after_predecessor();
     constexpr int G = Row::G, V = Row::V, P = Row::P;
-    const LaneId<G> id;
-    const long long stride = (long long)gridDim.x * kWarpsPerBlock * (32 / G);
-    long long base = ((long long)blockIdx.x * kWarpsPerBlock + id.warp) * (32 / G);   // the warp's first row: the shuffles need all its lanes
+    __shared__ LnRed red;
+    const LnLane<G> id;
+    const long long stride = (long long)gridDim.x * id.kRows;
+    long long base = (long long)blockIdx.x * id.kRows + id.first;   // the warp's first row: the shuffles need all its lanes
     const Row r(a, id.gl, base + id.gid);
     float2 ga[V][P], be[V][P];
     r.cols(a.gamma, 1.f, ga);
@@ -391,7 +440,7 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(false, CK)) ln_fwd_ke
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int q = 0; q < P; ++q) sum = __fadd2_rn(sum, x[v][q]);   // what is no column is zero
-        const float mean = ln_sum<G>(sum.x + sum.y) * a.inv_c;
+        const float mean = ln_sum<G>(sum.x + sum.y, red, 0) * a.inv_c;
         float2 dev = make_float2(0.f, 0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -401,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(false, CK)) ln_fwd_ke
 #pragma unroll
             for (int q = 0; q < P; ++q) dev = __ffma2_rn(x[v][q], x[v][q], dev);
         }
-        const float rstd = __frsqrt_rn(fmaf(ln_sum<G>(dev.x + dev.y), a.inv_c, a.eps));
+        const float rstd = __frsqrt_rn(fmaf(ln_sum<G>(dev.x + dev.y, red, 1), a.inv_c, a.eps));
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -434,9 +483,10 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_ker
     after_predecessor();
     constexpr int G = Row::G, V = Row::V, P = Row::P;
     extern __shared__ float smem[];   // [copies][2][C]
-    const LaneId<G> id;
-    const long long stride = (long long)gridDim.x * kWarpsPerBlock * (32 / G);
-    long long base = ((long long)blockIdx.x * kWarpsPerBlock + id.warp) * (32 / G);
+    __shared__ LnRed red;
+    const LnLane<G> id;
+    const long long stride = (long long)gridDim.x * id.kRows;
+    long long base = (long long)blockIdx.x * id.kRows + id.first;
     const Row r(a, id.gl, base + id.gid);
     float2 ga[V][P], s0[V][P], s1[V][P];
     r.cols(a.gamma, 1.f, ga);
@@ -458,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_ker
         q.mu = !CK && live ? __ldg(a.mean_in + row) : 0.f;
         q.rs = live ? __ldg(a.rstd_in + row) : 0.f;
     };
-    const auto work = [&](long long base, const Asked &in) {
+    const auto work = [&](long long base, const Asked &in, int which) {
         const long long row = base + id.gid;
         float2 x[V][P], g[V][P], along2 = make_float2(0.f, 0.f), level2 = along2;
         const float2 rs = ln_splat(in.rs);
@@ -481,8 +531,8 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_ker
                 along2 = __ffma2_rn(g[v][q], x[v][q], along2);
             }
         }
-        const float level = ln_sum<G>(level2.x + level2.y) * a.inv_c;
-        const float along = ln_sum<G>(along2.x + along2.y) * a.inv_c;
+        const float2 both = ln_sum2<G>(make_float2(level2.x + level2.y, along2.x + along2.y), red, which);
+        const float level = both.x * a.inv_c, along = both.y * a.inv_c;
         if (row >= a.n) return;
         const float2 minus_along = ln_splat(-along), minus_level = ln_splat(-level);
 #pragma unroll
@@ -495,12 +545,24 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_ker
     if (base < a.n) ask(base, one);
     for (; base < a.n; base += 2 * stride) {
         ask(base + stride, two);
-        work(base, one);
+        work(base, one, 0);
         if (base + stride >= a.n) break;
         ask(base + 2 * stride, one);
-        work(base + stride, two);
+        work(base + stride, two, 1);
     }
     if (!a.partial) return;
+    if constexpr (id.kBlock) {   // a column is one thread's
+        float *const p = a.partial + (size_t)blockIdx.x * 2 * a.C;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int e = 0; e < Row::E; ++e)
+                if (r.has(v, e)) {
+                    p[r.col(v) + e] = e & 1 ? s1[v][e / 2].y : s1[v][e / 2].x;
+                    p[a.C + r.col(v) + e] = e & 1 ? s0[v][e / 2].y : s0[v][e / 2].x;
+                }
+        return;
+    }
     // The groups of a warp, then the warps, which have a copy each where they fit (one after the other otherwise).  Rows that start at
     // different places of a vector have different columns in a lane: their groups add to shared memory in turn.
     if constexpr (!Row::kShifted) {
@@ -555,9 +617,9 @@ template <typename Row>
 __global__ void __launch_bounds__(kThreads, 2) ln_pack_kernel(const LnArgs a) {
     after_predecessor();
     constexpr int G = Row::G, V = Row::V, P = Row::P;
-    const LaneId<G> id;
-    const long long stride = (long long)gridDim.x * kWarpsPerBlock * (32 / G);
-    long long base = ((long long)blockIdx.x * kWarpsPerBlock + id.warp) * (32 / G);
+    const LnLane<G> id;
+    const long long stride = (long long)gridDim.x * id.kRows;
+    long long base = (long long)blockIdx.x * id.kRows + id.first;
     const Row r(a, id.gl, base + id.gid);
     const auto ask = [&](long long base, typename Row::raw_t(&raw)[V]) { r.ask(a.x, base + id.gid, base + id.gid < a.n, raw); };
     const auto work = [&](long long base, const typename Row::raw_t(&raw)[V]) {
@@ -580,9 +642,9 @@ template <typename Row>
 __global__ void __launch_bounds__(kThreads, 2) ln_unpack_kernel(const LnArgs a) {
     after_predecessor();
     constexpr int G = Row::G, V = Row::V, P = Row::P;
-    const LaneId<G> id;
-    const long long stride = (long long)gridDim.x * kWarpsPerBlock * (32 / G);
-    long long row = ((long long)blockIdx.x * kWarpsPerBlock + id.warp) * (32 / G) + id.gid;
+    const LnLane<G> id;
+    const long long stride = (long long)gridDim.x * id.kRows;
+    long long row = (long long)blockIdx.x * id.kRows + id.first + id.gid;
     const Row r(a, id.gl, row);
     const auto work = [&](long long row, const typename Row::Packed(&raw)[V]) {
         float2 x[V][P];
@@ -600,12 +662,13 @@ __global__ void __launch_bounds__(kThreads, 2) ln_unpack_kernel(const LnArgs a) 
     }
 }
 
-// ---- rows longer than the registers of a warp: a block takes a row and reads it again for every pass (from L1 or L2) ----------
+// ---- rows longer than the registers of a block: it takes a row and reads it again for every pass (from L1 or L2) ----------
 template <typename T>
 __device__ __forceinline__ float ln_load(const void *base, long long at) { return (float)static_cast<const T *>(base)[at]; }
 
 __device__ __forceinline__ float ln_block_sum(float x, float *red) {   // red: kWarpsPerBlock floats; the same order in every block
-    x = ln_sum<32>(x);
+    #pragma unroll
+    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
     __syncthreads();
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
     __syncthreads();
@@ -698,21 +761,24 @@ __global__ void __launch_bounds__(kThreads) ln_long_sums_kernel(const LnArgs a, 
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------
-// How rows of C columns are spread over lanes: E columns a slot, V slots in G lanes, shifted or not; E = 0: longer than a warp's
+// How rows of C columns are spread over lanes: E columns a slot, V slots in G lanes, shifted or not; E = 0: longer than a block's
 // registers.
 struct LnShape {
     int E, G, V;
     bool shifted;
 };
 // Every (E, G, V) of a kind of row in ascending E G V: the first that covers the row is taken.
-#define SAR_LN_8(X) X(8, 4, 1) X(8, 4, 2) X(8, 4, 3) X(8, 8, 2) X(8, 8, 3) X(8, 16, 2) X(8, 16, 3) X(8, 32, 2) X(8, 32, 3) X(8, 32, 4)
-#define SAR_LN_4(X) X(4, 4, 1) X(4, 4, 2) X(4, 8, 2) X(4, 8, 3) X(4, 16, 2) X(4, 16, 3) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6) X(4, 32, 8)
+#define SAR_LN_8(X) X(8, 4, 1) X(8, 4, 2) X(8, 4, 3) X(8, 8, 2) X(8, 8, 3) X(8, 16, 2) X(8, 16, 3) X(8, 32, 2) X(8, 32, 3) X(8, 32, 4) X(8, 256, 1) X(8, 256, 2) X(8, 256, 4)
+#define SAR_LN_4(X) X(4, 4, 1) X(4, 4, 2) X(4, 8, 2) X(4, 8, 3) X(4, 16, 2) X(4, 16, 3) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6) X(4, 32, 8) X(4, 256, 2) X(4, 256, 4) X(4, 256, 8)
+// ... float32 in the backward pass, which carries two sums for each column: 1,024 columns in a block, 250,000 rows 484 us, in a warp
+// 522, from the checkpoint 430 and 493 (forward 407 and 326)
+#define SAR_LN_4B(X) X(4, 4, 1) X(4, 4, 2) X(4, 8, 2) X(4, 8, 3) X(4, 16, 2) X(4, 16, 3) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6) X(4, 256, 1) X(4, 256, 2) X(4, 256, 4) X(4, 256, 8)
 #define SAR_LN_8S(X) X(8, 16, 2) X(8, 32, 2) X(8, 32, 3) X(8, 32, 4)
 #define SAR_LN_4S(X) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6) X(4, 32, 8)
 // ... and narrow shifted rows, for what reads checkpoints or only packs
 #define SAR_LN_8N(X) X(8, 4, 1) X(8, 4, 2) X(8, 8, 2)
 #define SAR_LN_4N(X) X(4, 8, 1) X(4, 8, 2) X(4, 16, 2)
-#define SAR_LN_1(X) X(1, 4, 1) X(1, 4, 4) X(1, 4, 8) X(1, 8, 6) X(1, 8, 8) X(1, 16, 6) X(1, 16, 8) X(1, 32, 8) X(1, 32, 32)
+#define SAR_LN_1(X) X(1, 4, 1) X(1, 4, 4) X(1, 4, 8) X(1, 8, 6) X(1, 8, 8) X(1, 16, 6) X(1, 16, 8) X(1, 32, 8) X(1, 256, 4) X(1, 256, 8)
 // Columns from which rows that are no whole vectors are taken shifted.  64 million values, us, one column a lane and slot against
 // shifted: 95 bf16 forward 93 / 96, with checkpoint 187 / 205, backward 157 / 162; 191 bf16 111 / 97, 265 / 203, 191 / 159; 191
 // float32 123 / 113, 289 / 275, 169 / 156.  Checkpoints: 47 bf16 packed 173 / 141, unpacked 117 / 99, backward from
@@ -746,7 +812,11 @@ static inline sar_status ln_dispatch(const LnShape &s, Fn &&f) {
     if constexpr (sizeof(T) == 2) {
         SAR_LN_8(SAR_LN_CASE)
     }
-    SAR_LN_4(SAR_LN_CASE)
+    if constexpr (sizeof(T) == 4 && (PASS == kLnBwd || PASS == kLnBwd8)) {
+        SAR_LN_4B(SAR_LN_CASE)
+    } else {
+        SAR_LN_4(SAR_LN_CASE)
+    }
     SAR_LN_1(SAR_LN_CASE)
 #undef SAR_LN_CASE
 #undef SAR_LN_SHIFTED
@@ -766,7 +836,11 @@ static inline LnShape ln_shape(int32_t C, sar_dtype t, LnPass pass, size_t array
     if (E == 8 && may(8)) {
         SAR_LN_8(SAR_LN_FIT)
     } else if (may(4)) {
-        SAR_LN_4(SAR_LN_FIT)
+        if (E == 4 && (pass == kLnBwd || pass == kLnBwd8)) {
+            SAR_LN_4B(SAR_LN_FIT)
+        } else {
+            SAR_LN_4(SAR_LN_FIT)
+        }
     } else if (C >= (from_ckpt ? kCkptShiftedFrom : kLnShiftedFrom) && arrays >= 16 && codes >= (size_t)E) {
         s.shifted = true;
         need = C + E - 1;   // wherever in a vector the row starts
@@ -781,7 +855,10 @@ static inline LnShape ln_shape(int32_t C, sar_dtype t, LnPass pass, size_t array
             }
             SAR_LN_4S(SAR_LN_FIT)
         }
-    } else {
+    }
+    if (s.E == 0) {
+        s.shifted = false;
+        need = C;
         SAR_LN_1(SAR_LN_FIT)
     }
 #undef SAR_LN_FIT
@@ -825,7 +902,7 @@ static sar_status ln_forward_of(const LnShape &s, const LnArgs &a, cudaStream_t 
     return ln_dispatch<T, kLnFwd>(s, [&](auto cfg) -> sar_status {
         using Row = typename decltype(cfg)::row;
         static const unsigned most = ln_resident(ln_fwd_kernel<Row, CK>, 0);
-        return ln_launch(name, ln_fwd_kernel<Row, CK>, blocks_for(a.n, Row::G), most, 0, a, st);
+        return ln_launch(name, ln_fwd_kernel<Row, CK>, ln_grid<Row::G>(a.n), most, 0, a, st);
     });
 }
 
@@ -845,10 +922,10 @@ static sar_status ln_backward_of(const LnShape &s, const LnArgs &a, unsigned *re
     }
     return ln_dispatch<T, CK ? kLnBwd8 : kLnBwd>(s, [&](auto cfg) -> sar_status {
         using Row = typename decltype(cfg)::row;
-        static const unsigned most = ln_resident(ln_bwd_kernel<Row, CK>, kLnSmem);
-        const unsigned want = blocks_for((a.n + 1) / 2, Row::G);   // two rows per lane group, which it asks for at once, before a block pays for its record
+        static const unsigned most = ln_resident(ln_bwd_kernel<Row, CK>, Row::G > 32 ? 0 : kLnSmem);
+        const unsigned want = ln_grid<Row::G>((a.n + 1) / 2);   // two rows per lane group, which it asks for at once, before a block pays for its record
         *records = want < 1 ? 1 : want < most ? want : most;
-        return ln_launch(name, ln_bwd_kernel<Row, CK>, want, most, a.partial ? (size_t)ln_copies(a.C) * 2 * a.C * 4 : 0, a, st);
+        return ln_launch(name, ln_bwd_kernel<Row, CK>, want, most, Row::G <= 32 && a.partial ? (size_t)ln_copies(a.C) * 2 * a.C * 4 : 0, a, st);
     });
 }
 

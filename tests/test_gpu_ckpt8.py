@@ -72,6 +72,13 @@ def test_rows_that_are_no_whole_vectors(n, c, dt):
     assert (back[n * c:] == 7).all() and same(back[:n * c].view(n, c).double().cpu().numpy(), oracle.ckpt8_unpack(want_codes, want_scales))
 
 
+@pytest.mark.parametrize("c", [1027, 1028, 1500, 2044, 2047, 2049, 2052, 4100, 8188, 8196])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 2, 1203])
+def test_rows_that_a_block_shares(n, c, dt):
+    test_pack_and_unpack(n, c, dt)
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("skip_x,skip_codes", [(1, 0), (0, 1), (4, 4), (2, 0)])
 def test_addresses_that_are_not_aligned(dt, skip_x, skip_codes):

@@ -178,6 +178,31 @@ def test_rows_that_are_no_whole_vectors(n, c, dt):
     test_backward_from_the_checkpoint(n, c, dt)
 
 
+@pytest.mark.parametrize("c", [772, 1020, 1027, 1028, 1032, 1536, 2044, 2047, 2049, 2052, 4096, 4100, 8188, 8192, 8196])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 78, 1501])
+def test_rows_that_a_block_shares(n, c, dt):
+    """Rows of more columns than a warp holds, to the most that a block does and one vector more, all four passes."""
+    test_forward(n, c, dt, 1.0)
+    test_forward_with_the_checkpoint_of_its_rows(n, c, dt, 1.0)
+    test_backward(n, c, dt, 1.0)
+    test_backward_from_the_checkpoint(n, c, dt)
+
+
+@pytest.mark.parametrize("c", [1021, 2000, 2047, 4100, 8192])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_wide_rows_in_place(c, dt):
+    """The result over x or over gy, as for other rows; without weight gradients the same gx."""
+    from paper_2111_06483_b200 import api, binding as B
+    test_in_place(c, dt)
+    x, gy, gamma, beta = problem(700, c, dt, 1.0, c)
+    _, saved = api.ln_forward(x, 1e-5, gamma, beta)
+    gx, _, _ = api.ln_backward(x, gy, saved, gamma)
+    alone = torch.empty_like(gx)
+    B.sar_ln_bwd(x, *saved, gamma, gy, alone, None, None, None)
+    assert torch.equal(alone, gx)
+
+
 @pytest.mark.parametrize("c", [5, 47, 127, 333, 1021])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_what_lies_before_and_behind_stays(c, dt):
