@@ -9,6 +9,8 @@
 #include "sar_dispatch.cuh"
 #include "sar_tc.cuh"
 
+#include <utility>
+
 namespace sar {
 
 constexpr int kTileRows = 128;      // rows of a product's tile: all lanes of tensor memory
@@ -727,11 +729,12 @@ __global__ void __launch_bounds__(512) grouped_sums_reduce_kernel(const int64_t 
 }
 
 // dW[g] = the sum of group g's records, times gamma, plus beta times the sums of dz's columns.  4 outputs a thread; SHARES warps share
-// the records of the same outputs where there are too few outputs to fill the device (the order is fixed either way).
+// the records of the same outputs where there are too few outputs to fill the device (the order is fixed either way).  turned: the
+// records are dW's transpose, [d_in][d_out] here with the names swapped.
 template <int SHARES>
 __global__ void __launch_bounds__(SHARES == 32 ? 1024 : 256) grouped_weight_reduce_kernel(const int64_t *__restrict__ offsets, long long n, int d_in, int d_out, int chunk_rows,
                                                                     const float *__restrict__ part, const float *__restrict__ sums, int sum_shares,
-                                                                    const float *__restrict__ gamma, const float *__restrict__ beta, float *__restrict__ dw) {
+                                                                    const float *__restrict__ gamma, const float *__restrict__ beta, bool turned, float *__restrict__ dw) {
     after_predecessor();
     constexpr int kAcross = SHARES == 1 ? 256 : 32;
     const int g = blockIdx.y;
@@ -772,7 +775,12 @@ __global__ void __launch_bounds__(SHARES == 32 ? 1024 : 256) grouped_weight_redu
         const float k = __ldg(beta + row);
         acc.x = fmaf(k, col.x, acc.x), acc.y = fmaf(k, col.y, acc.y), acc.z = fmaf(k, col.z, acc.z), acc.w = fmaf(k, col.w, acc.w);
     }
-    *reinterpret_cast<float4 *>(dw + g * size + x) = acc;
+    if (turned) {
+        float *to = dw + g * size + (long long)c * d_in + row;
+        to[0] = acc.x, to[d_in] = acc.y, to[2ll * d_in] = acc.z, to[3ll * d_in] = acc.w;
+    } else {
+        *reinterpret_cast<float4 *>(dw + g * size + x) = acc;
+    }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
@@ -879,9 +887,21 @@ static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out, bool c
     return w;
 }
 
+// A tile is twice as wide as it is high, so dW^T = dz^T h can take fewer of them, and rows are read once a tile and chunk.  That pays
+// where no rows are whole lines of 128 bytes: a panel's row is then two requests to L2, which is what bounds such widths (300,000
+// rows, us, as they lie and turned: 136 x 72 50 / 39, 264 x 40 62 / 57, 456 x 72 90 / 78, 200 x 120 52 / 58; but 256 x 64 42 / 48,
+// 256 x 72 47 / 51).  Rows of a checkpoint are always the first operand, which the makers write.
+static bool weight_turned(int64_t n, int groups, int d_in, int d_out) {
+    if (d_in % 64 == 0 || d_out % 64 == 0) return false;
+    const WeightPlan a = weight_plan(n, groups, d_in, d_out, false), b = weight_plan(n, groups, d_out, d_in, false);
+    return b.m_tiles * b.n_tiles < a.m_tiles * a.n_tiles;
+}
+
 static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, const int64_t *offsets, const void *h, const int8_t *codes,
                                  const uint8_t *scales, const float *gamma, const float *beta, const void *dz, float *dw, int32_t *flag,
                                  void *workspace, size_t workspace_bytes, cudaStream_t st) {
+    const bool turned = h && weight_turned(n, groups, d_in, d_out);
+    if (turned) std::swap(d_in, d_out), std::swap(h, dz);
     const WeightPlan w = weight_plan(n, groups, d_in, d_out, !h);
     if (!workspace || !sar_aligned(workspace, 16) || workspace_bytes < w.part_bytes + w.sum_bytes + w.total_bytes) return SAR_ERR_WORKSPACE;
     WeightArgs p{};
@@ -933,7 +953,7 @@ static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_
     const int across = many ? 256 : 32;
     SAR_LAUNCH("linear_grouped_bwd_weight_reduce", st,
                launch(reduce, dim3((unsigned)((quads + across - 1) / across), (unsigned)groups), few ? 1024 : 256, 0, st, offsets, (long long)n, (int)d_in, (int)d_out,
-                      w.chunk_rows, p.part, sums, 2 * w.m_tiles, gamma, beta, dw));
+                      w.chunk_rows, p.part, sums, 2 * w.m_tiles, gamma, beta, turned, dw));
     return sar_after_launch();
 }
 
@@ -961,8 +981,10 @@ sar_status sar_linear_grouped_bwd_input(int64_t n, int32_t groups, int32_t d_in,
 
 size_t sar_linear_grouped_workspace_bytes(int64_t n, int32_t groups, int32_t d_in, int32_t d_out) {
     if (n < 1 || n > INT32_MAX || groups < 1 || d_in < 1 || d_out < 1) return 0;
-    const WeightPlan w = weight_plan(n, groups, d_in, d_out, false);   // the scratch is the same either way
-    return w.part_bytes + w.sum_bytes + w.total_bytes + 256;
+    size_t most = 0;   // of rows and of a checkpoint, as they lie and turned
+    for (const WeightPlan &w : {weight_plan(n, groups, d_in, d_out, true), weight_plan(n, groups, d_out, d_in, false)})
+        most = w.part_bytes + w.sum_bytes + w.total_bytes > most ? w.part_bytes + w.sum_bytes + w.total_bytes : most;
+    return most + 256;
 }
 
 static sar_status grouped_zero(int32_t groups, int32_t d_in, int32_t d_out, float *dw, void *stream) {

@@ -97,6 +97,13 @@ def test_widths(d_in, d_out):
     check_all(*problem([200, 0, 1, 333], d_in, d_out))
 
 
+@pytest.mark.parametrize("d_in,d_out", [(136, 8), (264, 40), (456, 72), (520, 200), (1032, 120)])
+@pytest.mark.parametrize("sizes", [[5], [200, 0, 1, 333], [7, 900, 0, 65] * 16])
+def test_weight_gradients_taken_turned(sizes, d_in, d_out):
+    """Widths whose transposed gradient takes fewer tiles, with few outputs and with many, rows of no group around them."""
+    check_all(*problem(sizes, d_in, d_out, 3, 70))
+
+
 @pytest.mark.parametrize("sizes", [[0], [0, 0, 5], [128, 128], [127, 1, 129], [1] * 40, [3, 700, 0, 0, 65, 2000], [31, 33, 0] * 11])
 @pytest.mark.parametrize("before,behind", [(0, 0), (5, 0), (0, 9), (130, 200)])
 def test_groups_and_rows_of_no_group(sizes, before, behind):
