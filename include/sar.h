@@ -597,7 +597,8 @@ SAR_API sar_status sar_bn_bwd_apply_act(int64_t n, int32_t C, sar_dtype t, const
  *                     anything infinite or NaN.  Every value comes back within 2^(s - 127), a 64th of top at most; the bytes
  *                     are the same on every path and device.
  *   sar_ckpt8_unpack  the values that the checkpoint stands for (exact in float32; in bf16 as well).
- * Arrays aligned to 16 bytes (codes to 8) move 16 bytes at a time whatever C; others work as well, column by column.
+ * Arrays aligned to 16 bytes (codes to 8) move 16 bytes at a time whatever C from 16 to about 1,000, and beyond where C is a
+ * multiple of 32; others work as well, in fours or column by column.
  * n = 0 is allowed.  Errors: SAR_ERR_INVALID_ARG, SAR_ERR_UNSUPPORTED (C > 2^20),
  * SAR_ERR_ALIGNMENT (x not aligned to its type).
  * ------------------------------------------------------------------------------------------- */
@@ -618,8 +619,9 @@ SAR_API sar_status sar_ckpt8_unpack(int64_t n, int32_t C, sar_dtype t, const int
  *   sar_ln_bwd_ckpt8   sar_ln_bwd with xhat = what the checkpoint stands for (gx may be gy).
  * Scratch of the backward calls where dgamma or dbeta is asked for: sar_ln_workspace_bytes(C).  Sums over the rows are formed in
  * a fixed order (no atomics), block partials are added in float64.  n = 0 is allowed (dgamma, dbeta are written as zeros).
- * Arrays aligned to 16 bytes (codes to 8) move 16 bytes at a time whatever C; others work as well, column by column; rows of
- * more than about 1,000 columns are read again for each of the row's sums.
+ * Arrays aligned to 16 bytes (codes to 8) move 16 bytes at a time where C is a multiple of 8 (bf16) or 4, and whatever C from 128
+ * to about 1,000; others work as well, column by column.  Rows are read once up to 8,192 columns (2,048 column by column) and again
+ * for each of the row's sums beyond.
  * Errors: SAR_ERR_INVALID_ARG (NULL arrays, eps < 0 or NaN), SAR_ERR_UNSUPPORTED (C > 2^20), SAR_ERR_ALIGNMENT (arrays not
  * aligned to their type), SAR_ERR_WORKSPACE.
  * ------------------------------------------------------------------------------------------- */
@@ -639,8 +641,8 @@ SAR_API sar_status sar_ln_bwd_ckpt8(int64_t n, int32_t C, sar_dtype t, const int
  * The projection of nodes of several types, one weight matrix for each (Appendix A's W_r with the relation's rows lying
  * together): rows offsets[g] .. offsets[g+1] of the node arrays belong to group g.  offsets: DEVICE, int64 [groups + 1],
  * ascending, within 0 .. n; the sizes are read on the device alone, groups may be empty and of any length, and the calls can be
- * captured once and replayed with other offsets; NULL with groups = 1 means all rows.  (Offsets that descend or leave the array are read as the largest one before
- * them and as the array's ends.)  Weights [groups, d_in, d_out].
+ * captured once and replayed with other offsets; NULL with groups = 1 means all rows.  (Offsets that descend or leave the array
+ * are read as the largest one before them and as the array's ends.)  Weights [groups, d_in, d_out].
  *   sar_linear_grouped             z[i] = h[i] W[g]                (bf16 out)
  *   sar_linear_grouped_bwd_input   dh[i] = dz[i] W[g]^T            (bf16 out)
  *   sar_linear_grouped_bwd_weight  dw[g] = sum over g's rows of h[i]^T dz[i]   (float32 out; zeros for an empty group; sums in
@@ -649,7 +651,7 @@ SAR_API sar_status sar_ln_bwd_ckpt8(int64_t n, int32_t C, sar_dtype t, const int
  *   sar_linear_grouped_bwd_weight_ckpt8  the same with h = gamma * v + beta, v what the checkpoint (codes, scales) stands for;
  *                                  gamma, beta [d_in] float32 may be NULL (1 / 0): the weight gradient behind sar_ln_fwd_ckpt8.
  * Rows of no group (before offsets[0], from offsets[groups] on) take part in nothing; z and dh are left there as they were, or
- * written as zeros with flags = SAR_GROUPED_ZERO_REST.  flag (DEVICE int, may be NULL) is set to 1 if a wait inside the kernel
+ * written as zeros with flags = SAR_GROUPED_ZERO_REST.  Neither may overlap the rows or the weights (SAR_ERR_INVALID_ARG).  flag (DEVICE int, may be NULL) is set to 1 if a wait inside the kernel
  * ran out of its bound (seconds), which leaves results unwritten; the library's tests check that it stays 0.
  * Arrays are 16-byte aligned (codes 8), t must be SAR_BF16, d_in and d_out multiples of 8 up to 2^20, groups <= SAR_MAX_GROUPS,
  * n < 2^31 - 2048 (SAR_ERR_UNSUPPORTED otherwise).  Scratch of the weight calls: sar_linear_grouped_workspace_bytes.  n = 0 is

@@ -798,6 +798,15 @@ static sar_status grouped_check(int64_t n, int32_t groups, int32_t d_in, int32_t
     return SAR_OK;
 }
 
+static bool overlap(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes) {
+    const char *x = static_cast<const char *>(a), *y = static_cast<const char *>(b);
+    return x < y + b_bytes && y < x + a_bytes;
+}
+// a result over the rows or the weights: other blocks may still have to read them
+static sar_status grouped_apart(int64_t n, int64_t groups, int64_t d_in, int64_t d_out, const void *rows, int64_t d_rows, const void *w, const void *out, int64_t d_result) {
+    return overlap(out, n * d_result * 2, rows, n * d_rows * 2) || overlap(out, n * d_result * 2, w, groups * d_in * d_out * 2) ? SAR_ERR_INVALID_ARG : SAR_OK;
+}
+
 static int round_up_int(int x, int a) { return (x + a - 1) / a * a; }
 
 // out [n, N] = rows [n, K] times W[g] (WT: its transpose)
@@ -927,14 +936,14 @@ static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_
     const uint64_t h_dims[2] = {(uint64_t)d_in, (uint64_t)n}, z_dims[2] = {(uint64_t)d_out, (uint64_t)n};
     if (h) SAR_TRY(tc_tensor_map(&p.h, h, 2, h_dims, box));
     SAR_TRY(tc_tensor_map(&p.dz, dz, 2, z_dims, box));
-    const bool overlap = n * (d_in + d_out) <= kOverlapElems;
+    const bool early = n * (d_in + d_out) <= kOverlapElems;
     const unsigned blocks = (unsigned)(w.chunks * w.m_tiles * w.n_tiles);
     if (h) {
         SAR_TRY(ensure_smem(grouped_weight_kernel<false>, w.smem));
-        SAR_LAUNCH("linear_grouped_bwd_weight", st, launch_if(overlap, grouped_weight_kernel<false>, blocks, kWeightThreads, w.smem, st, p));
+        SAR_LAUNCH("linear_grouped_bwd_weight", st, launch_if(early, grouped_weight_kernel<false>, blocks, kWeightThreads, w.smem, st, p));
     } else {
         SAR_TRY(ensure_smem(grouped_weight_kernel<true>, w.smem));
-        SAR_LAUNCH("linear_grouped_bwd_weight_ckpt8", st, launch_if(overlap, grouped_weight_kernel<true>, blocks, kWeightThreads8, w.smem, st, p));
+        SAR_LAUNCH("linear_grouped_bwd_weight_ckpt8", st, launch_if(early, grouped_weight_kernel<true>, blocks, kWeightThreads8, w.smem, st, p));
     }
     SAR_TRY(sar_after_launch());
     const long long quads = (long long)d_in * d_out / 4;
@@ -968,6 +977,7 @@ sar_status sar_linear_grouped(int64_t n, int32_t groups, int32_t d_in, int32_t d
     if (flags & ~(uint32_t)SAR_GROUPED_ZERO_REST) return SAR_ERR_INVALID_ARG;
     if (n == 0) return grouped_check(n, groups, d_in, d_out, t, offsets, {});
     SAR_TRY(grouped_check(n, groups, d_in, d_out, t, offsets, {h, w, z}));
+    SAR_TRY(grouped_apart(n, groups, d_in, d_out, h, d_in, w, z, d_out));
     return grouped_rows<false>(n, groups, d_in, d_out, offsets, h, w, z, flags, flag, static_cast<cudaStream_t>(stream), "linear_grouped");
 }
 
@@ -976,6 +986,7 @@ sar_status sar_linear_grouped_bwd_input(int64_t n, int32_t groups, int32_t d_in,
     if (flags & ~(uint32_t)SAR_GROUPED_ZERO_REST) return SAR_ERR_INVALID_ARG;
     if (n == 0) return grouped_check(n, groups, d_in, d_out, t, offsets, {});
     SAR_TRY(grouped_check(n, groups, d_in, d_out, t, offsets, {dz, w, dh}));
+    SAR_TRY(grouped_apart(n, groups, d_in, d_out, dz, d_out, w, dh, d_in));
     return grouped_rows<true>(n, groups, d_out, d_in, offsets, dz, w, dh, flags, flag, static_cast<cudaStream_t>(stream), "linear_grouped_bwd_input");
 }
 

@@ -87,6 +87,17 @@ def test_grouped_products(lib):
     assert lib.sar_linear_grouped_workspace_bytes(c_int64(0), c_int32(1), c_int32(8), c_int32(8)) == 0
 
 
+def test_results_over_operands_are_refused(lib):
+    """z over any part of the rows (n d 2 bytes) or of the weights, from either side."""
+    n, G, di, do, z = 100, 3, 64, 32, 1 << 24
+    for fn, rows, result in ((lib.sar_linear_grouped, n * di * 2, n * do * 2), (lib.sar_linear_grouped_bwd_input, n * do * 2, n * di * 2)):
+        for at, size, far in ((6, rows, 7), (7, G * di * do * 2, 6)):
+            for start in (z, z + result - 16, z - size + 16):
+                args = [c_int64(n), c_int32(G), c_int32(di), c_int32(do), BF16, P, P, P, c_void_p(z), c_uint32(0), NULL, NULL]
+                args[at], args[far] = c_void_p(start), c_void_p(1 << 30)
+                assert fn(*args) == INVALID
+
+
 def test_tensors_that_are_not_on_a_device_are_refused():
     from paper_2111_06483_b200 import api
     x, o = torch.zeros(4, 32, dtype=torch.bfloat16), torch.tensor([0, 4])
