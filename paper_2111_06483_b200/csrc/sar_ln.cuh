@@ -52,7 +52,7 @@ static inline unsigned ln_grid(long long rows) { return (unsigned)((rows + LnLan
 
 // Sums over a group's lanes.  A block's go by way of red[which]: two of them in turn, so that a sum costs one barrier.
 struct LnRed {
-    float2 red[2][kWarpsPerBlock];
+    alignas(16) float2 red[2][kWarpsPerBlock];
 };
 template <int G>
 __device__ __forceinline__ float2 ln_sum2(float2 x, LnRed &r, int which) {
@@ -64,22 +64,33 @@ __device__ __forceinline__ float2 ln_sum2(float2 x, LnRed &r, int which) {
     if constexpr (G > 32) {
         if ((threadIdx.x & 31) == 0) r.red[which][threadIdx.x >> 5] = x;
         __syncthreads();
-        x = r.red[which][0];
+        const float4 *const all = reinterpret_cast<const float4 *>(r.red[which]);
+        x = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int w = 1; w < kWarpsPerBlock; ++w) x = __fadd2_rn(x, r.red[which][w]);
+        for (int w = 0; w < kWarpsPerBlock / 2; ++w) {
+            const float4 two = all[w];
+            x = __fadd2_rn(x, __fadd2_rn(make_float2(two.x, two.y), make_float2(two.z, two.w)));
+        }
     }
     return x;
 }
 template <int G>
 __device__ __forceinline__ float ln_sum(float x, LnRed &r, int which) {
     constexpr int W = G < 32 ? G : 32;
-    if constexpr (G > 32) {
-        return ln_sum2<G>(make_float2(x, 0.f), r, which).x;
-    } else {
 #pragma unroll
-        for (int d = W / 2; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d, W);
-        return x;
+    for (int d = W / 2; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d, W);
+    if constexpr (G > 32) {
+        float *const red = reinterpret_cast<float *>(r.red[which]);
+        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
+        __syncthreads();
+        x = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarpsPerBlock / 4; ++w) {
+            const float4 four = reinterpret_cast<const float4 *>(red)[w];
+            x += four.x + four.y + (four.z + four.w);
+        }
     }
+    return x;
 }
 __device__ __forceinline__ float2 ln_splat(float x) { return make_float2(x, x); }
 
