@@ -33,27 +33,31 @@ struct LnArgs {
     float *partial;               // [blocks][2][C] or null (no weight gradients asked for)
 };
 
-// Where a thread stands: lane gl of group gid of its warp, whose first row is the block's row `first`; a group is the whole block
-// where G is 256.
+// Where a thread stands: lane gl of group gid of its warp, whose first row is the block's row `first`.  Groups of 64 lanes and more
+// are several warps.
 template <int G>
 struct LnLane {
     static constexpr int kRows = kThreads / G;   // rows that a block has in hand
-    static constexpr bool kBlock = G > 32;
-    static_assert(!kBlock || G == kThreads, "a group is lanes of a warp or the block");
+    static constexpr bool kWarps = G > 32;
     int gl, gid, first;
     __device__ __forceinline__ LnLane() {
         gl = threadIdx.x & (G - 1);
-        gid = kBlock ? 0 : (threadIdx.x & 31) / G;
-        first = kBlock ? 0 : (threadIdx.x >> 5) * (32 / G);
+        gid = kWarps ? 0 : (threadIdx.x & 31) / G;
+        first = kRows == 1 ? 0 : kWarps ? threadIdx.x / G : (threadIdx.x >> 5) * (32 / G);
     }
 };
 template <int G>
 static inline unsigned ln_grid(long long rows) { return (unsigned)((rows + LnLane<G>::kRows - 1) / LnLane<G>::kRows); }
 
-// Sums over a group's lanes.  A block's go by way of red[which]: two of them in turn, so that a sum costs one barrier.
+// Sums over a group's lanes.  Several warps' go by way of red[which]: two of them in turn, so that a sum costs one barrier.
 struct LnRed {
     alignas(16) float2 red[2][kWarpsPerBlock];
 };
+template <int G>
+__device__ __forceinline__ void ln_group_sync() {
+    if constexpr (G == kThreads) __syncthreads();
+    else asm volatile("bar.sync %0, %1;\n" ::"r"(1u + threadIdx.x / G), "n"(G) : "memory");
+}
 template <int G>
 __device__ __forceinline__ float2 ln_sum2(float2 x, LnRed &r, int which) {
     constexpr int W = G < 32 ? G : 32;
@@ -63,11 +67,11 @@ __device__ __forceinline__ float2 ln_sum2(float2 x, LnRed &r, int which) {
     for (int d = W / 2; d > 0; d >>= 1) x.y += __shfl_xor_sync(0xffffffffu, x.y, d, W);
     if constexpr (G > 32) {
         if ((threadIdx.x & 31) == 0) r.red[which][threadIdx.x >> 5] = x;
-        __syncthreads();
-        const float4 *const all = reinterpret_cast<const float4 *>(r.red[which]);
+        ln_group_sync<G>();
+        const float4 *const all = reinterpret_cast<const float4 *>(r.red[which] + threadIdx.x / G * (G / 32));
         x = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < kWarpsPerBlock / 2; ++w) {
+        for (int w = 0; w < G / 64; ++w) {
             const float4 two = all[w];
             x = __fadd2_rn(x, __fadd2_rn(make_float2(two.x, two.y), make_float2(two.z, two.w)));
         }
@@ -82,11 +86,16 @@ __device__ __forceinline__ float ln_sum(float x, LnRed &r, int which) {
     if constexpr (G > 32) {
         float *const red = reinterpret_cast<float *>(r.red[which]);
         if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
-        __syncthreads();
+        ln_group_sync<G>();
+        const float *const mine = red + threadIdx.x / G * (G / 32);
         x = 0.f;
+        if constexpr (G == 64) {
+            const float2 two = *reinterpret_cast<const float2 *>(mine);
+            x = two.x + two.y;
+        }
 #pragma unroll
-        for (int w = 0; w < kWarpsPerBlock / 4; ++w) {
-            const float4 four = reinterpret_cast<const float4 *>(red)[w];
+        for (int w = 0; w < G / 128; ++w) {
+            const float4 four = reinterpret_cast<const float4 *>(mine)[w];
             x += four.x + four.y + (four.z + four.w);
         }
     }
@@ -97,9 +106,11 @@ __device__ __forceinline__ float2 ln_splat(float x) { return make_float2(x, x); 
 // A row across the G lanes of a group, each with V slots of E columns: 16 bytes (8 bf16, 4 float32), or one column where the
 // arrays are not aligned to that.  Few lanes with many columns each, 16 of bf16 and 8 of float32 where that covers the row,
 // rather than many lanes with few: a warp then has up to 8 rows in hand and joins their sums in 2 to 4 steps instead of 5
-// (a million rows of 256 bf16, forward: 32 lanes of 8 columns 208 us, 16 of 16 171).  Above 1,024 columns the group is the block:
-// a row still stays in registers and is read once (120,000 rows of 2,048 bf16, us, a block that reads its row again for every
-// pass against this: forward 564 / 210, with the checkpoint 1091 / 260, backward 945 / 274, from the checkpoint 1261 / 273).
+// (a million rows of 256 bf16, forward: 32 lanes of 8 columns 208 us, 16 of 16 171).  Wide rows take 64 lanes and more, up to the
+// block, so that they too stay in registers and are read once (us: 250,000 rows of 1,024 bf16, a warp against 64 lanes, forward with
+// the checkpoint 273 / 252, backward from it 292 / 252; float32, forward 326 / 309 with 128 lanes, with the checkpoint 449 / 357;
+// 120,000 rows of 2,048 bf16, a block that reads its row again for every pass against 128 lanes, forward 564 / 171, backward
+// 945 / 260, with the checkpoint 1091 / 239, from it 1261 / 278).
 //
 // LnRow: E divides C (or is 1).  Slot v of lane gl holds the columns from (v G + gl) E on, all or none of them.
 template <typename T_, int E_, int G_, int V_>
@@ -411,20 +422,17 @@ struct LnShiftedRow {
 
 // Blocks that an SM is to hold at least, which bounds the registers, for N columns a lane.  64 million values in rows of 256, us, as the
 // compiler likes and so: bf16 forward 106 registers 48, 80 (three blocks) 43; backward 138 86, 128 (two) 63, from the checkpoint 140
-// 107, 128 61; float32 forward with the checkpoint 84 118, 78 (three) 99.  Wider rows: two where the pass carries no sums (1,024
-// bf16 with the checkpoint 100, two blocks 79), one where it does (backward 87, two blocks 172: the sums leave the registers).
-// Rows of a block wait at a barrier for every sum, so other blocks have to fill in: 120,000 rows of 2,048 bf16 backward two blocks
-// 354, three 274, from the checkpoint 446, 315, four 273; 60,000 of 4,096 forward two 207, three 176, four 185, backward one 408,
-// two 255, three 442.
+// 107, 128 61; float32 forward with the checkpoint 84 118, 78 (three) 99.  Groups of several warps wait for each other at every sum,
+// so other blocks have to fill in: 60,000 rows of 4,096 bf16 forward two 207, three 176, four 185, backward one 408, two 255,
+// three 442 (the sums leave the registers).
 template <typename Row>
 constexpr int ln_blocks(bool bwd, bool ck) {
     constexpr int N = Row::E * Row::V, E = Row::E;
-    if (Row::G > 32) return bwd ? (N <= 4 ? (E == 1 ? 3 : 4) : N <= 8 ? (E == 8 ? 4 : E == 4 ? 3 : 2) : N <= 16 ? 2 : 1) : N <= 8 ? 4 : N <= 16 && E != 4 ? 3 : 2;
+    if (Row::G > 32) return bwd ? (N <= 4 ? 3 : N <= 8 ? (E == 4 ? 3 : 2) : N <= 16 ? 2 : 1) : N <= 8 ? 4 : N <= 16 && E != 4 ? 3 : 2;
     if (E == 1) return bwd && N > 4 ? 2 : 3;
     if (bwd) return N <= 8 && ck && E == 4 && !Row::kShifted ? 3 : N <= (Row::kShifted && E == 4 ? 12 : 16) ? 2 : 1;
     if (Row::kShifted) return N <= 24 ? 2 : 1;
-    if (E == 8) return N <= 16 && !ck ? 3 : 2;
-    return N <= 8 ? 3 : N >= 32 && !ck ? 1 : 2;
+    return E == 8 ? (N <= 16 && !ck ? 3 : 2) : N <= 8 ? 3 : 2;
 }
 
 // Rows are walked one ahead: a group asks for its next row before it works on the one it has (two sets of registers in turn),
@@ -493,7 +501,7 @@ template <typename Row, bool CK>
 __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_kernel(const LnArgs a) {
     after_predecessor();
     constexpr int G = Row::G, V = Row::V, P = Row::P;
-    extern __shared__ float smem[];   // [copies][2][C]
+    extern __shared__ float smem[];   // [copies][2][C]; groups of several warps: [2][C] where there is more than one
     __shared__ LnRed red;
     const LnLane<G> id;
     const long long stride = (long long)gridDim.x * id.kRows;
@@ -562,16 +570,26 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_ker
         work(base + stride, two, 1);
     }
     if (!a.partial) return;
-    if constexpr (id.kBlock) {   // a column is one thread's
+    if constexpr (id.kWarps) {   // a column is one thread's in each group: the groups' one after the other
         float *const p = a.partial + (size_t)blockIdx.x * 2 * a.C;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
+        for (int t = id.kRows - 1; t >= 0; --t) {
+            if (id.first == t) {
+                float *const to = t == 0 ? p : smem;
 #pragma unroll
-            for (int e = 0; e < Row::E; ++e)
-                if (r.has(v, e)) {
-                    p[r.col(v) + e] = e & 1 ? s1[v][e / 2].y : s1[v][e / 2].x;
-                    p[a.C + r.col(v) + e] = e & 1 ? s0[v][e / 2].y : s0[v][e / 2].x;
-                }
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int e = 0; e < Row::E; ++e)
+                        if (r.has(v, e)) {
+                            const int c = r.col(v) + e;
+                            float along = e & 1 ? s1[v][e / 2].y : s1[v][e / 2].x, level = e & 1 ? s0[v][e / 2].y : s0[v][e / 2].x;
+                            if (t < id.kRows - 1) along += smem[c], level += smem[a.C + c];
+                            to[c] = along;
+                            to[a.C + c] = level;
+                        }
+            }
+            if (t > 0) __syncthreads();
+        }
         return;
     }
     // The groups of a warp, then the warps, which have a copy each where they fit (one after the other otherwise).  Rows that start at
@@ -779,14 +797,11 @@ struct LnShape {
     bool shifted;
 };
 // Every (E, G, V) of a kind of row in ascending E G V: the first that covers the row is taken.
-#define SAR_LN_8(X) X(8, 4, 1) X(8, 4, 2) X(8, 4, 3) X(8, 8, 2) X(8, 8, 3) X(8, 16, 2) X(8, 16, 3) X(8, 32, 2) X(8, 32, 3) X(8, 32, 4) X(8, 256, 1) X(8, 256, 2) X(8, 256, 4)
-#define SAR_LN_4(X) X(4, 4, 1) X(4, 4, 2) X(4, 8, 2) X(4, 8, 3) X(4, 16, 2) X(4, 16, 3) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6) X(4, 32, 8) X(4, 256, 2) X(4, 256, 4) X(4, 256, 8)
-// ... float32 in the backward pass, which carries two sums for each column: 1,024 columns in a block, 250,000 rows 484 us, in a warp
-// 522, from the checkpoint 430 and 493 (forward 407 and 326)
-#define SAR_LN_4B(X) X(4, 4, 1) X(4, 4, 2) X(4, 8, 2) X(4, 8, 3) X(4, 16, 2) X(4, 16, 3) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6) X(4, 256, 1) X(4, 256, 2) X(4, 256, 4) X(4, 256, 8)
+#define SAR_LN_8(X) X(8, 4, 1) X(8, 4, 2) X(8, 4, 3) X(8, 8, 2) X(8, 8, 3) X(8, 16, 2) X(8, 16, 3) X(8, 32, 2) X(8, 32, 3) X(8, 64, 2) X(8, 64, 3) X(8, 128, 2) X(8, 256, 2) X(8, 256, 4)
+#define SAR_LN_4(X) X(4, 4, 1) X(4, 4, 2) X(4, 8, 2) X(4, 8, 3) X(4, 16, 2) X(4, 16, 3) X(4, 32, 2) X(4, 32, 3) X(4, 64, 2) X(4, 64, 3) X(4, 128, 2) X(4, 128, 3) X(4, 256, 2) X(4, 256, 4) X(4, 256, 8)
 // ... bf16 that divides into fours but not eights, where the pass reads x: 16 columns a lane here, too.  A million rows of 100, us, 8 a
 // lane against 16: forward 92 / 92, with the checkpoint 167 / 151, backward 160 / 115; from the checkpoint 152 / 155
-#define SAR_LN_4H(X) X(4, 4, 1) X(4, 4, 2) X(4, 4, 4) X(4, 8, 3) X(4, 8, 4) X(4, 16, 3) X(4, 16, 4) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6) X(4, 32, 8) X(4, 256, 2) X(4, 256, 4) X(4, 256, 8)
+#define SAR_LN_4H(X) X(4, 4, 1) X(4, 4, 2) X(4, 4, 4) X(4, 8, 3) X(4, 8, 4) X(4, 16, 3) X(4, 16, 4) X(4, 32, 3) X(4, 32, 4) X(4, 64, 3) X(4, 64, 4) X(4, 128, 4) X(4, 256, 4) X(4, 256, 8)
 #define SAR_LN_8S(X) X(8, 16, 2) X(8, 32, 2) X(8, 32, 3) X(8, 32, 4)
 #define SAR_LN_4S(X) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6) X(4, 32, 8)
 // ... and narrow shifted rows, for what reads checkpoints or only packs
@@ -826,9 +841,7 @@ static inline sar_status ln_dispatch(const LnShape &s, Fn &&f) {
     if constexpr (sizeof(T) == 2) {
         SAR_LN_8(SAR_LN_CASE)
     }
-    if constexpr (sizeof(T) == 4 && (PASS == kLnBwd || PASS == kLnBwd8)) {
-        SAR_LN_4B(SAR_LN_CASE)
-    } else if constexpr (sizeof(T) == 2 && (PASS == kLnFwd || PASS == kLnBwd)) {
+    if constexpr (sizeof(T) == 2 && (PASS == kLnFwd || PASS == kLnBwd)) {
         SAR_LN_4H(SAR_LN_CASE)
     } else {
         SAR_LN_4(SAR_LN_CASE)
@@ -852,9 +865,7 @@ static inline LnShape ln_shape(int32_t C, sar_dtype t, LnPass pass, size_t array
     if (E == 8 && may(8)) {
         SAR_LN_8(SAR_LN_FIT)
     } else if (may(4)) {
-        if (E == 4 && (pass == kLnBwd || pass == kLnBwd8)) {
-            SAR_LN_4B(SAR_LN_FIT)
-        } else if (E == 8 && (pass == kLnFwd || pass == kLnBwd)) {
+        if (E == 8 && (pass == kLnFwd || pass == kLnBwd)) {
             SAR_LN_4H(SAR_LN_FIT)
         } else {
             SAR_LN_4(SAR_LN_FIT)
@@ -940,10 +951,10 @@ static sar_status ln_backward_of(const LnShape &s, const LnArgs &a, unsigned *re
     }
     return ln_dispatch<T, CK ? kLnBwd8 : kLnBwd>(s, [&](auto cfg) -> sar_status {
         using Row = typename decltype(cfg)::row;
-        static const unsigned most = ln_resident(ln_bwd_kernel<Row, CK>, Row::G > 32 ? 0 : kLnSmem);
+        static const unsigned most = ln_resident(ln_bwd_kernel<Row, CK>, Row::G == kThreads ? 0 : kLnSmem);
         const unsigned want = ln_grid<Row::G>((a.n + 1) / 2);   // two rows per lane group, which it asks for at once, before a block pays for its record
         *records = want < 1 ? 1 : want < most ? want : most;
-        return ln_launch(name, ln_bwd_kernel<Row, CK>, want, most, Row::G <= 32 && a.partial ? (size_t)ln_copies(a.C) * 2 * a.C * 4 : 0, a, st);
+        return ln_launch(name, ln_bwd_kernel<Row, CK>, want, most, !a.partial || Row::G == kThreads ? 0 : (size_t)(Row::G > 32 ? 1 : ln_copies(a.C)) * 2 * a.C * 4, a, st);
     });
 }
 

@@ -189,6 +189,17 @@ def test_rows_that_a_block_shares(n, c, dt):
     test_backward_from_the_checkpoint(n, c, dt)
 
 
+@pytest.mark.parametrize("c", [388, 392, 508, 512, 516, 520, 764, 768, 776, 1016, 1024, 1280, 1532, 1536, 1540, 1544, 2040])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 2, 3, 79, 1502])
+def test_rows_that_several_warps_share(n, c, dt):
+    """Rows of more than a warp's columns, several to a block, whose last ones have no row."""
+    test_forward(n, c, dt, 1.0)
+    test_forward_with_the_checkpoint_of_its_rows(n, c, dt, 1.0)
+    test_backward(n, c, dt, 1.0)
+    test_backward_from_the_checkpoint(n, c, dt)
+
+
 @pytest.mark.parametrize("c", [1021, 2000, 2047, 4100, 8192])
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_wide_rows_in_place(c, dt):
