@@ -352,7 +352,6 @@ struct WeightArgs {
 constexpr int kAdders = 8, kMakers = 8;   // warps; the adders' work is laid out for 8
 constexpr int kWeightThreads = 64 + kAdders * 32, kWeightThreads8 = kWeightThreads + kMakers * 32;
 constexpr uint32_t kTurnBuf = 32 * 64;    // an adder's 32 rows of 16 sums on their way out
-constexpr uint32_t kSumCols = 256;        // where the sums lie in tensor memory, behind the accumulators
 struct WeightShared {
     alignas(8) uint64_t full[kStagesMax], empty[kStagesMax], made[kStagesMax], acc_full[2], acc_empty[2];
     uint32_t tmem;
@@ -368,7 +367,6 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     const uint32_t turns = (smem_addr(dyn) + (uint32_t)sizeof(WeightShared) + 1023u) & ~1023u, ring = turns + kAdders * kTurnBuf;
     const int panels = p.cols / 64;
     const uint32_t panel = p.step * 128, stage_bytes = (p.h_panels + panels) * panel, dz_at = p.h_panels * panel;
-    const uint32_t bufs = p.cols <= 128 ? 2 : 1;   // accumulators of 128 columns each, or one of up to 256
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *failed = &sh.failed;
 
@@ -395,6 +393,8 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     const int chunk = blockIdx.x / tiles, tile = blockIdx.x % tiles, m_tile = tile / p.n_tiles;
     const int m0 = m_tile * 128, n0 = tile % p.n_tiles * p.cols, cols = min(p.cols, p.d_out - n0);
     const int h_panels = p.d_in - m0 > 64 ? 2 : 1;   // with columns
+    // tensor memory: two accumulators and the sums where all three fit, one of up to 256 columns and the sums otherwise
+    const uint32_t apart = (cols + 31) & ~31, bufs = 3 * apart <= kTmemCols ? 2 : 1, sum_cols = bufs == 2 ? 2 * apart : kTmemCols / 2;
     const int chunk0 = (int)min((long long)p.n, (long long)chunk * p.chunk_rows), chunk1 = (int)min((long long)p.n, (long long)chunk0 + p.chunk_rows);
     int g0 = 0;   // the first group that ends behind the chunk's start
     for (int hi = p.G; g0 < hi;) {
@@ -470,11 +470,11 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                         const uint64_t da = tc_operand(at, panel, 1024), db = tc_operand(at + dz_at, panel, 1024);
 #pragma unroll
                         for (int j = 0; j < kStep / 16; ++j)
-                            if (j * 16 < rows) tc_mma(tmem + buf * 128, tc_advance(da, j * 2048), tc_advance(db, j * 2048), instr, r > r0 || j > 0);
+                            if (j * 16 < rows) tc_mma(tmem + buf * apart, tc_advance(da, j * 2048), tc_advance(db, j * 2048), instr, r > r0 || j > 0);
                         if (rows > kStep) {
 #pragma unroll
                             for (int j = kStep / 16; j < kStepMost / 16; ++j)
-                                if (j * 16 < rows) tc_mma(tmem + buf * 128, tc_advance(da, j * 2048), tc_advance(db, j * 2048), instr, true);
+                                if (j * 16 < rows) tc_mma(tmem + buf * apart, tc_advance(da, j * 2048), tc_advance(db, j * 2048), instr, true);
                         }
                         tc_commit(smem_addr(&sh.empty[s]));
                     }
@@ -548,8 +548,8 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                 const bool first = r0 == lo, last = r0 + kRunRows >= hi;
                 for (int c = part * 32; c < cols; c += kAdders / 4 * 32) {
                     uint32_t x[32], y[32];
-                    tmem_ask(tmem + buf * 128 + c + lanes, x);
-                    if (!first) tmem_ask(tmem + kSumCols + c + lanes, y);
+                    tmem_ask(tmem + buf * apart + c + lanes, x);
+                    if (!first) tmem_ask(tmem + sum_cols + c + lanes, y);
                     tmem_wait_load(x);
                     if (!first) {
                         tmem_tie(y);
@@ -557,7 +557,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                         for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) + __uint_as_float(y[e]));
                     }
                     if (!last) {
-                        tmem_store(tmem + kSumCols + c + lanes, x);
+                        tmem_store(tmem + sum_cols + c + lanes, x);
                     } else {
                         // A thread has a row of 32 sums.  Written so, a store touches 32 lines (128 x 256 sums: 10,000 cycles); turned in
                         // shared memory, where chunk q of row l lies at q ^ (l >> 1 & 3), it writes 64 bytes of 8 rows.
