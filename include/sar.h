@@ -651,14 +651,20 @@ SAR_API sar_status sar_ln_bwd_ckpt8(int64_t n, int32_t C, sar_dtype t, const int
  *   sar_linear_grouped_bwd_weight_ckpt8  the same with h = gamma * v + beta, v what the checkpoint (codes, scales) stands for;
  *                                  gamma, beta [d_in] float32 may be NULL (1 / 0): the weight gradient behind sar_ln_fwd_ckpt8.
  * Rows of no group (before offsets[0], from offsets[groups] on) take part in nothing; z and dh are left there as they were, or
- * written as zeros with flags = SAR_GROUPED_ZERO_REST.  Neither may overlap the rows or the weights (SAR_ERR_INVALID_ARG).  flag (DEVICE int, may be NULL) is set to 1 if a wait inside the kernel
- * ran out of its bound (seconds), which leaves results unwritten; the library's tests check that it stays 0.
+ * written as zeros with flags = SAR_GROUPED_ZERO_REST.  Neither may overlap the rows or the weights (SAR_ERR_INVALID_ARG).
+ * flag (DEVICE int, may be NULL) is set to 1 if a wait inside the kernel ran out of its limit, which leaves results unwritten;
+ * the library's tests check that it stays 0.  A block that gives up ends only after its copies and products in flight.
+ *   sar_set_wait_limit           the limit, in clock cycles, of each wait inside the launches of these four calls from now on (4e9
+ *                                by default, about two seconds, which a negative value brings back); returns the one before.
+ *                                With 0 a wait gives up that is not over at the first look.  Process-global; launches that
+ *                                a graph has captured keep theirs.  For tests and for GPUs shared with longer work.
  * Arrays are 16-byte aligned (codes 8), t must be SAR_BF16, d_in and d_out multiples of 8 up to 2^20, groups <= SAR_MAX_GROUPS,
  * n < 2^31 - 2048 (SAR_ERR_UNSUPPORTED otherwise).  Scratch of the weight calls: sar_linear_grouped_workspace_bytes.  n = 0 is
  * allowed (dw is then written as zeros).
  * ------------------------------------------------------------------------------------------- */
 #define SAR_MAX_GROUPS 1024
 #define SAR_GROUPED_ZERO_REST 1u
+SAR_API int64_t sar_set_wait_limit(int64_t cycles);
 SAR_API size_t sar_linear_grouped_workspace_bytes(int64_t n, int32_t groups, int32_t d_in, int32_t d_out);
 SAR_API sar_status sar_linear_grouped(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, sar_dtype t, const int64_t *offsets,
                                       const void *h, const void *w, void *z, uint32_t flags, int32_t *flag, void *stream);

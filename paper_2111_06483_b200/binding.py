@@ -43,7 +43,7 @@ EXPORTS = [
     "sar_propagate_workspace_bytes", "sar_propagate_workspace_bytes_at", "sar_propagate",
     "sar_ln_workspace_bytes", "sar_ln_fwd", "sar_ln_bwd", "sar_ln_fwd_ckpt8", "sar_ln_bwd_ckpt8", "sar_ckpt8_pack", "sar_ckpt8_unpack",
     "sar_linear_grouped_workspace_bytes", "sar_linear_grouped", "sar_linear_grouped_bwd_input", "sar_linear_grouped_bwd_weight",
-    "sar_linear_grouped_bwd_weight_ckpt8",
+    "sar_linear_grouped_bwd_weight_ckpt8", "sar_set_wait_limit",
 ]
 
 
@@ -90,6 +90,7 @@ def lib() -> ctypes.CDLL:
                      "sar_degree_order_workspace_bytes", "sar_plan_many_workspace_bytes", "sar_propagate_workspace_bytes", "sar_propagate_workspace_bytes_at",
                      "sar_ln_workspace_bytes", "sar_linear_grouped_workspace_bytes"):
             getattr(L, name).restype = c_size_t
+        L.sar_set_wait_limit.restype = c_int64
         _lib = L
     return _lib
 
@@ -931,6 +932,11 @@ def sar_ln_bwd_ckpt8(codes: torch.Tensor, scales: torch.Tensor, rstd: torch.Tens
 
 def sar_linear_grouped_workspace_bytes(n: int, groups: int, d_in: int, d_out: int) -> int:
     return int(lib().sar_linear_grouped_workspace_bytes(c_int64(n), c_int32(groups), c_int32(d_in), c_int32(d_out)))
+
+
+def sar_set_wait_limit(cycles: int) -> int:
+    """Limit of the waits inside the launches by group from now on, in clock cycles (negative: the default); returns the one before."""
+    return int(lib().sar_set_wait_limit(c_int64(cycles)))
 
 
 def _group_offsets(offsets: Optional[torch.Tensor], groups: int) -> None:

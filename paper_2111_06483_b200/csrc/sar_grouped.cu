@@ -9,6 +9,7 @@
 #include "sar_dispatch.cuh"
 #include "sar_tc.cuh"
 
+#include <atomic>
 #include <utility>
 
 namespace sar {
@@ -18,6 +19,7 @@ constexpr int kStep = 64;           // contraction per stage: 128 bytes of bf16
 constexpr int kPanel = 64 * 128;    // 64 rows of 128 bytes
 constexpr int kStepMost = 128;      // rows of a stage where they are the contraction
 constexpr int kGroupsMax = SAR_MAX_GROUPS;
+static std::atomic<long long> g_wait_limit{kWaitCycles};   // of the launches to come (sar_set_wait_limit)
 
 sar_status tc_tensor_map(CUtensorMap *map, const void *base, int rank, const uint64_t *dims, const uint32_t *box) {
     using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
@@ -95,6 +97,7 @@ struct RowsArgs {
     const int64_t *offsets;
     __nv_bfloat16 *out;
     int *flag;
+    long long wait_limit;
     int n, G, K, N;
     int cols;        // columns per slice (a multiple of 64 up to 256)
     int slices;      // slices of columns
@@ -108,8 +111,8 @@ constexpr int kRowsThreads = 192;
 constexpr int kStoreBuf = 32 * 128;   // a warp's 32 rows of 64 columns
 constexpr int kSlotsMax = 4, kStagesMax = 8;
 struct RowsShared {
-    alignas(8) uint64_t full[kStagesMax], empty[kStagesMax], w_full[kSlotsMax], w_empty[kSlotsMax], acc_full[2], acc_empty[2];
-    uint32_t tmem;
+    alignas(8) uint64_t full[kStagesMax], empty[kStagesMax], w_full[kSlotsMax], w_empty[kSlotsMax], acc_full[2], acc_empty[2], done;
+    uint32_t tmem, filled, sets;   // stages and sets of weights that copies were issued into
     int failed;
     GroupTable table;
 };
@@ -125,7 +128,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
     const uint32_t stage_bytes = kTileRows * 128 + (p.slots ? 0 : w_step);
     const uint32_t ring = base + 4 * p.store_bufs * kStoreBuf, weights = ring + p.stages * stage_bytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    volatile int *failed = &sh.failed;
+    const Waits waits{&sh.failed, p.wait_limit};
 
     // the table, tensor memory, the barriers and the maps, each by a warp of its own
     group_table(sh.table, p.offsets, p.G, p.n);
@@ -134,6 +137,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
         for (int i = 0; i < p.stages; ++i) bar_init(smem_addr(&sh.full[i]), 1), bar_init(smem_addr(&sh.empty[i]), 1);
         for (int i = 0; i < kSlotsMax; ++i) bar_init(smem_addr(&sh.w_full[i]), 1), bar_init(smem_addr(&sh.w_empty[i]), 1);
         for (int i = 0; i < 2; ++i) bar_init(smem_addr(&sh.acc_full[i]), 1), bar_init(smem_addr(&sh.acc_empty[i]), 4);
+        bar_init(smem_addr(&sh.done), 1);
         sh.failed = 0;
         bar_init_fence();
     }
@@ -168,7 +172,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
             while (t >= sh.table.tiles[g + 1]) ++g;
             if (p.slots && g != held) {
                 const uint32_t slot = ws.at, bar = smem_addr(&sh.w_full[slot]);
-                ok = warp_wait(smem_addr(&sh.w_empty[slot]), ws.round ^ 1, failed);
+                ok = warp_wait(smem_addr(&sh.w_empty[slot]), ws.round ^ 1, waits);
                 if (!ok) break;
                 if (one_lane()) {
                     bar_expect(bar, w_set);
@@ -187,7 +191,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
             const int row = sh.table.first[g] + (t - sh.table.tiles[g]) * kTileRows;
             for (int k = 0; k < p.steps; ++k, ++use, st.next(p.stages)) {
                 const uint32_t s = st.at, bar = smem_addr(&sh.full[s]), at = ring + s * stage_bytes;
-                ok = warp_wait(smem_addr(&sh.empty[s]), st.round ^ 1, failed);
+                ok = warp_wait(smem_addr(&sh.empty[s]), st.round ^ 1, waits);
                 if (!ok) break;
                 if (one_lane()) {
                     bar_expect(bar, stage_bytes);
@@ -202,10 +206,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
                 __syncwarp();
             }
         }
-        if (!ok) {   // the copies in flight end before the block does
-            for (uint32_t s = 0; s < (uint32_t)p.stages && s < use; ++s) bar_drain(smem_addr(&sh.full[s]), ((use - 1 - s) / p.stages) & 1);
-            for (uint32_t s = 0; s < (uint32_t)p.slots && s < set; ++s) bar_drain(smem_addr(&sh.w_full[s]), ((set - 1 - s) / p.slots) & 1);
-        }
+        if (lane == 0) sh.filled = use, sh.sets = set;
     } else if (warp == 1) {
         const uint32_t instr = tc_instr((cols + 15) & ~15, false, !WT);
         RingPlace st, ws, acc;
@@ -220,18 +221,18 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
                     __syncwarp();
                     ws.next(p.slots);
                 }
-                ok = warp_wait(smem_addr(&sh.w_full[ws.at]), ws.round, failed);
+                ok = warp_wait(smem_addr(&sh.w_full[ws.at]), ws.round, waits);
                 if (!ok) break;
                 wset = weights + ws.at * w_set;
                 held = g;
             }
-            ok = warp_wait(smem_addr(&sh.acc_empty[acc.at]), acc.round ^ 1, failed);
+            ok = warp_wait(smem_addr(&sh.acc_empty[acc.at]), acc.round ^ 1, waits);
             if (!ok) break;
             tc_after_sync();
             const uint32_t d = tmem + acc.at * 256;
             for (int k = 0; k < p.steps; ++k, st.next(p.stages)) {
                 const uint32_t at = ring + st.at * stage_bytes, b = p.slots ? wset + k * w_step : at + kTileRows * 128;
-                ok = warp_wait(smem_addr(&sh.full[st.at]), st.round, failed);
+                ok = warp_wait(smem_addr(&sh.full[st.at]), st.round, waits);
                 if (!ok) break;
                 const int left = (min(kStep, p.K - k * kStep) + 15) / 16;   // copies fill what lies beyond K with zeros
                 if (one_lane()) {
@@ -255,7 +256,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
         for (int t = t0; t < t1; ++t, acc.next(2)) {
             const uint32_t buf = acc.at;
             while (t >= sh.table.tiles[g + 1]) ++g;
-            if (!warp_wait(smem_addr(&sh.acc_full[buf]), acc.round, failed)) break;
+            if (!warp_wait(smem_addr(&sh.acc_full[buf]), acc.round, waits)) break;
             tc_after_sync();
             const int row = sh.table.first[g] + (t - sh.table.tiles[g]) * kTileRows + quad * 32;
             const int rows = min(32, sh.table.first[g + 1] - row);   // may be <= 0
@@ -314,6 +315,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
     tc_before_sync();
     __syncthreads();
     tc_after_sync();
+    if (sh.failed) {
+        if (threadIdx.x == 0) drain_copies(sh.full, p.stages, sh.filled), drain_copies(sh.w_full, p.slots, sh.sets);
+        if (warp == 1) drain_products(&sh.done);
+    }
     if (warp == 1) tmem_free(tmem);
     if (threadIdx.x == 0 && sh.failed && p.flag) *p.flag = 1;
 }
@@ -341,6 +346,7 @@ struct WeightArgs {
     float *part;     // [chunks + G][d_in][d_out]: chunk c's part of group g in record c + g (along the way both only grow)
     float *sums;     // [chunks + G][2 m_tiles][d_out]: sums of dz's columns, a share of the rows each, or null
     int *flag;
+    long long wait_limit;
     int n, G, d_in, d_out, nb;
     int cols;        // of a tile (a multiple of 64 up to 256)
     int m_tiles, n_tiles;
@@ -353,8 +359,8 @@ constexpr int kAdders = 8, kMakers = 8;   // warps; the adders' work is laid out
 constexpr int kWeightThreads = 64 + kAdders * 32, kWeightThreads8 = kWeightThreads + kMakers * 32;
 constexpr uint32_t kTurnBuf = 32 * 64;    // an adder's 32 rows of 16 sums on their way out
 struct WeightShared {
-    alignas(8) uint64_t full[kStagesMax], empty[kStagesMax], made[kStagesMax], acc_full[2], acc_empty[2];
-    uint32_t tmem;
+    alignas(8) uint64_t full[kStagesMax], empty[kStagesMax], made[kStagesMax], acc_full[2], acc_empty[2], done;
+    uint32_t tmem, filled;   // stages that copies were issued into
     int failed;
     GroupTable table;
 };
@@ -368,7 +374,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     const int panels = p.cols / 64;
     const uint32_t panel = p.step * 128, stage_bytes = (p.h_panels + panels) * panel, dz_at = p.h_panels * panel;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    volatile int *failed = &sh.failed;
+    const Waits waits{&sh.failed, p.wait_limit};
 
     group_table(sh.table, p.offsets, p.G, p.n);
     if (warp == 1) tmem_alloc(smem_addr(&sh.tmem));
@@ -376,6 +382,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
         // a stage is free when its products are done, and the adders have taken their sums of it
         for (int i = 0; i < p.stages; ++i) bar_init(smem_addr(&sh.full[i]), 1), bar_init(smem_addr(&sh.empty[i]), p.sums ? 1 + kAdders : 1), bar_init(smem_addr(&sh.made[i]), kMakers);
         for (int i = 0; i < 2; ++i) bar_init(smem_addr(&sh.acc_full[i]), 1), bar_init(smem_addr(&sh.acc_empty[i]), kAdders);
+        bar_init(smem_addr(&sh.done), 1);
         sh.failed = 0;
         bar_init_fence();
     }
@@ -428,7 +435,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
             if (!segment(g, lo, hi)) continue;
             for (int r = lo; r < hi; r += p.step, ++use, st.next(p.stages)) {
                 const uint32_t s = st.at, bar = smem_addr(&sh.full[s]), at = ring + s * stage_bytes;
-                ok = warp_wait(smem_addr(&sh.empty[s]), st.round ^ 1, failed);
+                ok = warp_wait(smem_addr(&sh.empty[s]), st.round ^ 1, waits);
                 if (!ok) break;
                 if (one_lane()) {
                     bar_expect(bar, ((CK ? 0 : h_panels) + panels) * panel);
@@ -439,8 +446,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                 __syncwarp();
             }
         }
-        if (!ok)
-            for (uint32_t s = 0; s < (uint32_t)p.stages && s < use; ++s) bar_drain(smem_addr(&sh.full[s]), ((use - 1 - s) / p.stages) & 1);
+        if (lane == 0) sh.filled = use;
     } else if (warp == 1) {
         const uint32_t instr = tc_instr((cols + 15) & ~15, true, true);
         RingPlace st, acc;
@@ -450,15 +456,15 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
             if (!segment(g, lo, hi)) continue;
             for (int r0 = lo; ok && r0 < hi; r0 += kRunRows, acc.next(bufs)) {
                 const uint32_t buf = acc.at;
-                ok = warp_wait(smem_addr(&sh.acc_empty[buf]), acc.round ^ 1, failed);
+                ok = warp_wait(smem_addr(&sh.acc_empty[buf]), acc.round ^ 1, waits);
                 if (!ok) break;
                 tc_after_sync();
                 const int r1 = min(hi, r0 + kRunRows);
                 for (int r = r0; r < r1; r += p.step, st.next(p.stages)) {
                     const uint32_t s = st.at, at = ring + s * stage_bytes;
                     const int rows = min(p.step, hi - r);
-                    ok = warp_wait(smem_addr(&sh.full[s]), st.round, failed);
-                    if (CK) ok = ok && warp_wait(smem_addr(&sh.made[s]), st.round, failed);
+                    ok = warp_wait(smem_addr(&sh.full[s]), st.round, waits);
+                    if (CK) ok = ok && warp_wait(smem_addr(&sh.made[s]), st.round, waits);
                     if (!ok) break;
                     if (!CK && rows % 16) {
                         clear(at, rows, 0, h_panels, lane, 32);
@@ -507,7 +513,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                     const int r1 = min(hi, r0 + kRunRows);
                     for (int r = r0; r < r1; r += p.step, st.next(p.stages)) {
                         // also where it is another block's turn: the arrival below belongs to this round of the stage
-                        ok = warp_wait(smem_addr(&sh.full[st.at]), st.round, failed);
+                        ok = warp_wait(smem_addr(&sh.full[st.at]), st.round, waits);
                         if (!ok) break;
                         if (want_sums && turn == m_tile) {
                             const uint32_t at = ring + st.at * stage_bytes + sum_at;
@@ -542,7 +548,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                     if (!ok) break;
                 }
                 const uint32_t buf = acc.at;
-                ok = warp_wait(smem_addr(&sh.acc_full[buf]), acc.round, failed);
+                ok = warp_wait(smem_addr(&sh.acc_full[buf]), acc.round, waits);
                 if (!ok) break;
                 tc_after_sync();
                 const bool first = r0 == lo, last = r0 + kRunRows >= hi;
@@ -655,7 +661,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                     if (r >= hi) break;
                     const uint32_t s = st.at, at = ring + s * stage_bytes;
                     const int rows = min(p.step, hi - r);
-                    ok = warp_wait(smem_addr(&sh.empty[s]), st.round ^ 1, failed);
+                    ok = warp_wait(smem_addr(&sh.empty[s]), st.round ^ 1, waits);
                     if (!ok) break;
                     if (h_cols) {
 #pragma unroll
@@ -668,7 +674,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
                     }
                     ask(code[d], scale[d], hi - r - kAhead * p.step);
                     if (rows % 16) {
-                        ok = warp_wait(smem_addr(&sh.full[s]), st.round, failed);
+                        ok = warp_wait(smem_addr(&sh.full[s]), st.round, waits);
                         if (!ok) break;
                         clear(at, rows, p.h_panels, p.h_panels + panels, me, kMakers * 32);   // h's rows are zeros already
                     }
@@ -684,6 +690,10 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     tc_before_sync();
     __syncthreads();
     tc_after_sync();
+    if (sh.failed) {
+        if (threadIdx.x == 0) drain_copies(sh.full, p.stages, sh.filled);
+        if (warp == 1) drain_products(&sh.done);
+    }
     if (warp == 1) tmem_free(tmem);
     if (threadIdx.x == 0 && sh.failed && p.flag) *p.flag = 1;
 }
@@ -817,6 +827,7 @@ static sar_status grouped_rows(int64_t n, int32_t groups, int K, int N, const in
     p.offsets = offsets;
     p.out = static_cast<__nv_bfloat16 *>(out);
     p.flag = flag;
+    p.wait_limit = g_wait_limit.load(std::memory_order_relaxed);
     p.n = (int)n;
     p.G = groups;
     p.K = K;
@@ -920,6 +931,7 @@ static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_
     p.part = static_cast<float *>(workspace);
     p.sums = beta ? reinterpret_cast<float *>(static_cast<char *>(workspace) + w.part_bytes) : nullptr;
     p.flag = flag;
+    p.wait_limit = g_wait_limit.load(std::memory_order_relaxed);
     p.n = (int)n;
     p.G = groups;
     p.d_in = d_in;
@@ -971,6 +983,8 @@ static sar_status grouped_weight(int64_t n, int32_t groups, int32_t d_in, int32_
 using namespace sar;
 
 extern "C" {
+
+int64_t sar_set_wait_limit(int64_t cycles) { return g_wait_limit.exchange(cycles < 0 ? kWaitCycles : cycles); }
 
 sar_status sar_linear_grouped(int64_t n, int32_t groups, int32_t d_in, int32_t d_out, sar_dtype t, const int64_t *offsets, const void *h,
                               const void *w, void *z, uint32_t flags, int32_t *flag, void *stream) {

@@ -21,31 +21,46 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// Waits until the phase of this parity is over.  A wait that lasts longer than kWaitCycles (seconds; a tile takes microseconds)
+__device__ __forceinline__ bool bar_over(uint32_t bar, uint32_t parity) {   // one look; bar_try may put the thread to sleep for a while
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.b32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Waits until the phase of this parity is over.  A wait that lasts longer than the limit (seconds; a tile takes microseconds)
 // gives up, and so do all waits of the block after it: *failed, in shared memory, is set, and the roles leave their loops.
+// With a limit of 0 a wait gives up that is not over at the first look.
 constexpr long long kWaitCycles = 4000000000ll;
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *failed) {
+struct Waits {
+    volatile int *failed;
+    long long limit;
+};
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const Waits &w) {
+    if (w.limit == 0) {
+        if (bar_over(bar, parity)) return true;
+        *w.failed = 1;
+        return false;
+    }
     if (bar_try(bar, parity)) return true;
     const long long t0 = clock64();
     for (;;) {
 #pragma unroll 1
         for (int i = 0; i < 64; ++i)
             if (bar_try(bar, parity)) return true;
-        if (*failed) return false;
-        if (clock64() - t0 > kWaitCycles) {
-            *failed = 1;
+        if (*w.failed) return false;
+        if (clock64() - t0 > w.limit) {
+            *w.failed = 1;
             return false;
         }
     }
 }
-// the same without regard to *failed: for the copies in flight of a block that has given up
+// the same without regard to *failed and the limit: for what a block that has given up still has in flight
 __device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
     const long long t0 = clock64();
     while (!bar_try(bar, parity) && clock64() - t0 < kWaitCycles) {
     }
 }
 // the same for all lanes of a warp together
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int *failed) { return __all_sync(0xffffffffu, bar_wait(bar, parity, failed)); }
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, const Waits &w) { return __all_sync(0xffffffffu, bar_wait(bar, parity, w)); }
 // One lane of a warp whose lanes are all here.  Copies and products take their operands from registers that a warp shares; behind a
 // test of the lane's number the compiler has to allow for several lanes with operands of their own, and goes over them one by one.
 __device__ __forceinline__ bool one_lane() {
@@ -105,6 +120,19 @@ __device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint3
 // the barrier gets an arrival when all products that this thread has issued are done
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(bar) : "memory");
+}
+// What a block that has given up still has in flight ends before the block does: the copies into `filled` buffers of a ring of `size`
+// (by any one thread), and the products of the thread that issued them (by its whole warp; `done`: a barrier of one arrival that
+// nothing else uses).  A role that has come to its end may have left copies or products behind that others have given up
+// waiting for, so this follows the last barrier of all roles.
+__device__ __forceinline__ void drain_copies(const uint64_t *full, uint32_t size, uint32_t filled) {
+    for (uint32_t s = 0; s < size && s < filled; ++s) bar_drain(smem_addr(&full[s]), ((filled - 1 - s) / size) & 1);
+}
+__device__ __forceinline__ void drain_products(uint64_t *done) {
+    if (one_lane()) tc_commit(smem_addr(done));
+    __syncwarp();
+    bar_drain(smem_addr(done), 0);
+    tc_after_sync();
 }
 // Columns of the warp's 32 lanes: thread l has columns at, at + 1, ... of lane l (the lanes that warp % 4 may reach).  The
 // registers of a load may be used after tmem_wait_load, through which they pass, so that no use of them is moved before it.
