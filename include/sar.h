@@ -652,8 +652,8 @@ SAR_API sar_status sar_ln_bwd_ckpt8(int64_t n, int32_t C, sar_dtype t, const int
  *                                  gamma, beta [d_in] float32 may be NULL (1 / 0): the weight gradient behind sar_ln_fwd_ckpt8.
  * Rows of no group (before offsets[0], from offsets[groups] on) take part in nothing; z and dh are left there as they were, or
  * written as zeros with flags = SAR_GROUPED_ZERO_REST.  Neither may overlap the rows or the weights (SAR_ERR_INVALID_ARG).
- * flag (DEVICE int, may be NULL) is set to 1 if a wait inside the kernel ran out of its limit, which leaves results unwritten;
- * the library's tests check that it stays 0.  A block that gives up ends only after its copies and products in flight.
+ * flag (DEVICE int, may be NULL) is set to 1 if a wait inside the kernel ran out of its limit.  A block that gives
+ * up ends only after its copies and products in flight, and all its results are NaN: rows of z and dh, tiles of dw.
  *   sar_set_wait_limit           the limit, in clock cycles, of each wait inside the launches of these four calls from now on (4e9
  *                                by default, about two seconds, which a negative value brings back); returns the one before.
  *                                With 0 a wait gives up that is not over at the first look.  Process-global; launches that

@@ -318,6 +318,14 @@ __global__ void __launch_bounds__(kRowsThreads, 1) grouped_rows_kernel(const __g
     if (sh.failed) {
         if (threadIdx.x == 0) drain_copies(sh.full, p.stages, sh.filled), drain_copies(sh.w_full, p.slots, sh.sets);
         if (warp == 1) drain_products(&sh.done);
+        // What is missing must not pass as a result: NaN in all of the block's tiles (the copies out have ended, the roles wait for them).
+        const int across = cols / 8;
+        for (int t = t0, g = g0; t < t1; ++t) {
+            while (t >= sh.table.tiles[g + 1]) ++g;
+            const int row = sh.table.first[g] + (t - sh.table.tiles[g]) * kTileRows, rows = min(kTileRows, sh.table.first[g + 1] - row);
+            for (int i = threadIdx.x; i < rows * across; i += kRowsThreads)
+                *reinterpret_cast<uint4 *>(p.out + (long long)(row + i / across) * p.N + n0 + i % across * 8) = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
+        }
     }
     if (warp == 1) tmem_free(tmem);
     if (threadIdx.x == 0 && sh.failed && p.flag) *p.flag = 1;
@@ -364,6 +372,20 @@ struct WeightShared {
     int failed;
     GroupTable table;
 };
+
+// NaN in the block's part of its records, and so in the sums over them.  A function of its own, called rarely: within the kernel it
+// keeps values over the roles' loops, which the 96 registers of the checkpoint's threads have no room for.
+__device__ __noinline__ void weight_gave_up(const WeightArgs &p, const GroupTable &table) {
+    const int tiles = p.m_tiles * p.n_tiles, chunk = blockIdx.x / tiles, tile = blockIdx.x % tiles;
+    const int m0 = tile / p.n_tiles * 128, n0 = tile % p.n_tiles * p.cols, across = min(p.cols, p.d_out - n0) / 4;
+    const long long chunk0 = (long long)chunk * p.chunk_rows, chunk1 = chunk0 + p.chunk_rows;
+    for (int g = 0; g < p.G; ++g) {
+        if (table.first[g] >= chunk1 || table.first[g + 1] <= chunk0 || table.first[g] == table.first[g + 1]) continue;
+        for (int i = threadIdx.x; i < min(128, p.d_in - m0) * across; i += blockDim.x)
+            *reinterpret_cast<uint4 *>(p.part + ((long long)(chunk + g) * p.d_in + m0 + i / across) * p.d_out + n0 + i % across * 4) =
+                make_uint4(0x7fffffffu, 0x7fffffffu, 0x7fffffffu, 0x7fffffffu);
+    }
+}
 
 template <bool CK>
 __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grouped_weight_kernel(const __grid_constant__ WeightArgs p) {
@@ -693,6 +715,7 @@ __global__ void __launch_bounds__(CK ? kWeightThreads8 : kWeightThreads, 1) grou
     if (sh.failed) {
         if (threadIdx.x == 0) drain_copies(sh.full, p.stages, sh.filled);
         if (warp == 1) drain_products(&sh.done);
+        weight_gave_up(p, sh.table);
     }
     if (warp == 1) tmem_free(tmem);
     if (threadIdx.x == 0 && sh.failed && p.flag) *p.flag = 1;

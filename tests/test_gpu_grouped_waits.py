@@ -60,3 +60,16 @@ def test_a_wait_that_runs_out_is_told_and_the_device_goes_on(sizes, d_in, d_out,
         out.fill_(float("nan"))
         call(flag)
         assert flag.item() == 0 and torch.equal(out, want)
+
+
+@pytest.mark.parametrize("sizes,d_in,d_out", SHAPES)
+def test_results_of_a_launch_that_gave_up_are_nan(sizes, d_in, d_out, no_patience):
+    """Whatever the arrays and the scratch held before: each value is NaN, or right where its block did not have to wait."""
+    for call, out in calls(sizes, d_in, d_out):
+        flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+        call(flag)
+        want = out.clone()
+        assert not want.isnan().any()
+        out.fill_(7.0)
+        no_patience(call, flag)
+        assert flag.item() == 1 and out.isnan().any() and (out.isnan() | (out == want)).all()
