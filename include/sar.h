@@ -66,7 +66,9 @@ typedef enum {
     SAR_ERR_ALIGNMENT = -3,   /* a pointer is not aligned to its element type               */
     SAR_ERR_WORKSPACE = -4,   /* workspace missing or smaller than *_workspace_bytes says   */
     SAR_ERR_CUDA = -5,        /* a CUDA runtime call or launch failed                       */
-    SAR_ERR_BAD_GRAPH = -6    /* sar_validate_part found an inconsistent graph              */
+    SAR_ERR_BAD_GRAPH = -6,   /* sar_validate_part found an inconsistent graph              */
+    SAR_ERR_WAIT = -7         /* a wait inside a kernel ran out of its limit: what the `flag` of sar_linear_grouped* says, for the
+                                 layers that read it; no call here returns it */
 } sar_status;
 
 typedef enum { SAR_F32 = 0, SAR_BF16 = 1 } sar_dtype;

@@ -505,6 +505,8 @@ def ln_backward(x: Optional[torch.Tensor], gy: torch.Tensor, saved, gamma: Optio
 
 # ----------------------------------------------------------------------------------------------
 # projection of nodes of several types: rows offsets[t] .. offsets[t+1] (int64, on the device) have type t and its matrix.
+# Should a wait inside one of these products run out (binding.sar_set_wait_limit), its results are NaN and the next of these calls
+# raises SarError (code SAR_ERR_WAIT), as CUDA reports what fails in a kernel.
 
 def typed_linear_forward(h: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, out: Optional[torch.Tensor] = None):
     """z[i] = h[i] W[type(i)]; h [n, d_in], W [types, d_in, d_out] (bf16).  Rows of no type (before offsets[0], from the last

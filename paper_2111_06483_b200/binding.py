@@ -18,6 +18,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libsar.so")
 
 SAR_OK = 0
+SAR_ERR_WAIT = -7
 SAR_F32, SAR_BF16 = 0, 1
 SAR_FIRST, SAR_LAST, SAR_MEAN, SAR_KEEP_NUMERATOR, SAR_RELU_OUT, SAR_SAME_WORKSPACE = 1, 2, 4, 8, 16, 32
 SAR_MAX_PARTS = 64

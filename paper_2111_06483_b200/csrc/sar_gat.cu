@@ -382,6 +382,7 @@ const char *sar_status_string(sar_status s) {
         case SAR_ERR_WORKSPACE: return "workspace missing or too small";
         case SAR_ERR_CUDA: return "CUDA error";
         case SAR_ERR_BAD_GRAPH: return "inconsistent graph";
+        case SAR_ERR_WAIT: return "a wait inside a kernel ran out of its limit, its results are NaN";
     }
     return "unknown status";
 }

@@ -551,6 +551,8 @@ PyObject *sage_forward(Args &a) {   // parts, bounds, h, W, W_res, inv
     return tuple(pre, agg);
 }
 
+int32_t *wait_flag();
+
 // The weight gradient's operand is the aggregate, or its checkpoint (codes and scales) where the forward call kept that.
 PyObject *sage_backward_of(Args &a, bool ckpt) {
     const auto parts = a.integers(), bounds = a.integers();
@@ -571,7 +573,7 @@ PyObject *sage_backward_of(Args &a, bool ckpt) {
     if (ckpt) {
         const at::Tensor gws = bytes(L.sar_linear_grouped_workspace_bytes(n, 1, d_in, d_out), h);
         SAR(sar_linear_grouped_bwd_weight_ckpt8, n, 1, d_in, d_out, t, nullptr, static_cast<const int8_t *>(ptr(agg)), static_cast<const uint8_t *>(ptr(scales)),
-            nullptr, nullptr, ptr(g), f32m(dW), nullptr, ptrm(gws), gws.nbytes(), stream());
+            nullptr, nullptr, ptr(g), f32m(dW), wait_flag(), ptrm(gws), gws.nbytes(), stream());
     } else {
         SAR(sar_linear_bwd_weight, n, d_in, d_out, t, ptr(agg), ptr(g), f32m(dW), ptrm(ws), ws.nbytes(), stream());
     }
@@ -640,6 +642,24 @@ struct Matrix {
     }
 };
 at::Tensor scales_for(int64_t n, int64_t C, const at::Tensor &like) { return empty({n, (C + SAR_CKPT8_BLOCK - 1) / SAR_CKPT8_BLOCK}, at::kByte, like); }
+// Where a wait inside a product by group ran out: a word of pinned host memory, which kernels on every device can write and the host
+// reads without waiting for them.  Like CUDA's own errors of running kernels it is reported by the next call.  It is there for as
+// long as the process: captured graphs hold its address.
+int32_t *wait_flag() {
+    static int32_t *flag = nullptr;
+    if (!flag) {
+        void *p = nullptr;
+        cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;   // the first call may be one that is being captured
+        (void)cudaThreadExchangeStreamCaptureMode(&mode);
+        const cudaError_t e = cudaHostAlloc(&p, sizeof(int32_t), cudaHostAllocPortable | cudaHostAllocMapped);
+        (void)cudaThreadExchangeStreamCaptureMode(&mode);
+        check("cudaHostAlloc", e == cudaSuccess ? SAR_OK : SAR_ERR_CUDA);
+        flag = static_cast<int32_t *>(p);
+        *flag = 0;
+    }
+    if (__atomic_exchange_n(flag, 0, __ATOMIC_RELAXED)) check("an earlier product by group", SAR_ERR_WAIT);
+    return flag;
+}
 int8_t *i8m(const at::Tensor &t) { return static_cast<int8_t *>(t.mutable_data_ptr()); }
 uint8_t *u8m(const at::Tensor &t) { return static_cast<uint8_t *>(t.mutable_data_ptr()); }
 const int8_t *i8(const at::Tensor &t) { return static_cast<const int8_t *>(t.const_data_ptr()); }
@@ -734,8 +754,8 @@ PyObject *typed_rows(Args &a, bool transposed) {   // rows, W, offsets, out or N
     } else {
         out = empty({m.n, N}, x.scalar_type(), x);
     }
-    if (transposed) SAR(sar_linear_grouped_bwd_input, m.n, (int32_t)T, (int32_t)N, m.C, m.t, po, ptr(x), ptr(W), ptrm(out), flags, nullptr, stream());
-    else SAR(sar_linear_grouped, m.n, (int32_t)T, m.C, (int32_t)N, m.t, po, ptr(x), ptr(W), ptrm(out), flags, nullptr, stream());
+    if (transposed) SAR(sar_linear_grouped_bwd_input, m.n, (int32_t)T, (int32_t)N, m.C, m.t, po, ptr(x), ptr(W), ptrm(out), flags, wait_flag(), stream());
+    else SAR(sar_linear_grouped, m.n, (int32_t)T, m.C, (int32_t)N, m.t, po, ptr(x), ptr(W), ptrm(out), flags, wait_flag(), stream());
     return wrap(out);
 }
 PyObject *typed_forward(Args &a) { return typed_rows(a, false); }
@@ -750,7 +770,7 @@ PyObject *typed_backward_weight(Args &a) {   // h, offsets, gz
     const int64_t T = o.numel() - 1;
     const int64_t *po = group_offsets(o, T);
     const at::Tensor dW = empty({T, m.C, z.C}, at::kFloat, h), ws = bytes(L.sar_linear_grouped_workspace_bytes(m.n, (int32_t)T, m.C, z.C), h);
-    SAR(sar_linear_grouped_bwd_weight, m.n, (int32_t)T, m.C, z.C, m.t, po, ptr(h), ptr(g), f32m(dW), nullptr, ptrm(ws), ws.nbytes(), stream());
+    SAR(sar_linear_grouped_bwd_weight, m.n, (int32_t)T, m.C, z.C, m.t, po, ptr(h), ptr(g), f32m(dW), wait_flag(), ptrm(ws), ws.nbytes(), stream());
     return wrap(dW);
 }
 
@@ -766,7 +786,7 @@ PyObject *typed_backward_weight_ckpt8(Args &a) {   // codes, scales, offsets, gz
     const float *pg = f32(gamma, C), *pb = f32(beta, C);
     const int64_t *po = group_offsets(o, T);
     const at::Tensor dW = empty({T, C, z.C}, at::kFloat, g), ws = bytes(L.sar_linear_grouped_workspace_bytes(z.n, (int32_t)T, (int32_t)C, z.C), g);
-    SAR(sar_linear_grouped_bwd_weight_ckpt8, z.n, (int32_t)T, (int32_t)C, z.C, z.t, po, i8(codes), u8(scales), pg, pb, ptr(g), f32m(dW), nullptr, ptrm(ws),
+    SAR(sar_linear_grouped_bwd_weight_ckpt8, z.n, (int32_t)T, (int32_t)C, z.C, z.t, po, i8(codes), u8(scales), pg, pb, ptr(g), f32m(dW), wait_flag(), ptrm(ws),
         ws.nbytes(), stream());
     return wrap(dW);
 }

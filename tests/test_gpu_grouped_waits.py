@@ -73,3 +73,40 @@ def test_results_of_a_launch_that_gave_up_are_nan(sizes, d_in, d_out, no_patienc
         out.fill_(7.0)
         no_patience(call, flag)
         assert flag.item() == 1 and out.isnan().any() and (out.isnan() | (out == want)).all()
+
+
+def test_the_next_call_of_the_api_reports_it(no_patience):
+    from paper_2111_06483_b200 import api, binding as B
+    n, d = 500, 64
+    h, W, dz, o = problem([200, 300], d, d)
+    c, square = api.ckpt8_pack(h), W[0].contiguous()
+    gen = torch.Generator().manual_seed(3)
+    g = api.Graph.from_coo(n, *(torch.randint(0, n, (4000,), generator=gen, dtype=torch.int32).cuda() for _ in range(2)))
+    _, saved = api.sage_layer_forward(g, h, square, square, checkpoint=True)
+    for call in (lambda: api.typed_linear_forward(h, W, o), lambda: api.typed_linear_backward_input(dz, W, o), lambda: api.typed_linear_backward_weight(h, o, dz),
+                 lambda: api.typed_linear_backward_weight(c, o, dz), lambda: api.sage_layer_backward(g, h, square, square, saved, dz)[1]):
+        want, got = call(), []
+        no_patience(lambda: got.append(call()))
+        assert got[0].isnan().any()
+        with pytest.raises(B.SarError) as e:
+            call()
+        assert e.value.code == B.SAR_ERR_WAIT
+        assert torch.equal(call(), want)   # reported once
+
+
+def test_a_replayed_graph_reports_it_to_the_next_call(no_patience):
+    from paper_2111_06483_b200 import api, binding as B
+    h, W, dz, o = problem([200, 300], 64, 64)
+    want = api.typed_linear_forward(h, W, o)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        no_wait_z = []
+        B.sar_set_wait_limit(0)
+        no_wait_z.append(api.typed_linear_forward(h, W, o))
+        B.sar_set_wait_limit(-1)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert no_wait_z[0].isnan().any()
+    with pytest.raises(B.SarError):
+        api.typed_linear_forward(h, W, o)
+    assert torch.equal(api.typed_linear_forward(h, W, o), want)
