@@ -854,8 +854,9 @@ def _holds(t: Optional[torch.Tensor], dtype: torch.dtype, n: int, what: str) -> 
 
 
 def _checkpoint_holds(codes: torch.Tensor, scales: torch.Tensor, n: int, C: int) -> None:
-    _holds(codes, torch.int8, n * C, "codes")
-    _holds(scales, torch.uint8, n * ((C + SAR_CKPT8_BLOCK - 1) // SAR_CKPT8_BLOCK), "scales")
+    # of exactly these shapes: rows of another width would be decoded with other rows' scales
+    for t, dtype, shape in ((codes, torch.int8, (n, C)), (scales, torch.uint8, (n, (C + SAR_CKPT8_BLOCK - 1) // SAR_CKPT8_BLOCK))):
+        assert t.dtype == dtype and tuple(t.shape) == shape, f"checkpoint: expected {dtype} of {shape}"
 
 
 def sar_ckpt8_pack(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor) -> None:

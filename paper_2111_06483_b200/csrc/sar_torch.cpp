@@ -131,9 +131,11 @@ void require_matrix(const at::Tensor &t, const at::Tensor &like, int64_t rows, i
     require(t.dim() == 2 && t.size(0) == rows && t.size(1) == cols, "a weight matrix of another shape");
     require(t.scalar_type() == like.scalar_type(), "tensors of one storage type expected");
 }
+// Of exactly these shapes: rows of another width would be decoded with other rows' scales.
 void require_checkpoint(const at::Tensor &codes, const at::Tensor &scales, int64_t n, int64_t C) {
-    require(codes.scalar_type() == at::kChar && codes.numel() >= n * C, "expected int8 codes, one per value");
-    require(scales.scalar_type() == at::kByte && scales.numel() >= n * ((C + SAR_CKPT8_BLOCK - 1) / SAR_CKPT8_BLOCK), "expected a uint8 scale per block");
+    require(codes.scalar_type() == at::kChar && codes.dim() == 2 && codes.size(0) == n && codes.size(1) == C, "expected int8 codes, one per value");
+    require(scales.scalar_type() == at::kByte && scales.dim() == 2 && scales.size(0) == n && scales.size(1) == (C + SAR_CKPT8_BLOCK - 1) / SAR_CKPT8_BLOCK,
+            "expected a uint8 scale per block of a row");
 }
 void require_rows(const at::Tensor &t, int64_t n) { require(t.dim() > 0 && t.size(0) >= n, "a node array has fewer rows than the graph"); }
 // ... of every piece of a graph: its destinations and its slice of the sources

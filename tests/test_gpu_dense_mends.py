@@ -1,0 +1,37 @@
+"""Calls of the layer normalisation, the 8-bit checkpoints and the products by group at the edges of what they take."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def test_codes_and_scales_of_different_shapes_are_refused():
+    """A checkpoint that was cut along one of its arrays: every row behind the first would be decoded with another row's scales."""
+    from paper_2111_06483_b200 import api, binding as B
+    n, C = 10, 64
+    x = torch.randn(n, C, device="cuda").bfloat16()
+    c, rstd = api.ckpt8_pack(x), torch.ones(n, device="cuda")
+    o = torch.tensor([0, n], device="cuda")
+    codes, narrow = c.codes[:, :32].contiguous(), x[:, :32].contiguous()
+    ws, dw = torch.empty(1 << 20, dtype=torch.uint8, device="cuda"), torch.empty(1, 32, C, device="cuda")
+    for scales in (c.scales, c.scales.view(-1), c.scales[:, :1].repeat(2, 1), c.scales[:, :1].contiguous().view(1, -1)):
+        cut = api.Checkpoint8(codes, scales)
+        for call in (lambda: api.ckpt8_unpack(cut), lambda: api.ln_backward(None, narrow, (cut, rstd)), lambda: api.typed_linear_backward_weight(cut, o, x),
+                     lambda: B.sar_ckpt8_unpack(codes, scales, narrow), lambda: B.sar_ln_bwd_ckpt8(codes, scales, rstd, None, narrow, narrow, None, None, None),
+                     lambda: B.sar_linear_grouped_bwd_weight_ckpt8(codes, scales, None, None, x, o, dw, ws)):
+            with pytest.raises(AssertionError):
+                call()
+    api.ckpt8_unpack(api.Checkpoint8(codes, c.scales[:, :1].contiguous()))
+
+
+def test_a_layer_refuses_a_checkpoint_of_another_width():
+    from paper_2111_06483_b200 import api
+    n, d = 60, 64
+    gen = torch.Generator().manual_seed(3)
+    g = api.Graph.from_coo(n, *(torch.randint(0, n, (400,), generator=gen, dtype=torch.int32).cuda() for _ in range(2)))
+    h, W = torch.randn(n, d, generator=gen).bfloat16().cuda(), torch.randn(d, d, generator=gen).bfloat16().cuda()
+    _, (c, inv) = api.sage_layer_forward(g, h, W, W, checkpoint=True)
+    for bad in (api.Checkpoint8(c.codes, torch.cat([c.scales, c.scales], 1)), api.Checkpoint8(torch.cat([c.codes, c.codes], 1), c.scales),
+                api.Checkpoint8(c.codes.view(n * 2, d // 2), c.scales.view(n * 2, -1))):
+        with pytest.raises(AssertionError):
+            api.sage_layer_backward(g, h, W, W, (bad, inv), h)
