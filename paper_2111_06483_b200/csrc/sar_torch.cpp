@@ -632,6 +632,11 @@ struct On {
         require(((!ts.defined() || ts.device() == x.device()) && ...), "tensors on one device expected");
     }
 };
+// A size that the library takes in 32 bits: cut off, it would be another size that the library accepts.
+int32_t size32(int64_t size) {
+    if (size > INT32_MAX) check("a size of 2^31 and more", SAR_ERR_UNSUPPORTED);
+    return (int32_t)size;
+}
 struct Matrix {
     int64_t n;
     int32_t C;
@@ -639,7 +644,7 @@ struct Matrix {
     explicit Matrix(const at::Tensor &x) {
         if (x.dim() != 2) fail(PyExc_ValueError, "expected [n, columns]");
         n = x.size(0);
-        C = (int32_t)x.size(1);
+        C = size32(x.size(1));
         t = code(x);
     }
 };
@@ -681,10 +686,11 @@ PyObject *ckpt8_unpack(Args &a) {   // codes, scales, bf16?
     const bool bf16 = a.flag();
     const On on(codes, scales);
     require(codes.dim() == 2, "expected codes [n, columns]");
-    const int64_t n = codes.size(0), C = codes.size(1);
+    const int64_t n = codes.size(0);
+    const int32_t C = size32(codes.size(1));
     require_checkpoint(codes, scales, n, C);
     const at::Tensor x = empty(codes.sizes(), bf16 ? at::kBFloat16 : at::kFloat, codes);
-    SAR(sar_ckpt8_unpack, n, (int32_t)C, bf16 ? SAR_BF16 : SAR_F32, i8(codes), u8(scales), ptrm(x), stream());
+    SAR(sar_ckpt8_unpack, n, C, bf16 ? SAR_BF16 : SAR_F32, i8(codes), u8(scales), ptrm(x), stream());
     return wrap(x);
 }
 
@@ -746,7 +752,7 @@ PyObject *typed_rows(Args &a, bool transposed) {   // rows, W, offsets, out or N
     const On on(x, W, o, out);
     const Matrix m(x);
     require(W.dim() == 3 && W.size(transposed ? 2 : 1) == m.C && W.scalar_type() == x.scalar_type(), "a weight matrix per type of the rows' width and type expected");
-    const int64_t T = W.size(0), N = W.size(transposed ? 1 : 2);
+    const int32_t T = size32(W.size(0)), N = size32(W.size(transposed ? 1 : 2));
     const int64_t *po = group_offsets(o, T);
     const unsigned flags = out.defined() ? 0u : SAR_GROUPED_ZERO_REST;
     if (out.defined()) {
@@ -756,8 +762,8 @@ PyObject *typed_rows(Args &a, bool transposed) {   // rows, W, offsets, out or N
     } else {
         out = empty({m.n, N}, x.scalar_type(), x);
     }
-    if (transposed) SAR(sar_linear_grouped_bwd_input, m.n, (int32_t)T, (int32_t)N, m.C, m.t, po, ptr(x), ptr(W), ptrm(out), flags, wait_flag(), stream());
-    else SAR(sar_linear_grouped, m.n, (int32_t)T, m.C, (int32_t)N, m.t, po, ptr(x), ptr(W), ptrm(out), flags, wait_flag(), stream());
+    if (transposed) SAR(sar_linear_grouped_bwd_input, m.n, T, N, m.C, m.t, po, ptr(x), ptr(W), ptrm(out), flags, wait_flag(), stream());
+    else SAR(sar_linear_grouped, m.n, T, m.C, N, m.t, po, ptr(x), ptr(W), ptrm(out), flags, wait_flag(), stream());
     return wrap(out);
 }
 PyObject *typed_forward(Args &a) { return typed_rows(a, false); }
@@ -769,10 +775,10 @@ PyObject *typed_backward_weight(Args &a) {   // h, offsets, gz
     const Matrix m(h), z(g);
     require(z.n == m.n && z.t == m.t, "gz of other rows or another type than h");
     require(o.numel() > 1, "expected int64 offsets, one more than matrices");
-    const int64_t T = o.numel() - 1;
+    const int32_t T = size32(o.numel() - 1);
     const int64_t *po = group_offsets(o, T);
-    const at::Tensor dW = empty({T, m.C, z.C}, at::kFloat, h), ws = bytes(L.sar_linear_grouped_workspace_bytes(m.n, (int32_t)T, m.C, z.C), h);
-    SAR(sar_linear_grouped_bwd_weight, m.n, (int32_t)T, m.C, z.C, m.t, po, ptr(h), ptr(g), f32m(dW), wait_flag(), ptrm(ws), ws.nbytes(), stream());
+    const at::Tensor dW = empty({T, m.C, z.C}, at::kFloat, h), ws = bytes(L.sar_linear_grouped_workspace_bytes(m.n, T, m.C, z.C), h);
+    SAR(sar_linear_grouped_bwd_weight, m.n, T, m.C, z.C, m.t, po, ptr(h), ptr(g), f32m(dW), wait_flag(), ptrm(ws), ws.nbytes(), stream());
     return wrap(dW);
 }
 
@@ -782,13 +788,13 @@ PyObject *typed_backward_weight_ckpt8(Args &a) {   // codes, scales, offsets, gz
     const On on(g, codes, scales, o, gamma, beta);
     const Matrix z(g);
     require(codes.dim() == 2 && codes.size(0) == z.n, "gz of other rows than the checkpoint");
-    const int64_t C = codes.size(1), T = o.numel() - 1;
+    const int32_t C = size32(codes.size(1)), T = size32(o.numel() - 1);
     require(o.numel() > 1, "expected int64 offsets, one more than matrices");
     require_checkpoint(codes, scales, z.n, C);
     const float *pg = f32(gamma, C), *pb = f32(beta, C);
     const int64_t *po = group_offsets(o, T);
-    const at::Tensor dW = empty({T, C, z.C}, at::kFloat, g), ws = bytes(L.sar_linear_grouped_workspace_bytes(z.n, (int32_t)T, (int32_t)C, z.C), g);
-    SAR(sar_linear_grouped_bwd_weight_ckpt8, z.n, (int32_t)T, (int32_t)C, z.C, z.t, po, i8(codes), u8(scales), pg, pb, ptr(g), f32m(dW), wait_flag(), ptrm(ws),
+    const at::Tensor dW = empty({T, C, z.C}, at::kFloat, g), ws = bytes(L.sar_linear_grouped_workspace_bytes(z.n, T, C, z.C), g);
+    SAR(sar_linear_grouped_bwd_weight_ckpt8, z.n, T, C, z.C, z.t, po, i8(codes), u8(scales), pg, pb, ptr(g), f32m(dW), wait_flag(), ptrm(ws),
         ws.nbytes(), stream());
     return wrap(dW);
 }

@@ -35,3 +35,21 @@ def test_a_layer_refuses_a_checkpoint_of_another_width():
                 api.Checkpoint8(c.codes.view(n * 2, d // 2), c.scales.view(n * 2, -1))):
         with pytest.raises(AssertionError):
             api.sage_layer_backward(g, h, W, W, (bad, inv), h)
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """2^32 + 64 columns are not 64.  Arrays without rows hold no memory, whatever their width."""
+    from paper_2111_06483_b200 import api, binding as B
+    C = 2 ** 32 + 64
+    def none(*shape, dtype=torch.bfloat16):
+        return torch.empty(0, *shape, dtype=dtype, device="cuda")
+    x, few, o = none(C), none(64), torch.zeros(2, dtype=torch.int64, device="cuda")
+    row = none(dtype=torch.float32)
+    c = api.Checkpoint8(none(C, dtype=torch.int8), none(C // 32, dtype=torch.uint8))
+    W = torch.empty(1, C, 0, dtype=torch.bfloat16, device="cuda")
+    for call in (lambda: api.ln_forward(x), lambda: api.ln_forward(x, checkpoint=True), lambda: api.ln_backward(x, x, (row, row)), lambda: api.ln_backward(None, x, (c, row)),
+                 lambda: api.ckpt8_pack(x), lambda: api.ckpt8_unpack(c), lambda: api.typed_linear_forward(x, W, o), lambda: api.typed_linear_forward(none(0), W.view(1, 0, C), o),
+                 lambda: api.typed_linear_backward_weight(x, o, few), lambda: api.typed_linear_backward_weight(few, o, x), lambda: api.typed_linear_backward_weight(c, o, few)):
+        with pytest.raises(B.SarError) as e:
+            call()
+        assert e.value.code == -2
