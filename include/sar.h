@@ -661,8 +661,8 @@ SAR_API sar_status sar_ln_bwd_ckpt8(int64_t n, int32_t C, sar_dtype t, const int
  *                                With 0 a wait gives up that is not over at the first look.  Process-global; launches that
  *                                a graph has captured keep theirs.  For tests and for GPUs shared with longer work.
  * Arrays are 16-byte aligned (codes 8), t must be SAR_BF16, d_in and d_out multiples of 8 up to 2^20, groups <= SAR_MAX_GROUPS,
- * n < 2^31 - 2048 (SAR_ERR_UNSUPPORTED otherwise).  Scratch of the weight calls: sar_linear_grouped_workspace_bytes.  n = 0 is
- * allowed (dw is then written as zeros).
+ * n < 2^31 - 2048 (SAR_ERR_UNSUPPORTED otherwise).  Scratch of the weight calls: sar_linear_grouped_workspace_bytes, which
+ * never falls as n grows (what suffices for n rows suffices for fewer).  n = 0 is allowed (dw is then written as zeros).
  * ------------------------------------------------------------------------------------------- */
 #define SAR_MAX_GROUPS 1024
 #define SAR_GROUPED_ZERO_REST 1u

@@ -911,6 +911,7 @@ static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out, bool c
     long long chunks = kSms / tiles;
     if (chunks > (n + kStep - 1) / kStep) chunks = (n + kStep - 1) / kStep;   // short chunks cost a record each, but small calls wait for steps: 2,000 rows, 256 x 256, chunks of 64, 128, 256 rows and more 29, 35, 42 us
     if (chunks < 1) chunks = 1;
+    const size_t records = (size_t)(chunks + groups);   // of the scratch: what follows can only take fewer, but not fewer for fewer rows
     long long rows = (n + chunks - 1) / chunks;
     rows = (rows + kStep - 1) / kStep * kStep;
     w.chunk_rows = (int)rows;
@@ -924,8 +925,8 @@ static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out, bool c
     w.stages = (int)((kSharedMost - fixed) / stage);
     w.stages = w.stages > kStagesMax ? kStagesMax : w.stages;
     w.smem = fixed + w.stages * stage;
-    w.part_bytes = sar_round_up((size_t)(w.chunks + groups) * d_in * d_out * 4, 256);
-    w.sum_bytes = sar_round_up((size_t)(w.chunks + groups) * 2 * w.m_tiles * d_out * 4, 256);
+    w.part_bytes = sar_round_up(records * d_in * d_out * 4, 256);
+    w.sum_bytes = sar_round_up(records * 2 * w.m_tiles * d_out * 4, 256);
     w.total_bytes = sar_round_up((size_t)groups * d_out * 4, 256);
     return w;
 }

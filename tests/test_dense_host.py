@@ -18,3 +18,12 @@ def test_the_wait_limit_is_told_back_and_a_negative_one_brings_the_default_back(
 
 def test_a_wait_that_ran_out_has_a_status_of_its_own():
     assert B.lib().sar_status_string(B.SAR_ERR_WAIT).startswith(b"a wait inside a kernel ran out")
+
+
+@pytest.mark.parametrize("groups,d_in,d_out", [(1, 256, 256), (8, 64, 64), (64, 136, 72), (3, 200, 120), (2, 520, 392), (1024, 8, 8)])
+def test_scratch_for_many_rows_suffices_for_fewer(groups, d_in, d_out):
+    """The rows are cut into chunks of whole steps, so one row more can mean half as many chunks (256 x 256: 74 of 64 rows for 4,736
+    rows, 38 of 128 for 4,737)."""
+    rows = [1, 63, 64, 65, *range(100, 20_000, 61), 4736, 4737, 9472, 9473, 10 ** 6, 10 ** 6 + 1, 2 * 10 ** 9]
+    size = [B.sar_linear_grouped_workspace_bytes(n, groups, d_in, d_out) for n in sorted(rows)]
+    assert size == sorted(size)

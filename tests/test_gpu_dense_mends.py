@@ -53,3 +53,17 @@ def test_sizes_beyond_32_bits_are_refused():
         with pytest.raises(B.SarError) as e:
             call()
         assert e.value.code == -2
+
+
+def test_scratch_of_more_rows_serves_fewer():
+    from paper_2111_06483_b200 import binding as B
+    d = 256
+    gen = torch.Generator().manual_seed(4)
+    h, dz = (torch.randn(4737, d, generator=gen).bfloat16().cuda() for _ in range(2))
+    ws = torch.empty(B.sar_linear_grouped_workspace_bytes(4737, 1, d, d), dtype=torch.uint8, device="cuda")
+    for n in (4737, 4736, 64, 1):
+        dw = torch.empty(1, d, d, device="cuda")
+        B.sar_linear_grouped_bwd_weight(h[:n], dz[:n], None, dw, ws)
+        want = h[:n].double().t() @ dz[:n].double()
+        size = h[:n].double().abs().t() @ dz[:n].double().abs()
+        assert ((dw[0].double() - want).abs() <= (34 * 2.0 ** -22 + 160 * 2.0 ** -24) * size + 1e-30).all()   # the bound of the products' own tests
