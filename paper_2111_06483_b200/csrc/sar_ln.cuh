@@ -21,7 +21,7 @@ __host__ __device__ constexpr int ln_copies(int C) {
 struct LnArgs {
     long long n;
     int C;
-    float inv_c, eps;
+    float c, inv_c, eps;          // C, 1 / C
     const void *x, *gy;
     void *y;                      // forward: y; backward: gx
     const float *gamma, *beta;    // [C] or null
@@ -49,9 +49,10 @@ struct LnLane {
 template <int G>
 static inline unsigned ln_grid(long long rows) { return (unsigned)((rows + LnLane<G>::kRows - 1) / LnLane<G>::kRows); }
 
-// Sums over a group's lanes.  Several warps' go by way of red[which]: two of them in turn, so that a sum costs one barrier.
+// Sums over a group's lanes.  Several warps' go by way of red[which], never the same for two sums in a row, so that a sum costs one
+// barrier.
 struct LnRed {
-    alignas(16) float2 red[2][kWarpsPerBlock];
+    alignas(16) float2 red[3][kWarpsPerBlock];
 };
 template <int G>
 __device__ __forceinline__ void ln_group_sync() {
@@ -435,11 +436,39 @@ constexpr int ln_blocks(bool bwd, bool ck) {
     return E == 8 ? (N <= 16 && !ck ? 3 : 2) : N <= 8 ? 3 : 2;
 }
 
+// A sum and its product with 1 / C round, so the mean is off by some units in its last place, which against a small spread is no small
+// error (a constant row of 12345.678 came out at 0.3).
+// bf16: values within a factor of two of each other are whole multiples of 2^-7 of the least, so the sum of up to 65,536 of them is
+// exact, and divided it gives the float32 next to the mean; values further apart have a spread that the sum's error is small against.
+// float32: the mean of the deviations says how much the mean is off, without cancellation.  Rows whose mean is more than 8 deviations
+// from zero take that sum and correct what they have: below that the mean's error is less than 2^-21 deviations for each
+// addition that a term passes, and the sum would cost every row (1,360,000 rows of 47, with the checkpoint 159 us, with the sum in
+// every row 170).
+// The quotient is one of two forms with the same bits: a division, or the product corrected by its remainder (which is exact, so that the
+// result before its rounding is within 2^-22 units of the quotient, and no quotient by C lies that close to the middle of two
+// floats).  The compiler keeps more in registers around the division; what that does to the passes, us, corrected / divided:
+// 60,000 rows of 5,000 308 / 255, with the checkpoint 481 / 390; 1,000,000 of 100 with it 160 / 140; but 120,000 of 2,048
+// (128 lanes) 177 / 196 and 31,000 of 2,047, column by column, 90 / 101.
+template <typename T, bool DIVIDE>
+__device__ __forceinline__ float ln_mean(float sum, const LnArgs &a) {
+    if constexpr (sizeof(T) == 2 && DIVIDE) return __fdiv_rn(sum, a.c);
+    const float mean = sum * a.inv_c;
+    if constexpr (sizeof(T) == 4) return mean;
+    const float left = fmaf(-mean, a.c, sum);
+    return fabsf(left) < 1.f + fabsf(mean) ? fmaf(left, a.inv_c, mean) : mean;   // an infinite mean stays
+}
+__device__ __forceinline__ bool ln_far(float mean, float var, float eps) { return mean * mean > 64.f * (var + eps); }
+__device__ __forceinline__ float ln_variance(float squares, float off) {   // from the means of the deviations and of their squares
+    const float v = fmaf(-off, off, squares);
+    return v < 0.f ? 0.f : v;   // NaN stays
+}
+
 // Rows are walked one ahead: a group asks for its next row before it works on the one it has (two sets of registers in turn),
 // so that loads are in flight all the time.
 template <typename Row, bool CK>
 __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(false, CK)) ln_fwd_kernel(const LnArgs a) {
     after_predecessor();
+    using T = typename Row::T;
     constexpr int G = Row::G, V = Row::V, P = Row::P;
     __shared__ LnRed red;
     const LnLane<G> id;
@@ -459,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(false, CK)) ln_fwd_ke
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int q = 0; q < P; ++q) sum = __fadd2_rn(sum, x[v][q]);   // what is no column is zero
-        const float mean = ln_sum<G>(sum.x + sum.y, red, 0) * a.inv_c;
+        float mean = ln_mean<T, (Row::E > 1 && (CK || G != 128))>(ln_sum<G>(sum.x + sum.y, red, 0), a);
         float2 dev = make_float2(0.f, 0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -469,7 +498,24 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(false, CK)) ln_fwd_ke
 #pragma unroll
             for (int q = 0; q < P; ++q) dev = __ffma2_rn(x[v][q], x[v][q], dev);
         }
-        const float rstd = __frsqrt_rn(fmaf(ln_sum<G>(dev.x + dev.y, red, 1), a.inv_c, a.eps));
+        float var = ln_sum<G>(dev.x + dev.y, red, 1) * a.inv_c;
+        if (sizeof(T) == 4 && __any_sync(0xffffffffu, ln_far(mean, var, a.eps))) {   // the sums need all lanes; a group's lanes agree, and so do its warps
+            float2 rest = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int q = 0; q < P; ++q) rest = __fadd2_rn(rest, x[v][q]);
+            const float off = ln_sum<G>(rest.x + rest.y, red, 2) * a.inv_c;
+            mean += off;
+            var = ln_variance(var, off);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+#pragma unroll
+                for (int q = 0; q < P; ++q) x[v][q] = __fadd2_rn(x[v][q], ln_splat(-off));
+                r.clean(v, x[v]);
+            }
+        }
+        const float rstd = __frsqrt_rn(var + a.eps);
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -708,7 +754,7 @@ __device__ __forceinline__ float ln_block_sum(float x, float *red) {   // red: k
 }
 
 template <typename T, bool CK>
-__global__ void __launch_bounds__(kThreads) ln_fwd_long_kernel(const LnArgs a) {
+__global__ void __launch_bounds__(kThreads, 8) ln_fwd_long_kernel(const LnArgs a) {
     after_predecessor();
     __shared__ float red[kWarpsPerBlock];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -716,20 +762,27 @@ __global__ void __launch_bounds__(kThreads) ln_fwd_long_kernel(const LnArgs a) {
         const long long o = row * a.C;
         float sum = 0.f;
         for (int c = threadIdx.x; c < a.C; c += kThreads) sum += ln_load<T>(a.x, o + c);
-        const float mean = ln_block_sum(sum, red) * a.inv_c;
+        const float first = ln_mean<T, true>(ln_block_sum(sum, red), a);
         float dev = 0.f;
         for (int c = threadIdx.x; c < a.C; c += kThreads) {
-            const float d = ln_load<T>(a.x, o + c) - mean;
+            const float d = ln_load<T>(a.x, o + c) - first;
             dev = fmaf(d, d, dev);
         }
-        const float rstd = __frsqrt_rn(fmaf(ln_block_sum(dev, red), a.inv_c, a.eps));
+        float var = ln_block_sum(dev, red) * a.inv_c, off = 0.f;
+        if (sizeof(T) == 4 && ln_far(first, var, a.eps)) {
+            float rest = 0.f;
+            for (int c = threadIdx.x; c < a.C; c += kThreads) rest += ln_load<T>(a.x, o + c) - first;
+            off = ln_block_sum(rest, red) * a.inv_c;
+            var = ln_variance(var, off);
+        }
+        const float rstd = __frsqrt_rn(var + a.eps);
         if (threadIdx.x == 0) {
-            if (a.mean) a.mean[row] = mean;
+            if (a.mean) a.mean[row] = first + off;
             if (a.rstd) a.rstd[row] = rstd;
         }
         for (int b = warp; b < a.nb; b += kWarpsPerBlock) {   // 32 columns a warp, the block of a checkpoint
             const int c = b * kCkptBlock + lane;
-            const float xh = c < a.C ? (ln_load<T>(a.x, o + c) - mean) * rstd : 0.f;
+            const float xh = c < a.C ? (ln_load<T>(a.x, o + c) - first - off) * rstd : 0.f;
             if constexpr (CK) {
                 float top = ckpt_top(xh, 0.f, 0.f);
 #pragma unroll
@@ -906,7 +959,8 @@ static inline LnArgs ln_args(int64_t n, int32_t C) {
     LnArgs a{};
     a.n = n;
     a.C = C;
-    a.inv_c = 1.f / (float)C;
+    a.c = (float)C;
+    a.inv_c = 1.f / a.c;
     a.nb = (int)ckpt_blocks(C);
     return a;
 }

@@ -1,6 +1,9 @@
 """Calls of the layer normalisation, the 8-bit checkpoints and the products by group at the edges of what they take."""
+import numpy as np
 import pytest
 import torch
+
+import oracle
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +70,47 @@ def test_scratch_of_more_rows_serves_fewer():
         want = h[:n].double().t() @ dz[:n].double()
         size = h[:n].double().abs().t() @ dz[:n].double().abs()
         assert ((dw[0].double() - want).abs() <= (34 * 2.0 ** -22 + 160 * 2.0 ** -24) * size + 1e-30).all()   # the bound of the products' own tests
+
+
+@pytest.mark.parametrize("c", [3, 4, 12, 47, 64, 72, 100, 127, 191, 256, 333, 500, 764, 1000, 1021, 1500, 2048, 3001, 8192, 9001])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("level,steps", [(1000.0, 0), (12345.678, 0), (-10000.0 - 1 / 3, 0), (1000.0, 1), (-7777.7, 3)])
+def test_rows_of_little_spread_about_a_high_level(c, dt, level, steps):
+    """Constant rows, and rows within a few units in the last place of a level: xhat and 1 / sigma from the mean itself, not from one
+    that was rounded.  u = 2^-24, w a unit in the last place of the level.
+    The mean first taken is off by e <= (k + 2) u |level| with k additions one after the other (k as in the normalisation's tests), and so
+    are the deviations from it, exactly (Sterbenz).  They are small multiples of w in float32, and their sums exact.  What is left: the
+    rounding of e, of the deviation times 1 / sigma and of 1 / sigma itself, whose variance is a difference of at most v + 2 e^2 to
+    (k + 6) u of that.  The stored mean is rounded once more.  bf16: the row's sum is exact (whole multiples of 2^-7 of the level, less
+    than 2^24 of them) and so is what the quotient is off, so the deviations are taken from the mean rounded to float32 after one more
+    addition: 2 u |mean|, nothing in a constant row, whose mean is a float32.  That adds its square to the variance.  bf16 results:
+    half a step."""
+    from paper_2111_06483_b200 import api
+    U, n, eps = 2.0 ** -24, 9, 1e-5
+    gen = torch.Generator().manual_seed(c)
+    x = torch.full((n, c), level, dtype=torch.float32).to(dt)
+    w = torch.tensor(torch.finfo(dt).eps * 2.0 ** np.floor(np.log2(abs(level))))
+    x = (x.double() + torch.randint(-steps, steps + 1, (n, c), generator=gen) * w.double()).to(dt)
+    X = x.double().numpy()
+    _, mean, rstd, xhat = oracle.ln_forward(X, eps)
+    x = x.cuda()
+    y, (got_mean, got_rstd) = api.ln_forward(x, eps)
+    k = (c + 3) // 4 + 16 if c <= 128 else max(64, c // 32 * 2) + 16
+    e = np.abs(X).max() * (k + 2) * U if dt == torch.float32 else np.abs(X).max() * 2 * U   # bf16: the sum is exact
+    var = 1.0 / rstd ** 2 - eps
+    rel = (k + 6) * U * (var + 2 * e * e) / (var + eps)
+    rel = rel / 2 + rel * rel + 3 * U
+    if dt == torch.bfloat16 and steps:
+        rel = rel + (2 * U * np.abs(mean) * rstd) ** 2
+    tol = 4 * U * (np.abs(xhat) + 2 * e * rstd[:, None]) + np.abs(xhat) * rel[:, None]
+    if dt == torch.bfloat16 and steps:
+        tol = tol + 2 * U * np.abs(mean)[:, None] * rstd[:, None]
+    half = 0.0 if dt == torch.float32 else 2.0 ** -8 * (np.abs(xhat) + tol)
+    assert (np.abs(got_mean.double().cpu().numpy() - mean) <= 2 * U * np.abs(mean) + 4 * U * e).all()
+    assert (np.abs(got_rstd.double().cpu().numpy() - rstd) <= (rel + 2 * U) * rstd).all()
+    assert (np.abs(y.double().cpu().numpy() - xhat) <= tol + half).all()
+    y8, (ck, rstd8) = api.ln_forward(x, eps, checkpoint=True)
+    assert torch.equal(y8, y) and torch.equal(rstd8, got_rstd)
+    if steps == 0:
+        v = api.ckpt8_unpack(ck, torch.float32).double().cpu().numpy()
+        assert (np.abs(v) <= 2 * tol).all()   # of blocks whose largest value is within tol of zero
