@@ -619,7 +619,8 @@ SAR_API sar_status sar_ckpt8_unpack(int64_t n, int32_t C, sar_dtype t, const int
  *   sar_ln_fwd_ckpt8   sar_ln_fwd that leaves the checkpoint of xhat as well (codes, scales as sar_ckpt8_pack would give
  *                      them for xhat in float32): with rstd all that the backward pass needs.
  *   sar_ln_bwd_ckpt8   sar_ln_bwd with xhat = what the checkpoint stands for (gx may be gy).
- * Scratch of the backward calls where dgamma or dbeta is asked for: sar_ln_workspace_bytes(C).  Sums over the rows are formed in
+ * Scratch of the backward calls where dgamma or dbeta is asked for: sar_ln_workspace_bytes_rows(n, C), which never falls as n grows,
+ * or sar_ln_workspace_bytes(C), enough for any n (1,184 records of 2 C floats, 148 beyond 8,192 columns).  Sums over the rows are formed in
  * a fixed order (no atomics), block partials are added in float64.  n = 0 is allowed (dgamma, dbeta are written as zeros).
  * Arrays aligned to 16 bytes (codes to 8) move 16 bytes at a time where C is a multiple of 8 (bf16) or 4, and whatever C from 128
  * to about 1,000; others work as well, column by column.  Rows are read once up to 8,192 columns (2,048 column by column) and again
@@ -628,6 +629,7 @@ SAR_API sar_status sar_ckpt8_unpack(int64_t n, int32_t C, sar_dtype t, const int
  * aligned to their type), SAR_ERR_WORKSPACE.
  * ------------------------------------------------------------------------------------------- */
 SAR_API size_t sar_ln_workspace_bytes(int32_t C);
+SAR_API size_t sar_ln_workspace_bytes_rows(int64_t n, int32_t C);
 SAR_API sar_status sar_ln_fwd(int64_t n, int32_t C, sar_dtype t, const void *x, const float *gamma, const float *beta, float eps,
                               void *y, float *mean, float *rstd, void *stream);
 SAR_API sar_status sar_ln_bwd(int64_t n, int32_t C, sar_dtype t, const void *x, const float *mean, const float *rstd,

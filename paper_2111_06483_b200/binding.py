@@ -42,7 +42,7 @@ EXPORTS = [
     "sar_bn_combine_sums", "sar_degree_order_workspace_bytes", "sar_degree_order", "sar_relabel", "sar_permute_rows", "sar_linear_project", "sar_linear_bwd_input_relu",
     "sar_graph_from_coo", "sar_plan_many_workspace_bytes", "sar_plan_count_many", "sar_plan_fill_many", "sar_gather_i64",
     "sar_propagate_workspace_bytes", "sar_propagate_workspace_bytes_at", "sar_propagate",
-    "sar_ln_workspace_bytes", "sar_ln_fwd", "sar_ln_bwd", "sar_ln_fwd_ckpt8", "sar_ln_bwd_ckpt8", "sar_ckpt8_pack", "sar_ckpt8_unpack",
+    "sar_ln_workspace_bytes", "sar_ln_workspace_bytes_rows", "sar_ln_fwd", "sar_ln_bwd", "sar_ln_fwd_ckpt8", "sar_ln_bwd_ckpt8", "sar_ckpt8_pack", "sar_ckpt8_unpack",
     "sar_linear_grouped_workspace_bytes", "sar_linear_grouped", "sar_linear_grouped_bwd_input", "sar_linear_grouped_bwd_weight",
     "sar_linear_grouped_bwd_weight_ckpt8", "sar_set_wait_limit",
 ]
@@ -89,7 +89,7 @@ def lib() -> ctypes.CDLL:
                      "sar_gat_stack_arena_bytes", "sar_gat_bwd_noalloc_limit", "sar_gat_project_workspace_bytes",
                      "sar_bn_workspace_bytes", "sar_linear_workspace_bytes", "sar_gat_storing_workspace_bytes",
                      "sar_degree_order_workspace_bytes", "sar_plan_many_workspace_bytes", "sar_propagate_workspace_bytes", "sar_propagate_workspace_bytes_at",
-                     "sar_ln_workspace_bytes", "sar_linear_grouped_workspace_bytes"):
+                     "sar_ln_workspace_bytes", "sar_ln_workspace_bytes_rows", "sar_linear_grouped_workspace_bytes"):
             getattr(L, name).restype = c_size_t
         L.sar_set_wait_limit.restype = c_int64
         _lib = L
@@ -877,6 +877,10 @@ def sar_ckpt8_unpack(codes: torch.Tensor, scales: torch.Tensor, x: torch.Tensor)
 
 def sar_ln_workspace_bytes(C: int) -> int:
     return int(lib().sar_ln_workspace_bytes(c_int32(C)))
+
+
+def sar_ln_workspace_bytes_rows(n: int, C: int) -> int:
+    return int(lib().sar_ln_workspace_bytes_rows(c_int64(n), c_int32(C)))
 
 
 def sar_ln_fwd(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float, y: torch.Tensor,

@@ -13,7 +13,7 @@ namespace sar {
 
 static sar_status ln_check(int32_t C, sar_dtype t) {
     if (t != SAR_F32 && t != SAR_BF16) return SAR_ERR_INVALID_ARG;
-    return C > (1 << 20) ? SAR_ERR_UNSUPPORTED : SAR_OK;
+    return C > kLnMostColumns ? SAR_ERR_UNSUPPORTED : SAR_OK;
 }
 
 static sar_status ln_zero(int32_t C, float *dgamma, float *dbeta, cudaStream_t st) {
@@ -28,10 +28,11 @@ using namespace sar;
 
 extern "C" {
 
-size_t sar_ln_workspace_bytes(int32_t C) {
-    if (C < 1) return 0;
-    return (size_t)kLnBlocks * 2 * C * 4 + 256;
+size_t sar_ln_workspace_bytes_rows(int64_t n, int32_t C) {
+    if (n < 0 || C < 1 || C > kLnMostColumns) return 0;
+    return (size_t)ln_records_most(n, C) * 2 * C * 4 + 256;
 }
+size_t sar_ln_workspace_bytes(int32_t C) { return sar_ln_workspace_bytes_rows(INT64_MAX, C); }
 
 static sar_status ln_fwd_entry(int64_t n, int32_t C, sar_dtype t, const void *x, const float *gamma, const float *beta, float eps, void *y,
                                float *mean, float *rstd, int8_t *codes, uint8_t *scales, bool ckpt, void *stream) {
@@ -86,7 +87,7 @@ static sar_status ln_bwd_entry(int64_t n, int32_t C, sar_dtype t, const void *x,
     a.scales = const_cast<uint8_t *>(scales);
     const bool sums = dgamma || dbeta;
     if (sums) {
-        if (!workspace || !sar_aligned(workspace, 16) || workspace_bytes < (size_t)kLnBlocks * 2 * C * 4) return SAR_ERR_WORKSPACE;
+        if (!workspace || !sar_aligned(workspace, 16) || workspace_bytes < (size_t)ln_records_most(n, C) * 2 * C * 4) return SAR_ERR_WORKSPACE;
         a.partial = static_cast<float *>(workspace);
     }
     unsigned records = 0;

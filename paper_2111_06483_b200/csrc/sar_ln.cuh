@@ -965,6 +965,17 @@ static inline LnArgs ln_args(int64_t n, int32_t C) {
     return a;
 }
 
+constexpr int kLnMostColumns = 1 << 20;
+constexpr int kLnBlockColumns = 8192;   // that the registers of a block hold at most
+// Records of the weights' sums that the backward pass writes at most for n rows.  Blocks take two rows at least; rows longer than a
+// block's registers are cut into slices of 64 rows and more (ln_slices), so that 2^20 columns take 1.2 GB for many rows, not 10.
+static inline int ln_slices(long long n) { return (int)((n - 1) / 64 + 1 < kSms ? (n - 1) / 64 + 1 : kSms); }
+static inline int ln_records_most(long long n, int32_t C) {
+    if (n < 1) return 0;
+    if (C > kLnBlockColumns) return ln_slices(n);
+    return (int)((n - 1) / 2 + 1 < kLnBlocks ? (n - 1) / 2 + 1 : kLnBlocks);
+}
+
 // blocks of a kernel that run at once: each walks its rows (a constant of the kernel and the device)
 template <typename K>
 static unsigned ln_resident(K kernel, size_t smem) {
@@ -995,7 +1006,7 @@ static sar_status ln_backward_of(const LnShape &s, const LnArgs &a, unsigned *re
     const char *name = CK ? "ln_bwd_ckpt8" : "ln_bwd";
     if (s.E == 0) {
         // the sums first: gx may be written over gy or x
-        const int slices = (int)((a.n + 63) / 64 < kSms ? (a.n + 63) / 64 : kSms);
+        const int slices = ln_slices(a.n);
         if (a.partial) {
             SAR_LAUNCH("ln_bwd_sums", st, launch_if(a.n * a.C <= kOverlapElems, ln_long_sums_kernel<T, CK>, (unsigned)(((long long)slices * a.C + kThreads - 1) / kThreads), kThreads, 0, st, a, slices));
             SAR_TRY(sar_after_launch());

@@ -27,3 +27,17 @@ def test_scratch_for_many_rows_suffices_for_fewer(groups, d_in, d_out):
     rows = [1, 63, 64, 65, *range(100, 20_000, 61), 4736, 4737, 9472, 9473, 10 ** 6, 10 ** 6 + 1, 2 * 10 ** 9]
     size = [B.sar_linear_grouped_workspace_bytes(n, groups, d_in, d_out) for n in sorted(rows)]
     assert size == sorted(size)
+
+
+def test_scratch_of_the_normalisation_follows_the_records():
+    record = 2 * 4
+    for C in (1, 47, 64, 1000, 8192, 8193, 1 << 20):
+        size = [B.sar_ln_workspace_bytes_rows(n, C) for n in (0, 1, 2, 3, 64, 65, 300, 5000, 10 ** 6, 2 ** 40)]
+        assert size == sorted(size) and size[-1] <= B.sar_ln_workspace_bytes(C)
+        assert size[1] >= record * C
+    assert B.sar_ln_workspace_bytes_rows(300, 1000) < 160 * record * 1000
+    assert B.sar_ln_workspace_bytes_rows(300, 1 << 20) < 6 * record * (1 << 20)
+    assert B.sar_ln_workspace_bytes(1 << 20) < 150 * record * (1 << 20)
+    for n, C in ((-1, 64), (5, 0), (5, (1 << 20) + 1)):
+        assert B.sar_ln_workspace_bytes_rows(n, C) == 0
+    assert B.sar_ln_workspace_bytes((1 << 20) + 1) == 0   # which the calls refuse

@@ -114,3 +114,39 @@ def test_rows_of_little_spread_about_a_high_level(c, dt, level, steps):
     if steps == 0:
         v = api.ckpt8_unpack(ck, torch.float32).double().cpu().numpy()
         assert (np.abs(v) <= 2 * tol).all()   # of blocks whose largest value is within tol of zero
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("c", [1, 47, 64, 333, 1024, 1027, 2048, 4095, 8192, 8193])
+@pytest.mark.parametrize("n", [1, 3, 65, 9473])
+def test_the_scratch_for_these_rows_is_enough(n, c, dt):
+    """The backward passes write no byte behind it, and give what they give with more."""
+    from paper_2111_06483_b200 import api, binding as B
+    gen = torch.Generator().manual_seed(n + c)
+    x, gy = (torch.randn(n, c, generator=gen).to(dt).cuda() for _ in range(2))
+    gamma = torch.randn(c, generator=gen).cuda()
+    _, (mean, rstd) = api.ln_forward(x)
+    _, (ck, _) = api.ln_forward(x, checkpoint=True)
+    size, most = B.sar_ln_workspace_bytes_rows(n, c), B.sar_ln_workspace_bytes(c)
+    assert size <= most
+    for backward in (lambda gx, dg, db, ws: B.sar_ln_bwd(x, mean, rstd, gamma, gy, gx, dg, db, ws),
+                     lambda gx, dg, db, ws: B.sar_ln_bwd_ckpt8(ck.codes, ck.scales, rstd, gamma, gy, gx, dg, db, ws)):
+        got = []
+        for room in (size, most):
+            buffer = torch.full((room + 4096,), 0xAB, dtype=torch.uint8, device="cuda")
+            out = [torch.empty_like(x), torch.empty(c, device="cuda"), torch.empty(c, device="cuda")]
+            backward(*out, buffer[:room])
+            assert (buffer[room:] == 0xAB).all()
+            got.append(out)
+        assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_a_backward_pass_over_few_wide_rows_takes_little_memory():
+    from paper_2111_06483_b200 import api
+    x = torch.randn(2, 1 << 20, device="cuda")
+    _, saved = api.ln_forward(x)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    api.ln_backward(x, x, saved)
+    assert torch.cuda.max_memory_allocated() - before < 64 << 20   # gx, dgamma, dbeta and one record: 24 MB
