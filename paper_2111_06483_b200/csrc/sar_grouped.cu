@@ -931,12 +931,16 @@ static WeightPlan weight_plan(int64_t n, int groups, int d_in, int d_out, bool c
     return w;
 }
 
-// A tile is twice as wide as it is high, so dW^T = dz^T h can take fewer of them, and rows are read once a tile and chunk.  That pays
-// where no rows are whole lines of 128 bytes: a panel's row is then two requests to L2, which is what bounds such widths (300,000
-// rows, us, as they lie and turned: 136 x 72 50 / 39, 264 x 40 62 / 57, 456 x 72 90 / 78, 200 x 120 52 / 58; but 256 x 64 42 / 48,
-// 256 x 72 47 / 51).  Rows of a checkpoint are always the first operand, which the makers write.
+// A tile is twice as wide as it is high, so dW^T = dz^T h can take fewer of them, and dz is read once a tile of h's columns.  It pays where
+// that reading is dear, dz's rows ending in half a sector of 32 bytes, but dz is narrow, and where there are rows enough for what the
+// records cost, which are written to dW across its rows.  us, as they lie and turned: 300,000 rows of one group 136 x 72 50 / 39,
+// 168 x 24 45 / 38, 264 x 40 61 / 56, 456 x 72 88 / 72; of 64 groups 56 / 48, 45 / 45, 67 / 68, 103 / 97; a million of
+// 64 groups 456 x 104 294 / 218.  Not so whole sectors (200 x 48 39 / 39, 200 x 112 of 200,000 rows 36 / 39), wide dz (200 x 120 51 / 51, with 64
+// groups 60 / 69; 160 x 120 40 / 45), h in whole lines (256 x 72 45 / 47), few rows (20,000 of 4 groups 136 x 72 13 / 14,
+// 456 x 72 17 / 25) and many groups (100,000 rows of 64 200 x 72 29 / 35; of 8, 12,500 each, between 25 / 23 and 29 / 33).  Rows of a
+// checkpoint are always the first operand, which the makers write.
 static bool weight_turned(int64_t n, int groups, int d_in, int d_out) {
-    if (d_in % 64 == 0 || d_out % 64 == 0) return false;
+    if (d_in % 64 == 0 || d_out % 16 == 0 || d_out > 104 || n < 50000 || n < 2048ll * groups) return false;
     const WeightPlan a = weight_plan(n, groups, d_in, d_out, false), b = weight_plan(n, groups, d_out, d_in, false);
     return b.m_tiles * b.n_tiles < a.m_tiles * a.n_tiles;
 }

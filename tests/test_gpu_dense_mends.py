@@ -150,3 +150,22 @@ def test_a_backward_pass_over_few_wide_rows_takes_little_memory():
     before = torch.cuda.memory_allocated()
     api.ln_backward(x, x, saved)
     assert torch.cuda.max_memory_allocated() - before < 64 << 20   # gx, dgamma, dbeta and one record: 24 MB
+
+
+@pytest.mark.parametrize("d_in,d_out", [(136, 8), (136, 72), (264, 40), (456, 104), (1032, 24), (200, 120), (256, 72), (200, 48)])
+@pytest.mark.parametrize("sizes", [[50_000], [20_001, 0, 1, 39_000, 65], [2500] * 24])
+def test_weight_gradients_of_many_rows_taken_turned_or_not(sizes, d_in, d_out):
+    """Widths whose transposed gradient takes fewer tiles, on either side of the rule, with rows of no group around them that hold NaN.
+    The bound is that of the products by group: 34 additions by truncation, 2^-22, and the joined runs and chunks, 2^-24 each."""
+    from paper_2111_06483_b200 import api
+    gen = torch.Generator(device="cuda").manual_seed(d_in + len(sizes))
+    n, before = sum(sizes) + 40, 7
+    h, dz = (torch.randn(n, d, generator=gen, device="cuda").bfloat16() for d in (d_in, d_out))
+    edges = (before + np.cumsum([0] + sizes)).tolist()
+    for t in (h, dz):
+        t[:before], t[edges[-1]:] = float("nan"), float("inf")
+    dw = api.typed_linear_backward_weight(h, torch.tensor(edges, device="cuda"), dz)
+    for g, (a, b) in enumerate(zip(edges, edges[1:])):
+        x, y = h[a:b].double(), dz[a:b].double()
+        size = x.abs().t() @ y.abs()
+        assert ((dw[g].double() - x.t() @ y).abs() <= (34 * 2.0 ** -22 + (n // 512 + 160) * 2.0 ** -24) * size).all()
