@@ -619,6 +619,9 @@ SAR_API sar_status sar_ckpt8_unpack(int64_t n, int32_t C, sar_dtype t, const int
  *   sar_ln_fwd_ckpt8   sar_ln_fwd that leaves the checkpoint of xhat as well (codes, scales as sar_ckpt8_pack would give
  *                      them for xhat in float32): with rstd all that the backward pass needs.
  *   sar_ln_bwd_ckpt8   sar_ln_bwd with xhat = what the checkpoint stands for (gx may be gy).
+ *   sar_ln_bwd_grouped, sar_ln_bwd_ckpt8_grouped   the same over the rows of some group of sar_linear_grouped (offsets: DEVICE,
+ *                      [groups + 1], read as there): what other rows hold, NaN and infinities too, reaches nothing, and their gx is
+ *                      zero.  The backward pass of a normalisation that feeds sar_linear_grouped.
  * Scratch of the backward calls where dgamma or dbeta is asked for: sar_ln_workspace_bytes_rows(n, C), which never falls as n grows,
  * or sar_ln_workspace_bytes(C), enough for any n (1,184 records of 2 C floats, 148 beyond 8,192 columns).  Sums over the rows are formed in
  * a fixed order (no atomics), block partials are added in float64.  n = 0 is allowed (dgamma, dbeta are written as zeros).
@@ -640,6 +643,13 @@ SAR_API sar_status sar_ln_fwd_ckpt8(int64_t n, int32_t C, sar_dtype t, const voi
 SAR_API sar_status sar_ln_bwd_ckpt8(int64_t n, int32_t C, sar_dtype t, const int8_t *codes, const uint8_t *scales, const float *rstd,
                                     const float *gamma, const void *gy, void *gx, float *dgamma, float *dbeta, void *workspace,
                                     size_t workspace_bytes, void *stream);
+
+SAR_API sar_status sar_ln_bwd_grouped(int64_t n, int32_t groups, int32_t C, sar_dtype t, const int64_t *offsets, const void *x,
+                                      const float *mean, const float *rstd, const float *gamma, const void *gy, void *gx, float *dgamma,
+                                      float *dbeta, void *workspace, size_t workspace_bytes, void *stream);
+SAR_API sar_status sar_ln_bwd_ckpt8_grouped(int64_t n, int32_t groups, int32_t C, sar_dtype t, const int64_t *offsets, const int8_t *codes,
+                                            const uint8_t *scales, const float *rstd, const float *gamma, const void *gy, void *gx,
+                                            float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------------------------
  * The projection of nodes of several types, one weight matrix for each (Appendix A's W_r with the relation's rows lying

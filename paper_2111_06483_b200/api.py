@@ -495,12 +495,14 @@ def ln_forward(x: torch.Tensor, eps: float = 1e-5, gamma: Optional[torch.Tensor]
     return y, (Checkpoint8(*saved[:2]), saved[2]) if checkpoint else tuple(saved)
 
 
-def ln_backward(x: Optional[torch.Tensor], gy: torch.Tensor, saved, gamma: Optional[torch.Tensor] = None):
-    """Returns (gx, dgamma, dbeta); x may be None where saved holds a checkpoint."""
+def ln_backward(x: Optional[torch.Tensor], gy: torch.Tensor, saved, gamma: Optional[torch.Tensor] = None,
+                offsets: Optional[torch.Tensor] = None):
+    """Returns (gx, dgamma, dbeta); x may be None where saved holds a checkpoint.  With offsets (as in typed_linear_forward) the rows
+    of no type take part in nothing, whatever they hold, and their gx is zero."""
     first, rstd = saved
     if isinstance(first, Checkpoint8):
-        return B.native().ln_backward_ckpt8(first.codes, first.scales, gy, rstd, gamma)
-    return B.native().ln_backward(x, gy, first, rstd, gamma)
+        return B.native().ln_backward_ckpt8(first.codes, first.scales, gy, rstd, gamma, offsets)
+    return B.native().ln_backward(x, gy, first, rstd, gamma, offsets)
 
 
 # ----------------------------------------------------------------------------------------------
@@ -538,7 +540,9 @@ def typed_linear_backward(h, W: torch.Tensor, offsets: torch.Tensor, gz: torch.T
 def typed_layer_forward(x: torch.Tensor, W: torch.Tensor, offsets: torch.Tensor, gamma: Optional[torch.Tensor] = None,
                         beta: Optional[torch.Tensor] = None, eps: float = 1e-5, checkpoint: bool = True):
     """z = LN(x) W[type]: the normalised projection that feeds an aggregation over nodes of several types.  Returns (z, saved);
-    with checkpoint=True saved is 1.03 bytes a value and a float a row, otherwise x and LN(x) are kept."""
+    with checkpoint=True saved is 1.03 bytes a value and a float a row, otherwise x and LN(x) are kept.  Gradients from a checkpoint
+    are those of rows within a 64th of their block's largest (pass checkpoint=False for exact ones).  Rows of no type take part in
+    nothing, whatever they hold: z and gx are zero there."""
     y, saved = ln_forward(x, eps, gamma, beta, checkpoint)
     z = typed_linear_forward(y, W, offsets)
     return z, saved if checkpoint else (x, y, *saved)
@@ -550,11 +554,11 @@ def typed_layer_backward(W: torch.Tensor, offsets: torch.Tensor, saved, gz: torc
     gy = typed_linear_backward_input(gz, W, offsets)
     if isinstance(saved[0], Checkpoint8):
         dW = typed_linear_backward_weight(saved[0], offsets, gz, gamma, beta)
-        gx, dgamma, dbeta = ln_backward(None, gy, saved, gamma)
+        gx, dgamma, dbeta = ln_backward(None, gy, saved, gamma, offsets)
     else:
         x, y, mean, rstd = saved
         dW = typed_linear_backward_weight(y, offsets, gz)
-        gx, dgamma, dbeta = ln_backward(x, gy, (mean, rstd), gamma)
+        gx, dgamma, dbeta = ln_backward(x, gy, (mean, rstd), gamma, offsets)
     return gx, dW, dgamma, dbeta
 
 

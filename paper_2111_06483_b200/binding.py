@@ -44,7 +44,7 @@ EXPORTS = [
     "sar_propagate_workspace_bytes", "sar_propagate_workspace_bytes_at", "sar_propagate",
     "sar_ln_workspace_bytes", "sar_ln_workspace_bytes_rows", "sar_ln_fwd", "sar_ln_bwd", "sar_ln_fwd_ckpt8", "sar_ln_bwd_ckpt8", "sar_ckpt8_pack", "sar_ckpt8_unpack",
     "sar_linear_grouped_workspace_bytes", "sar_linear_grouped", "sar_linear_grouped_bwd_input", "sar_linear_grouped_bwd_weight",
-    "sar_linear_grouped_bwd_weight_ckpt8", "sar_set_wait_limit",
+    "sar_linear_grouped_bwd_weight_ckpt8", "sar_set_wait_limit", "sar_ln_bwd_grouped", "sar_ln_bwd_ckpt8_grouped",
 ]
 
 
@@ -934,6 +934,41 @@ def sar_ln_bwd_ckpt8(codes: torch.Tensor, scales: torch.Tensor, rstd: torch.Tens
     _check("sar_ln_bwd_ckpt8", lib().sar_ln_bwd_ckpt8(c_int64(n), c_int32(C), ctypes.c_int(_dtype(gy)), _ptr(codes),
                                                       _ptr(scales), _ptr(rstd), _ptr(gamma), _ptr(gy), _ptr(gx), _ptr(dgamma),
                                                       _ptr(dbeta), w, wb, _stream()))
+
+
+def sar_ln_bwd_grouped(x: torch.Tensor, offsets: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma: Optional[torch.Tensor],
+                       gy: torch.Tensor, gx: torch.Tensor, dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor],
+                       workspace: Optional[torch.Tensor]) -> None:
+    """sar_ln_bwd over rows offsets[0] .. offsets[-1]; the others' gx is zero."""
+    n, C = x.shape
+    groups = offsets.numel() - 1
+    _here(x, offsets, mean, rstd, gamma, gy, gx, dgamma, dbeta, workspace)
+    _group_offsets(offsets, groups)
+    for t in (gy, gx):
+        _holds(t, x.dtype, n * C, "gy, gx")
+    for t, k in ((mean, n), (rstd, n), (gamma, C), (dgamma, C), (dbeta, C)):
+        _holds(t, torch.float32, k, "mean, rstd, gamma, dgamma, dbeta")
+    w, wb = _ws(workspace)
+    _check("sar_ln_bwd_grouped", lib().sar_ln_bwd_grouped(
+        c_int64(n), c_int32(groups), c_int32(C), ctypes.c_int(_dtype(x)), _ptr(offsets), _ptr(x), _ptr(mean), _ptr(rstd), _ptr(gamma),
+        _ptr(gy), _ptr(gx), _ptr(dgamma), _ptr(dbeta), w, wb, _stream()))
+
+
+def sar_ln_bwd_ckpt8_grouped(codes: torch.Tensor, scales: torch.Tensor, offsets: torch.Tensor, rstd: torch.Tensor,
+                             gamma: Optional[torch.Tensor], gy: torch.Tensor, gx: torch.Tensor, dgamma: Optional[torch.Tensor],
+                             dbeta: Optional[torch.Tensor], workspace: Optional[torch.Tensor]) -> None:
+    n, C = gy.shape
+    groups = offsets.numel() - 1
+    _here(codes, scales, offsets, rstd, gamma, gy, gx, dgamma, dbeta, workspace)
+    _group_offsets(offsets, groups)
+    _holds(gx, gy.dtype, n * C, "gx")
+    for t, k in ((rstd, n), (gamma, C), (dgamma, C), (dbeta, C)):
+        _holds(t, torch.float32, k, "rstd, gamma, dgamma, dbeta")
+    _checkpoint_holds(codes, scales, n, C)
+    w, wb = _ws(workspace)
+    _check("sar_ln_bwd_ckpt8_grouped", lib().sar_ln_bwd_ckpt8_grouped(
+        c_int64(n), c_int32(groups), c_int32(C), ctypes.c_int(_dtype(gy)), _ptr(offsets), _ptr(codes), _ptr(scales), _ptr(rstd), _ptr(gamma),
+        _ptr(gy), _ptr(gx), _ptr(dgamma), _ptr(dbeta), w, wb, _stream()))
 
 
 def sar_linear_grouped_workspace_bytes(n: int, groups: int, d_in: int, d_out: int) -> int:

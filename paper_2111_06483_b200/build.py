@@ -23,7 +23,7 @@ TORCH_EXT = os.path.join(PKG, "_sar_torch.so")
 ROW_PASSES = ["fwd", "fwd_part", "dst", "dst_part", "src", "sum"]   # one translation unit per pass and storage type
 SOURCES = ["sar_linear.cu"] + [f"sar_lean_{p}_{t}.cu" for p in ("fwd", "bwd_dst", "bwd_src") for t in ("f32", "bf16")] + [f"sar_rows_{p}_{t}.cu" for p in ROW_PASSES for t in ("f32", "bf16")] + [
     "sar_gat.cu", "sar_span.cu", "sar_rows_merge.cu", "sar_graph.cu", "sar_host.cu", "sar_noalloc.cu", "sar_storing.cu",
-    "sar_glue.cu", "sar_norm.cu", "sar_rgcn.cu", "sar_ln.cu", *[f"sar_ln_{p}_{t}.cu" for p in ("fwd", "bwd") for t in ("f32", "bf16")], "sar_ckpt8.cu", "sar_ckpt8_rows_f32.cu", "sar_ckpt8_rows_bf16.cu", "sar_grouped.cu"]
+    "sar_glue.cu", "sar_norm.cu", "sar_rgcn.cu", "sar_ln.cu", *[f"sar_ln_{p}_{t}.cu" for p in ("fwd", "bwd", "bwd_grouped") for t in ("f32", "bf16")], "sar_ckpt8.cu", "sar_ckpt8_rows_f32.cu", "sar_ckpt8_rows_bf16.cu", "sar_grouped.cu"]
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--expt-relaxed-constexpr",

@@ -66,11 +66,14 @@ sar_status sar_ln_fwd_ckpt8(int64_t n, int32_t C, sar_dtype t, const void *x, co
     return ln_fwd_entry(n, C, t, x, gamma, beta, eps, y, nullptr, rstd, codes, scales, true, stream);
 }
 
-static sar_status ln_bwd_entry(int64_t n, int32_t C, sar_dtype t, const void *x, const float *mean, const int8_t *codes, const uint8_t *scales,
+static sar_status ln_bwd_entry(int64_t n, bool grouped, int32_t groups, const int64_t *offsets, int32_t C, sar_dtype t, const void *x, const float *mean, const int8_t *codes, const uint8_t *scales,
                                bool ckpt, const float *rstd, const float *gamma, const void *gy, void *gx, float *dgamma, float *dbeta,
                                void *workspace, size_t workspace_bytes, void *stream) {
     if (n < 0 || C < 1 || (n > 0 && (!rstd || !gy || !gx || (ckpt ? !codes || !scales : !x || !mean)))) return SAR_ERR_INVALID_ARG;
+    if (grouped && (groups < 1 || (!offsets && n > 0))) return SAR_ERR_INVALID_ARG;
     SAR_TRY(ln_check(C, t));
+    if (grouped && groups > SAR_MAX_GROUPS) return SAR_ERR_UNSUPPORTED;
+    SAR_TRY(check_elem_align({offsets}, 8));
     const LnShape s = ln_shape(C, t, ckpt ? kLnBwd8 : kLnBwd, ln_alignment({x, gy, gx}), ln_alignment({codes}));
     SAR_TRY(check_elem_align({mean, rstd, gamma, dgamma, dbeta}, 4));
     SAR_TRY(check_elem_align({x, gy, gx}, sar_elem_size(t)));
@@ -85,25 +88,40 @@ static sar_status ln_bwd_entry(int64_t n, int32_t C, sar_dtype t, const void *x,
     a.rstd_in = rstd;
     a.codes = const_cast<int8_t *>(codes);
     a.scales = const_cast<uint8_t *>(scales);
+    a.offsets = offsets;
+    a.groups = groups;
     const bool sums = dgamma || dbeta;
     if (sums) {
         if (!workspace || !sar_aligned(workspace, 16) || workspace_bytes < (size_t)ln_records_most(n, C) * 2 * C * 4) return SAR_ERR_WORKSPACE;
         a.partial = static_cast<float *>(workspace);
     }
     unsigned records = 0;
-    SAR_TRY((t == SAR_F32 ? ln_backward_f32 : ln_backward_bf16)(s, a, ckpt, &records, st));
+    auto pass = grouped ? (t == SAR_F32 ? ln_backward_grouped_f32 : ln_backward_grouped_bf16) : t == SAR_F32 ? ln_backward_f32 : ln_backward_bf16;
+    SAR_TRY(pass(s, a, ckpt, &records, st));
     return sums ? reduce_partials("ln_reduce", (int)records, 2 * C, C, a.partial, 1.0, dgamma, dbeta, st) : SAR_OK;
 }
 
 sar_status sar_ln_bwd(int64_t n, int32_t C, sar_dtype t, const void *x, const float *mean, const float *rstd, const float *gamma,
                       const void *gy, void *gx, float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream) {
-    return ln_bwd_entry(n, C, t, x, mean, nullptr, nullptr, false, rstd, gamma, gy, gx, dgamma, dbeta, workspace, workspace_bytes, stream);
+    return ln_bwd_entry(n, false, 0, nullptr, C, t, x, mean, nullptr, nullptr, false, rstd, gamma, gy, gx, dgamma, dbeta, workspace, workspace_bytes, stream);
+}
+
+sar_status sar_ln_bwd_grouped(int64_t n, int32_t groups, int32_t C, sar_dtype t, const int64_t *offsets, const void *x, const float *mean,
+                              const float *rstd, const float *gamma, const void *gy, void *gx, float *dgamma, float *dbeta,
+                              void *workspace, size_t workspace_bytes, void *stream) {
+    return ln_bwd_entry(n, true, groups, offsets, C, t, x, mean, nullptr, nullptr, false, rstd, gamma, gy, gx, dgamma, dbeta, workspace, workspace_bytes, stream);
 }
 
 sar_status sar_ln_bwd_ckpt8(int64_t n, int32_t C, sar_dtype t, const int8_t *codes, const uint8_t *scales, const float *rstd,
                             const float *gamma, const void *gy, void *gx, float *dgamma, float *dbeta, void *workspace,
                             size_t workspace_bytes, void *stream) {
-    return ln_bwd_entry(n, C, t, nullptr, nullptr, codes, scales, true, rstd, gamma, gy, gx, dgamma, dbeta, workspace, workspace_bytes, stream);
+    return ln_bwd_entry(n, false, 0, nullptr, C, t, nullptr, nullptr, codes, scales, true, rstd, gamma, gy, gx, dgamma, dbeta, workspace, workspace_bytes, stream);
+}
+
+sar_status sar_ln_bwd_ckpt8_grouped(int64_t n, int32_t groups, int32_t C, sar_dtype t, const int64_t *offsets, const int8_t *codes,
+                                    const uint8_t *scales, const float *rstd, const float *gamma, const void *gy, void *gx, float *dgamma,
+                                    float *dbeta, void *workspace, size_t workspace_bytes, void *stream) {
+    return ln_bwd_entry(n, true, groups, offsets, C, t, nullptr, nullptr, codes, scales, true, rstd, gamma, gy, gx, dgamma, dbeta, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

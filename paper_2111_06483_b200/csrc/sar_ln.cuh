@@ -31,6 +31,31 @@ struct LnArgs {
     uint8_t *scales;
     int nb;
     float *partial;               // [blocks][2][C] or null (no weight gradients asked for)
+    const int64_t *offsets;       // [groups + 1]: the rows that take part, of the backward kernels that know groups
+    int groups;
+};
+
+// The rows that take part: all, or those of some group, from the first offset to the largest (offsets read as the products by group
+// read them), which every thread of the block learns from shared memory.
+template <bool GROUPED>
+struct LnTaking {
+    __device__ __forceinline__ LnTaking(const LnArgs &, long long *) {}
+    __device__ __forceinline__ bool has(long long) const { return true; }
+};
+template <>
+struct LnTaking<true> {
+    const long long *range;
+    __device__ __forceinline__ LnTaking(const LnArgs &a, long long *shared) : range(shared) {
+        if (threadIdx.x < 32) {
+            const auto at = [&](int g) { return min(max((long long)__ldg(reinterpret_cast<const long long *>(a.offsets) + g), 0ll), a.n); };
+            long long end = 0;
+            for (int g = threadIdx.x; g <= a.groups; g += 32) end = max(end, at(g));
+            for (int d = 16; d > 0; d >>= 1) end = max(end, __shfl_xor_sync(0xffffffffu, end, d));
+            if (threadIdx.x == 0) shared[0] = at(0), shared[1] = end;
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ bool has(long long row) const { return row >= range[0] && row < range[1]; }
 };
 
 // Where a thread stands: lane gl of group gid of its warp, whose first row is the block's row `first`.  Groups of 64 lanes and more
@@ -543,9 +568,11 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(false, CK)) ln_fwd_ke
     }
 }
 
-template <typename Row, bool CK>
+template <typename Row, bool CK, bool GROUPED>
 __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_kernel(const LnArgs a) {
     after_predecessor();
+    __shared__ long long range[GROUPED ? 2 : 1];
+    const LnTaking<GROUPED> taking(a, range);
     constexpr int G = Row::G, V = Row::V, P = Row::P;
     extern __shared__ float smem[];   // [copies][2][C]; groups of several warps: [2][C] where there is more than one
     __shared__ LnRed red;
@@ -566,7 +593,7 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_ker
     };
     const auto ask = [&](long long base, Asked &q) {
         const long long row = base + id.gid;
-        const bool live = row < a.n;
+        const bool live = row < a.n && taking.has(row);   // others are zeros, and so is their gx
         r.ask(a.gy, row, live, q.g);
         if constexpr (CK) r.ask(a, row, live, q.c);
         else r.ask(a.x, row, live, q.x);
@@ -803,11 +830,17 @@ __device__ __forceinline__ float ln_long_xhat(const LnArgs &a, long long row, in
     else return (ln_load<T>(a.x, row * a.C + c) - mean) * rstd;
 }
 
-template <typename T, bool CK>
+template <typename T, bool CK, bool GROUPED>
 __global__ void __launch_bounds__(kThreads) ln_bwd_long_kernel(const LnArgs a) {
     after_predecessor();
     __shared__ float red[kWarpsPerBlock];
+    __shared__ long long range[GROUPED ? 2 : 1];
+    const LnTaking<GROUPED> taking(a, range);
     for (long long row = blockIdx.x; row < a.n; row += gridDim.x) {
+        if (GROUPED && !taking.has(row)) {
+            for (int c = threadIdx.x; c < a.C; c += kThreads) Elem<T>::store1(static_cast<T *>(a.y) + row * a.C + c, 0.f);
+            continue;
+        }
         const float mean = CK ? 0.f : a.mean_in[row], rstd = a.rstd_in[row];
         float along = 0.f, level = 0.f;
         for (int c = threadIdx.x; c < a.C; c += kThreads) {
@@ -826,14 +859,17 @@ __global__ void __launch_bounds__(kThreads) ln_bwd_long_kernel(const LnArgs a) {
 }
 
 // the sums over the rows for long rows: thread (slice, column) walks every slices-th row
-template <typename T, bool CK>
+template <typename T, bool CK, bool GROUPED>
 __global__ void __launch_bounds__(kThreads) ln_long_sums_kernel(const LnArgs a, int slices) {
     after_predecessor();
+    __shared__ long long range[GROUPED ? 2 : 1];
+    const LnTaking<GROUPED> taking(a, range);
     const long long id = (long long)blockIdx.x * kThreads + threadIdx.x;
     if (id >= (long long)slices * a.C) return;
     const int slice = (int)(id / a.C), c = (int)(id - (long long)slice * a.C);
     float s0 = 0.f, s1 = 0.f;
     for (long long row = slice; row < a.n; row += slices) {
+        if (GROUPED && !taking.has(row)) continue;
         const float g = ln_load<T>(a.gy, row * a.C + c);
         s0 += g;
         s1 = fmaf(g, ln_long_xhat<T, CK>(a, row, c, CK ? 0.f : __ldg(a.mean_in + row), __ldg(a.rstd_in + row)), s1);
@@ -1001,25 +1037,25 @@ static sar_status ln_forward_of(const LnShape &s, const LnArgs &a, cudaStream_t 
 }
 
 // the row pass and the records of the weights' sums (a.partial); *records: how many
-template <typename T, bool CK>
+template <typename T, bool CK, bool GROUPED = false>
 static sar_status ln_backward_of(const LnShape &s, const LnArgs &a, unsigned *records, cudaStream_t st) {
-    const char *name = CK ? "ln_bwd_ckpt8" : "ln_bwd";
+    const char *name = GROUPED ? (CK ? "ln_bwd_ckpt8_grouped" : "ln_bwd_grouped") : CK ? "ln_bwd_ckpt8" : "ln_bwd";
     if (s.E == 0) {
         // the sums first: gx may be written over gy or x
         const int slices = ln_slices(a.n);
         if (a.partial) {
-            SAR_LAUNCH("ln_bwd_sums", st, launch_if(a.n * a.C <= kOverlapElems, ln_long_sums_kernel<T, CK>, (unsigned)(((long long)slices * a.C + kThreads - 1) / kThreads), kThreads, 0, st, a, slices));
+            SAR_LAUNCH("ln_bwd_sums", st, launch_if(a.n * a.C <= kOverlapElems, ln_long_sums_kernel<T, CK, GROUPED>, (unsigned)(((long long)slices * a.C + kThreads - 1) / kThreads), kThreads, 0, st, a, slices));
             SAR_TRY(sar_after_launch());
         }
         *records = (unsigned)slices;
-        return ln_launch(name, ln_bwd_long_kernel<T, CK>, (unsigned)(a.n < kLnBlocks ? a.n : kLnBlocks), kLnBlocks, 0, a, st);
+        return ln_launch(name, ln_bwd_long_kernel<T, CK, GROUPED>, (unsigned)(a.n < kLnBlocks ? a.n : kLnBlocks), kLnBlocks, 0, a, st);
     }
     return ln_dispatch<T, CK ? kLnBwd8 : kLnBwd>(s, [&](auto cfg) -> sar_status {
         using Row = typename decltype(cfg)::row;
-        static const unsigned most = ln_resident(ln_bwd_kernel<Row, CK>, Row::G == kThreads ? 0 : kLnSmem);
+        static const unsigned most = ln_resident(ln_bwd_kernel<Row, CK, GROUPED>, Row::G == kThreads ? 0 : kLnSmem);
         const unsigned want = ln_grid<Row::G>((a.n + 1) / 2);   // two rows per lane group, which it asks for at once, before a block pays for its record
         *records = want < 1 ? 1 : want < most ? want : most;
-        return ln_launch(name, ln_bwd_kernel<Row, CK>, want, most, !a.partial || Row::G == kThreads ? 0 : (size_t)(Row::G > 32 ? 1 : ln_copies(a.C)) * 2 * a.C * 4, a, st);
+        return ln_launch(name, ln_bwd_kernel<Row, CK, GROUPED>, want, most, !a.partial || Row::G == kThreads ? 0 : (size_t)(Row::G > 32 ? 1 : ln_copies(a.C)) * 2 * a.C * 4, a, st);
     });
 }
 
@@ -1028,6 +1064,9 @@ sar_status ln_forward_f32(const LnShape &s, const LnArgs &a, bool ckpt, cudaStre
 sar_status ln_forward_bf16(const LnShape &s, const LnArgs &a, bool ckpt, cudaStream_t st);
 sar_status ln_backward_f32(const LnShape &s, const LnArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
 sar_status ln_backward_bf16(const LnShape &s, const LnArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
+// ... over the rows of some group (a.offsets): kernels of their own, the others have no register to spare
+sar_status ln_backward_grouped_f32(const LnShape &s, const LnArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
+sar_status ln_backward_grouped_bf16(const LnShape &s, const LnArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
 // checkpoints row by row: x -> codes and scales, and back to y
 sar_status ln_checkpoint_f32(const LnShape &s, const LnArgs &a, bool unpack, cudaStream_t st);
 sar_status ln_checkpoint_bf16(const LnShape &s, const LnArgs &a, bool unpack, cudaStream_t st);

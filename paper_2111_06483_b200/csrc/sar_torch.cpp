@@ -28,7 +28,7 @@ namespace {
     X(sar_bn_stats) X(sar_bn_rstd) X(sar_bn_apply) X(sar_bn_bwd_stats) X(sar_bn_bwd_apply)                             \
     X(sar_graph_workspace_bytes) X(sar_graph_from_coo) X(sar_csr_split_indptr) X(sar_csr_split_indices)                \
     X(sar_csc_slice_indptr) X(sar_plan_many_workspace_bytes) X(sar_plan_count_many) X(sar_plan_fill_many) X(sar_gather_i64) \
-    X(sar_ln_workspace_bytes_rows) X(sar_ln_fwd) X(sar_ln_bwd) X(sar_ln_fwd_ckpt8) X(sar_ln_bwd_ckpt8) X(sar_ckpt8_pack) X(sar_ckpt8_unpack) \
+    X(sar_ln_workspace_bytes_rows) X(sar_ln_fwd) X(sar_ln_bwd) X(sar_ln_fwd_ckpt8) X(sar_ln_bwd_ckpt8) X(sar_ln_bwd_grouped) X(sar_ln_bwd_ckpt8_grouped) X(sar_ckpt8_pack) X(sar_ckpt8_unpack) \
     X(sar_linear_grouped_workspace_bytes) X(sar_linear_grouped) X(sar_linear_grouped_bwd_input) X(sar_linear_grouped_bwd_weight) \
     X(sar_linear_grouped_bwd_weight_ckpt8)
 
@@ -713,38 +713,49 @@ PyObject *ln_forward(Args &a) {   // x, eps, gamma, beta, checkpoint -> y, mean,
     return tuple(y, mean, rstd);
 }
 
-PyObject *ln_backward(Args &a) {   // x, gy, mean, rstd, gamma
+const int64_t *group_offsets(const at::Tensor &o, int64_t groups) {
+    require(o.scalar_type() == at::kLong && o.dim() == 1 && o.numel() == groups + 1, "expected int64 offsets, one more than matrices");
+    return static_cast<const int64_t *>(o.const_data_ptr());
+}
+PyObject *ln_backward(Args &a) {   // x, gy, mean, rstd, gamma, offsets or None
     const at::Tensor &x = a.tensor(), &gy = a.tensor(), &mean = a.tensor(), &rstd = a.tensor();
-    const at::Tensor gamma = a.optional();
-    const On on(x, gy, mean, rstd, gamma);
+    const at::Tensor gamma = a.optional(), o = a.optional();
+    const On on(x, gy, mean, rstd, gamma, o);
     const Matrix m(x);
     require(gy.sizes() == x.sizes(), "gy of another shape than x");
     require_like(gy, x, m.n * m.C);
     const float *pm = f32(mean, m.n), *pr = f32(rstd, m.n), *pg = f32(gamma, m.C);
     const at::Tensor ws = bytes(L.sar_ln_workspace_bytes_rows(m.n, m.C), x);
     const at::Tensor gx = empty(x.sizes(), x.scalar_type(), x), dg = empty({m.C}, at::kFloat, x), db = empty({m.C}, at::kFloat, x);
+    if (o.defined()) {
+        const int32_t T = size32(o.numel() - 1);
+        SAR(sar_ln_bwd_grouped, m.n, T, m.C, m.t, group_offsets(o, T), ptr(x), pm, pr, pg, ptr(gy), ptrm(gx), f32m(dg), f32m(db), ptrm(ws), ws.nbytes(), stream());
+        return tuple(gx, dg, db);
+    }
     SAR(sar_ln_bwd, m.n, m.C, m.t, ptr(x), pm, pr, pg, ptr(gy), ptrm(gx), f32m(dg), f32m(db), ptrm(ws), ws.nbytes(), stream());
     return tuple(gx, dg, db);
 }
 
-PyObject *ln_backward_ckpt8(Args &a) {   // codes, scales, gy, rstd, gamma
+PyObject *ln_backward_ckpt8(Args &a) {   // codes, scales, gy, rstd, gamma, offsets or None
     const at::Tensor &codes = a.tensor(), &scales = a.tensor(), &gy = a.tensor(), &rstd = a.tensor();
-    const at::Tensor gamma = a.optional();
-    const On on(gy, codes, scales, rstd, gamma);
+    const at::Tensor gamma = a.optional(), o = a.optional();
+    const On on(gy, codes, scales, rstd, gamma, o);
     const Matrix m(gy);
     require(gy.sizes() == codes.sizes(), "gy of another shape than the checkpoint");
     require_checkpoint(codes, scales, m.n, m.C);
     const float *pr = f32(rstd, m.n), *pg = f32(gamma, m.C);
     const at::Tensor ws = bytes(L.sar_ln_workspace_bytes_rows(m.n, m.C), gy);
     const at::Tensor gx = empty(gy.sizes(), gy.scalar_type(), gy), dg = empty({m.C}, at::kFloat, gy), db = empty({m.C}, at::kFloat, gy);
+    if (o.defined()) {
+        const int32_t T = size32(o.numel() - 1);
+        SAR(sar_ln_bwd_ckpt8_grouped, m.n, T, m.C, m.t, group_offsets(o, T), i8(codes), u8(scales), pr, pg, ptr(gy), ptrm(gx), f32m(dg), f32m(db), ptrm(ws),
+            ws.nbytes(), stream());
+        return tuple(gx, dg, db);
+    }
     SAR(sar_ln_bwd_ckpt8, m.n, m.C, m.t, i8(codes), u8(scales), pr, pg, ptr(gy), ptrm(gx), f32m(dg), f32m(db), ptrm(ws), ws.nbytes(), stream());
     return tuple(gx, dg, db);
 }
 
-const int64_t *group_offsets(const at::Tensor &o, int64_t groups) {
-    require(o.scalar_type() == at::kLong && o.dim() == 1 && o.numel() == groups + 1, "expected int64 offsets, one more than matrices");
-    return static_cast<const int64_t *>(o.const_data_ptr());
-}
 // rows [n, K] times W [types, d_in, d_out] or its transposes; rows of no type: zeros in a new array, kept in a given one
 PyObject *typed_rows(Args &a, bool transposed) {   // rows, W, offsets, out or None
     const at::Tensor &x = a.tensor(), &W = a.tensor(), &o = a.tensor();

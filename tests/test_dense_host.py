@@ -41,3 +41,16 @@ def test_scratch_of_the_normalisation_follows_the_records():
     for n, C in ((-1, 64), (5, 0), (5, (1 << 20) + 1)):
         assert B.sar_ln_workspace_bytes_rows(n, C) == 0
     assert B.sar_ln_workspace_bytes((1 << 20) + 1) == 0   # which the calls refuse
+
+
+def test_refusals_of_the_normalisation_s_gradients_by_group():
+    from ctypes import c_int32, c_int64, c_size_t, c_void_p
+    lib, P, odd, null, lots = B.lib(), c_void_p(1 << 20), c_void_p((1 << 20) + 4), c_void_p(0), c_size_t(1 << 40)
+    rows = (c_int64(10), c_int32(3), c_int32(64), 0, P, P, P, P, P, P, P, P, P, P, lots, null)      # n, groups, C, t, offsets, x, mean, rstd, gamma, gy, gx, ...
+    packed = (c_int64(10), c_int32(3), c_int32(64), 0, P, P, P, P, P, P, P, P, P, P, lots, null)    # ... offsets, codes, scales, rstd, gamma, gy, gx, ...
+    for fn, good in ((lib.sar_ln_bwd_grouped, rows), (lib.sar_ln_bwd_ckpt8_grouped, packed)):
+        for status, at, value in ((-1, 0, c_int64(-1)), (-1, 1, c_int32(0)), (-2, 1, c_int32(1025)), (-1, 2, c_int32(0)), (-1, 3, 7), (-1, 4, null), (-3, 4, odd),
+                                  (-1, 5, null), (-1, 6, null), (-1, 7, null), (-1, 9, null), (-1, 10, null), (-4, 13, null), (-4, 14, c_size_t(64))):
+            args = list(good)
+            args[at] = value
+            assert fn(*args) == status, (fn.__name__, at)

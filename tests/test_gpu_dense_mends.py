@@ -169,3 +169,54 @@ def test_weight_gradients_of_many_rows_taken_turned_or_not(sizes, d_in, d_out):
         x, y = h[a:b].double(), dz[a:b].double()
         size = x.abs().t() @ y.abs()
         assert ((dw[g].double() - x.t() @ y).abs() <= (34 * 2.0 ** -22 + (n // 512 + 160) * 2.0 ** -24) * size).all()
+
+
+@pytest.mark.parametrize("c", [1, 24, 47, 64, 100, 333, 1024, 1027, 2048, 5000, 8200])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("offsets", [[30, 30, 200, 333], [0, 400], [390, 400, 400], [400, 400], [50, 20, 90, 60], [-5, 2 ** 40]])
+def test_the_normalisation_s_gradients_over_the_rows_of_some_group(c, dt, offsets):
+    """Rows of no group hold NaN and infinities in every array: all results are those of a call where these rows are zeros, bit for bit."""
+    from paper_2111_06483_b200 import api
+    n = 400
+    gen = torch.Generator().manual_seed(c)
+    x, gy = (torch.randn(n, c, generator=gen).to(dt).cuda() for _ in range(2))
+    gamma = torch.randn(c, generator=gen).cuda()
+    _, (mean, rstd) = api.ln_forward(x)
+    _, (ck, _) = api.ln_forward(x, checkpoint=True)
+    o = torch.tensor(offsets, device="cuda")
+    rows = oracle.group_rows(offsets, n)
+    out = torch.ones(n, dtype=torch.bool, device="cuda")
+    out[rows[0][0]:rows[-1][1]] = False
+
+    def filled(t, value):
+        return torch.where(out.view(-1, *[1] * (t.dim() - 1)), torch.full_like(t, value), t)
+    nan, inf = float("nan"), float("inf")
+    clean = [filled(t, 0) for t in (x, gy, mean, rstd, ck.codes, ck.scales)]
+    dirty = [filled(t, v) for t, v in ((x, nan), (gy, inf), (mean, inf), (rstd, nan), (ck.codes, 99), (ck.scales, 255))]
+    for checkpoint in (False, True):
+        def gradients(arrays, *more):
+            x, gy, mean, rstd, codes, scales = arrays
+            return api.ln_backward(x, gy, (api.Checkpoint8(codes, scales) if checkpoint else mean, rstd), gamma, *more)
+        want, got = gradients(clean), gradients(dirty, o)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and not got[0][out].any()
+
+
+@pytest.mark.parametrize("checkpoint", [False, True])
+def test_what_rows_of_no_type_hold_reaches_nothing_in_a_typed_layer(checkpoint):
+    """A padded batch: NaN and infinities behind the last node and before the first, in x and in the upstream gradient."""
+    from paper_2111_06483_b200 import api
+    n, d_in, d_out = 300, 96, 72
+    gen = torch.Generator().manual_seed(5)
+    x, gz = (torch.randn(n, d, generator=gen).bfloat16().cuda() for d in (d_in, d_out))
+    W = (torch.randn(2, d_in, d_out, generator=gen) / d_in ** 0.5).bfloat16().cuda()
+    gamma, beta = torch.rand(d_in, generator=gen).cuda() + 0.5, torch.randn(d_in, generator=gen).cuda()
+    o = torch.tensor([20, 100, 250], device="cuda")
+
+    def step():
+        z, saved = api.typed_layer_forward(x, W, o, gamma, beta, checkpoint=checkpoint)
+        return (z, *api.typed_layer_backward(W, o, saved, gz, gamma, beta))
+    want = step()
+    x[:20], x[250:], gz[:20], gz[250:] = float("nan"), float("inf"), float("inf"), float("nan")
+    got = step()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert not got[0][:20].any() and not got[1][250:].any() and not any(t.isnan().any() for t in got)
