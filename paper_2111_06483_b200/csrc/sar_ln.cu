@@ -79,7 +79,7 @@ static sar_status ln_bwd_entry(int64_t n, bool grouped, int32_t groups, const in
     SAR_TRY(check_elem_align({x, gy, gx}, sar_elem_size(t)));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (n == 0) return ln_zero(C, dgamma, dbeta, st);
-    LnArgs a = ln_args(n, C);
+    LnGroupedArgs a{ln_args(n, C), offsets, groups};
     a.x = x;
     a.gy = gy;
     a.y = gx;
@@ -88,16 +88,14 @@ static sar_status ln_bwd_entry(int64_t n, bool grouped, int32_t groups, const in
     a.rstd_in = rstd;
     a.codes = const_cast<int8_t *>(codes);
     a.scales = const_cast<uint8_t *>(scales);
-    a.offsets = offsets;
-    a.groups = groups;
     const bool sums = dgamma || dbeta;
     if (sums) {
         if (!workspace || !sar_aligned(workspace, 16) || workspace_bytes < (size_t)ln_records_most(n, C) * 2 * C * 4) return SAR_ERR_WORKSPACE;
         a.partial = static_cast<float *>(workspace);
     }
     unsigned records = 0;
-    auto pass = grouped ? (t == SAR_F32 ? ln_backward_grouped_f32 : ln_backward_grouped_bf16) : t == SAR_F32 ? ln_backward_f32 : ln_backward_bf16;
-    SAR_TRY(pass(s, a, ckpt, &records, st));
+    if (grouped) SAR_TRY((t == SAR_F32 ? ln_backward_grouped_f32 : ln_backward_grouped_bf16)(s, a, ckpt, &records, st));
+    else SAR_TRY((t == SAR_F32 ? ln_backward_f32 : ln_backward_bf16)(s, a, ckpt, &records, st));
     return sums ? reduce_partials("ln_reduce", (int)records, 2 * C, C, a.partial, 1.0, dgamma, dbeta, st) : SAR_OK;
 }
 

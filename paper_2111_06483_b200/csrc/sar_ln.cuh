@@ -6,6 +6,8 @@
 #include "sar_dispatch.cuh"
 #include "sar_rowkernels.cuh"
 
+#include <type_traits>
+
 namespace sar {
 
 constexpr int kSms = 148;
@@ -31,32 +33,31 @@ struct LnArgs {
     uint8_t *scales;
     int nb;
     float *partial;               // [blocks][2][C] or null (no weight gradients asked for)
-    const int64_t *offsets;       // [groups + 1]: the rows that take part, of the backward kernels that know groups
+};
+// ... of the backward kernels that know groups.  A type of its own: with two members more in LnArgs the other kernels came out with
+// other registers (31,000 rows of 2,047 bf16 backward 218 -> 313 us, a million of 256 from the checkpoint 243 -> 265).
+struct LnGroupedArgs : LnArgs {
+    const int64_t *offsets;       // [groups + 1]: the rows that take part
     int groups;
 };
 
-// The rows that take part: all, or those of some group, from the first offset to the largest (offsets read as the products by group
-// read them), which every thread of the block learns from shared memory.
-template <bool GROUPED>
-struct LnTaking {
-    __device__ __forceinline__ LnTaking(const LnArgs &, long long *) {}
-    __device__ __forceinline__ bool has(long long) const { return true; }
-};
-template <>
-struct LnTaking<true> {
-    const long long *range;
-    __device__ __forceinline__ LnTaking(const LnArgs &a, long long *shared) : range(shared) {
-        if (threadIdx.x < 32) {
-            const auto at = [&](int g) { return min(max((long long)__ldg(reinterpret_cast<const long long *>(a.offsets) + g), 0ll), a.n); };
-            long long end = 0;
-            for (int g = threadIdx.x; g <= a.groups; g += 32) end = max(end, at(g));
-            for (int d = 16; d > 0; d >>= 1) end = max(end, __shfl_xor_sync(0xffffffffu, end, d));
-            if (threadIdx.x == 0) shared[0] = at(0), shared[1] = end;
-        }
-        __syncthreads();
+// The rows of some group, from the first offset to the largest (offsets read as the products by group read them), for every thread of
+// the block.
+__device__ __forceinline__ long long *ln_range() {
+    __shared__ long long range[2];
+    return range;
+}
+__device__ __forceinline__ void ln_find_range(const LnGroupedArgs &a) {
+    if (threadIdx.x < 32) {
+        const auto at = [&](int g) { return min(max((long long)__ldg(reinterpret_cast<const long long *>(a.offsets) + g), 0ll), a.n); };
+        long long end = 0;
+        for (int g = threadIdx.x; g <= a.groups; g += 32) end = max(end, at(g));
+        for (int d = 16; d > 0; d >>= 1) end = max(end, __shfl_xor_sync(0xffffffffu, end, d));
+        if (threadIdx.x == 0) ln_range()[0] = at(0), ln_range()[1] = end;
     }
-    __device__ __forceinline__ bool has(long long row) const { return row >= range[0] && row < range[1]; }
-};
+    __syncthreads();
+}
+__device__ __forceinline__ bool ln_in_range(long long row) { return row >= ln_range()[0] && row < ln_range()[1]; }
 
 // Where a thread stands: lane gl of group gid of its warp, whose first row is the block's row `first`.  Groups of 64 lanes and more
 // are several warps.
@@ -568,12 +569,19 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(false, CK)) ln_fwd_ke
     }
 }
 
-template <typename Row, bool CK, bool GROUPED>
-__global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_kernel(const LnArgs a) {
+template <typename Row, bool CK, typename Args>
+__global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_kernel(const Args a) {
+    constexpr bool GROUPED = std::is_same<Args, LnGroupedArgs>::value;
     after_predecessor();
-    __shared__ long long range[GROUPED ? 2 : 1];
-    const LnTaking<GROUPED> taking(a, range);
     constexpr int G = Row::G, V = Row::V, P = Row::P;
+    // where the range is at hand, us, registers / shared memory: from the checkpoint a million rows of 256 bf16 251 / 282, of 100 165 / 160,
+    // 674,000 of 95 176 / 159, 120,000 of 2,048 (128 lanes) 272 / 255; from the rows a million of 256 254 / 252
+    constexpr bool kKeepRange = CK && G <= 32 && Row::E == 8;
+    long long begin, end;
+    if constexpr (GROUPED) {
+        ln_find_range(a);
+        if constexpr (kKeepRange) begin = ln_range()[0], end = ln_range()[1];
+    }
     extern __shared__ float smem[];   // [copies][2][C]; groups of several warps: [2][C] where there is more than one
     __shared__ LnRed red;
     const LnLane<G> id;
@@ -593,7 +601,9 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_ker
     };
     const auto ask = [&](long long base, Asked &q) {
         const long long row = base + id.gid;
-        const bool live = row < a.n && taking.has(row);   // others are zeros, and so is their gx
+        bool live = row < a.n;
+        if constexpr (GROUPED && kKeepRange) live = live && row >= begin && row < end;   // others are zeros, and so is their gx
+        else if constexpr (GROUPED) live = live && ln_in_range(row);
         r.ask(a.gy, row, live, q.g);
         if constexpr (CK) r.ask(a, row, live, q.c);
         else r.ask(a.x, row, live, q.x);
@@ -830,16 +840,18 @@ __device__ __forceinline__ float ln_long_xhat(const LnArgs &a, long long row, in
     else return (ln_load<T>(a.x, row * a.C + c) - mean) * rstd;
 }
 
-template <typename T, bool CK, bool GROUPED>
-__global__ void __launch_bounds__(kThreads) ln_bwd_long_kernel(const LnArgs a) {
+template <typename T, bool CK, typename Args>
+__global__ void __launch_bounds__(kThreads) ln_bwd_long_kernel(const Args a) {
+    constexpr bool GROUPED = std::is_same<Args, LnGroupedArgs>::value;
     after_predecessor();
     __shared__ float red[kWarpsPerBlock];
-    __shared__ long long range[GROUPED ? 2 : 1];
-    const LnTaking<GROUPED> taking(a, range);
+    if constexpr (GROUPED) ln_find_range(a);
     for (long long row = blockIdx.x; row < a.n; row += gridDim.x) {
-        if (GROUPED && !taking.has(row)) {
-            for (int c = threadIdx.x; c < a.C; c += kThreads) Elem<T>::store1(static_cast<T *>(a.y) + row * a.C + c, 0.f);
-            continue;
+        if constexpr (GROUPED) {
+            if (!ln_in_range(row)) {
+                for (int c = threadIdx.x; c < a.C; c += kThreads) Elem<T>::store1(static_cast<T *>(a.y) + row * a.C + c, 0.f);
+                continue;
+            }
         }
         const float mean = CK ? 0.f : a.mean_in[row], rstd = a.rstd_in[row];
         float along = 0.f, level = 0.f;
@@ -859,17 +871,19 @@ __global__ void __launch_bounds__(kThreads) ln_bwd_long_kernel(const LnArgs a) {
 }
 
 // the sums over the rows for long rows: thread (slice, column) walks every slices-th row
-template <typename T, bool CK, bool GROUPED>
-__global__ void __launch_bounds__(kThreads) ln_long_sums_kernel(const LnArgs a, int slices) {
+template <typename T, bool CK, typename Args>
+__global__ void __launch_bounds__(kThreads) ln_long_sums_kernel(const Args a, int slices) {
+    constexpr bool GROUPED = std::is_same<Args, LnGroupedArgs>::value;
     after_predecessor();
-    __shared__ long long range[GROUPED ? 2 : 1];
-    const LnTaking<GROUPED> taking(a, range);
+    if constexpr (GROUPED) ln_find_range(a);
     const long long id = (long long)blockIdx.x * kThreads + threadIdx.x;
     if (id >= (long long)slices * a.C) return;
     const int slice = (int)(id / a.C), c = (int)(id - (long long)slice * a.C);
     float s0 = 0.f, s1 = 0.f;
     for (long long row = slice; row < a.n; row += slices) {
-        if (GROUPED && !taking.has(row)) continue;
+        if constexpr (GROUPED) {
+            if (!ln_in_range(row)) continue;
+        }
         const float g = ln_load<T>(a.gy, row * a.C + c);
         s0 += g;
         s1 = fmaf(g, ln_long_xhat<T, CK>(a, row, c, CK ? 0.f : __ldg(a.mean_in + row), __ldg(a.rstd_in + row)), s1);
@@ -1019,8 +1033,8 @@ static unsigned ln_resident(K kernel, size_t smem) {
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kThreads, smem) != cudaSuccess) (void)cudaGetLastError();
     return (unsigned)(kSms * (per_sm < 1 ? 1 : per_sm > kLnBlocks / kSms ? kLnBlocks / kSms : per_sm));
 }
-template <typename K>
-static sar_status ln_launch(const char *name, K kernel, unsigned want, unsigned most, size_t smem, const LnArgs &a, cudaStream_t st) {
+template <typename K, typename Args>
+static sar_status ln_launch(const char *name, K kernel, unsigned want, unsigned most, size_t smem, const Args &a, cudaStream_t st) {
     SAR_LAUNCH(name, st, launch_if(a.n * a.C <= kOverlapElems, kernel, want < 1 ? 1 : want < most ? want : most, kThreads, smem, st, a));
     return sar_after_launch();
 }
@@ -1037,25 +1051,25 @@ static sar_status ln_forward_of(const LnShape &s, const LnArgs &a, cudaStream_t 
 }
 
 // the row pass and the records of the weights' sums (a.partial); *records: how many
-template <typename T, bool CK, bool GROUPED = false>
-static sar_status ln_backward_of(const LnShape &s, const LnArgs &a, unsigned *records, cudaStream_t st) {
-    const char *name = GROUPED ? (CK ? "ln_bwd_ckpt8_grouped" : "ln_bwd_grouped") : CK ? "ln_bwd_ckpt8" : "ln_bwd";
+template <typename T, bool CK, typename Args>
+static sar_status ln_backward_of(const LnShape &s, const Args &a, unsigned *records, cudaStream_t st) {
+    const char *name = std::is_same<Args, LnGroupedArgs>::value ? (CK ? "ln_bwd_ckpt8_grouped" : "ln_bwd_grouped") : CK ? "ln_bwd_ckpt8" : "ln_bwd";
     if (s.E == 0) {
         // the sums first: gx may be written over gy or x
         const int slices = ln_slices(a.n);
         if (a.partial) {
-            SAR_LAUNCH("ln_bwd_sums", st, launch_if(a.n * a.C <= kOverlapElems, ln_long_sums_kernel<T, CK, GROUPED>, (unsigned)(((long long)slices * a.C + kThreads - 1) / kThreads), kThreads, 0, st, a, slices));
+            SAR_LAUNCH("ln_bwd_sums", st, launch_if(a.n * a.C <= kOverlapElems, ln_long_sums_kernel<T, CK, Args>, (unsigned)(((long long)slices * a.C + kThreads - 1) / kThreads), kThreads, 0, st, a, slices));
             SAR_TRY(sar_after_launch());
         }
         *records = (unsigned)slices;
-        return ln_launch(name, ln_bwd_long_kernel<T, CK, GROUPED>, (unsigned)(a.n < kLnBlocks ? a.n : kLnBlocks), kLnBlocks, 0, a, st);
+        return ln_launch(name, ln_bwd_long_kernel<T, CK, Args>, (unsigned)(a.n < kLnBlocks ? a.n : kLnBlocks), kLnBlocks, 0, a, st);
     }
     return ln_dispatch<T, CK ? kLnBwd8 : kLnBwd>(s, [&](auto cfg) -> sar_status {
         using Row = typename decltype(cfg)::row;
-        static const unsigned most = ln_resident(ln_bwd_kernel<Row, CK, GROUPED>, Row::G == kThreads ? 0 : kLnSmem);
+        static const unsigned most = ln_resident(ln_bwd_kernel<Row, CK, Args>, Row::G == kThreads ? 0 : kLnSmem);
         const unsigned want = ln_grid<Row::G>((a.n + 1) / 2);   // two rows per lane group, which it asks for at once, before a block pays for its record
         *records = want < 1 ? 1 : want < most ? want : most;
-        return ln_launch(name, ln_bwd_kernel<Row, CK, GROUPED>, want, most, !a.partial || Row::G == kThreads ? 0 : (size_t)(Row::G > 32 ? 1 : ln_copies(a.C)) * 2 * a.C * 4, a, st);
+        return ln_launch(name, ln_bwd_kernel<Row, CK, Args>, want, most, !a.partial || Row::G == kThreads ? 0 : (size_t)(Row::G > 32 ? 1 : ln_copies(a.C)) * 2 * a.C * 4, a, st);
     });
 }
 
@@ -1064,9 +1078,9 @@ sar_status ln_forward_f32(const LnShape &s, const LnArgs &a, bool ckpt, cudaStre
 sar_status ln_forward_bf16(const LnShape &s, const LnArgs &a, bool ckpt, cudaStream_t st);
 sar_status ln_backward_f32(const LnShape &s, const LnArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
 sar_status ln_backward_bf16(const LnShape &s, const LnArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
-// ... over the rows of some group (a.offsets): kernels of their own, the others have no register to spare
-sar_status ln_backward_grouped_f32(const LnShape &s, const LnArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
-sar_status ln_backward_grouped_bf16(const LnShape &s, const LnArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
+// ... over the rows of some group: kernels of their own, the others have no register to spare
+sar_status ln_backward_grouped_f32(const LnShape &s, const LnGroupedArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
+sar_status ln_backward_grouped_bf16(const LnShape &s, const LnGroupedArgs &a, bool ckpt, unsigned *records, cudaStream_t st);
 // checkpoints row by row: x -> codes and scales, and back to y
 sar_status ln_checkpoint_f32(const LnShape &s, const LnArgs &a, bool unpack, cudaStream_t st);
 sar_status ln_checkpoint_bf16(const LnShape &s, const LnArgs &a, bool unpack, cudaStream_t st);
