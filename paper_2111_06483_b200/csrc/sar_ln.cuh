@@ -691,8 +691,9 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(true, CK)) ln_bwd_ker
                 }
             }
     }
-    // The warp's number once more, from a source the compiler does not see through: kept from the start it pushes a value that the
-    // rows need out of the registers (250,000 rows of 1,024 float32 from the checkpoint 625 us, so 492; 552 and 500 without one).
+    // The warp's number once more, from a source the compiler does not see through: kept from the start it can push a value that the
+    // rows need out of the registers (from the checkpoint 1,360,000 rows of 47 bf16 200 us, so 184; 500,000 of 512 266, so 262; a million
+    // of 256 float32 388, so 386; but 330,000 of 768 bf16 325, so 354; other widths and passes alike to 1 %).
     unsigned warp;
     asm volatile("shr.u32 %0, %1, 5;" : "=r"(warp) : "r"(threadIdx.x));
     const unsigned copies = ln_copies(a.C), turns = kWarpsPerBlock / copies;
