@@ -599,8 +599,9 @@ SAR_API sar_status sar_bn_bwd_apply_act(int64_t n, int32_t C, sar_dtype t, const
  *                     anything infinite or NaN.  Every value comes back within 2^(s - 127), a 64th of top at most; the bytes
  *                     are the same on every path and device.
  *   sar_ckpt8_unpack  the values that the checkpoint stands for (exact in float32; in bf16 as well).
- * Arrays aligned to 16 bytes (codes to 8) move 16 bytes at a time whatever C from 16 to about 1,000, and beyond where C is a
- * multiple of 32; others work as well, in fours or column by column.
+ * Arrays aligned to 16 bytes (codes to 8) run near the memory's rate where C is a multiple of 8 (bf16) or 4 (float32), and bf16 rows of
+ * a multiple of 4 take up to twice as long.  Other widths, and arrays aligned to less, work as well: 1.5 to 2.5 times as long in float32, 3 to
+ * 4 in bf16, 5 from 128 to 350 columns packed.  Of a checkpoint, s is at most 248 as packed; with more, values may leave float32.
  * n = 0 is allowed.  Errors: SAR_ERR_INVALID_ARG, SAR_ERR_UNSUPPORTED (C > 2^20),
  * SAR_ERR_ALIGNMENT (x not aligned to its type).
  * ------------------------------------------------------------------------------------------- */
@@ -625,9 +626,13 @@ SAR_API sar_status sar_ckpt8_unpack(int64_t n, int32_t C, sar_dtype t, const int
  * Scratch of the backward calls where dgamma or dbeta is asked for: sar_ln_workspace_bytes_rows(n, C), which never falls as n grows,
  * or sar_ln_workspace_bytes(C), enough for any n (1,184 records of 2 C floats, 148 beyond 8,192 columns).  Sums over the rows are formed in
  * a fixed order (no atomics), block partials are added in float64.  n = 0 is allowed (dgamma, dbeta are written as zeros).
- * Arrays aligned to 16 bytes (codes to 8) move 16 bytes at a time where C is a multiple of 8 (bf16) or 4, and whatever C from 128
- * to about 1,000; others work as well, column by column.  Rows are read once up to 8,192 columns (2,048 column by column) and again
- * for each of the row's sums beyond.
+ * Arrays aligned to 16 bytes (codes to 8) run near the memory's rate where C is a multiple of 8 (bf16) or 4 (float32) up to 4,096, and
+ * bf16 rows of a multiple of 4 take up to twice as long.  Other widths, and arrays aligned to less, work as well: 1.3 to 3 times as long in
+ * float32, 2.3 to 4.5 in bf16, more above 1,024 columns.  Rows are read once up to 8,192 columns (2,048 where they allow one column
+ * at a time) and again for each of the row's sums beyond.
+ * The mean is that of the row to a unit in its last place or so, and xhat is taken from a mean as exact as the row's spread needs (a constant
+ * row gives beta).  A row whose sum of squared deviations is no float32, values from about 1e18 on, comes out as
+ * rstd = 0 and y = beta.
  * Errors: SAR_ERR_INVALID_ARG (NULL arrays, eps < 0 or NaN), SAR_ERR_UNSUPPORTED (C > 2^20), SAR_ERR_ALIGNMENT (arrays not
  * aligned to their type), SAR_ERR_WORKSPACE.
  * ------------------------------------------------------------------------------------------- */

@@ -1,8 +1,8 @@
 // Checkpoints of node arrays in 8 bits: x[n, C] -> codes and block scales, and back (include/sar.h has the format and the
 // contracts).  Each is one pass over its arrays.  Whole blocks are counted through the array here, whatever the rows; rows whose last
 // block is short go row by row through the layer normalisation's kernels, without a division for every block (a million rows
-// of 100, us: float32 packed 113 either way, unpacked 126 here and 89 by rows; bf16 103 and 100, 107 and 71), unless they are longer
-// than a warp's registers.
+// of 100, us, here and by rows: float32 packed 108 and 101, unpacked 125 and 87; bf16 97 and 95, 106 and 68; of 72 bf16 70 and 44, 54
+// and 43), unless they are longer than a block's registers.
 #include "sar_ckpt8.cuh"
 #include "sar_ln.cuh"
 
@@ -191,7 +191,7 @@ sar_status sar_ckpt8_pack(int64_t n, int32_t C, sar_dtype t, const void *x, int8
     SAR_TRY(ckpt_check(n, C, t, x, codes, scales));
     if (n == 0) return SAR_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const LnShape s = ln_shape(C, t, kLnCkpt, ln_alignment({x}), ln_alignment({codes}));
+    const LnShape s = ln_shape(C, t, kLnPack, ln_alignment({x}), ln_alignment({codes}));
     if (C % kCkptBlock != 0 && s.E > 0) {
         LnArgs a = ln_args(n, C);
         a.x = x;

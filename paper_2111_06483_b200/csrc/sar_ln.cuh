@@ -451,7 +451,9 @@ struct LnShiftedRow {
 // compiler likes and so: bf16 forward 106 registers 48, 80 (three blocks) 43; backward 138 86, 128 (two) 63, from the checkpoint 140
 // 107, 128 61; float32 forward with the checkpoint 84 118, 78 (three) 99.  Groups of several warps wait for each other at every sum,
 // so other blocks have to fill in: 60,000 rows of 4,096 bf16 forward two 207, three 176, four 185, backward one 408, two 255,
-// three 442 (the sums leave the registers).
+// three 442 (the sums leave the registers).  For these bounds whole vectors spill up to 60 bytes (across 256
+// lanes up to 180), single columns up to 140, shifted rows 100 to 230 backward in slots of 8 and 250 to 350 forward in six of 4; other
+// bounds have not been measured for the last two.
 template <typename Row>
 constexpr int ln_blocks(bool bwd, bool ck) {
     constexpr int N = Row::E * Row::V, E = Row::E;
@@ -904,26 +906,29 @@ struct LnShape {
 #define SAR_LN_8(X) X(8, 4, 1) X(8, 4, 2) X(8, 4, 3) X(8, 8, 2) X(8, 8, 3) X(8, 16, 2) X(8, 16, 3) X(8, 32, 2) X(8, 32, 3) X(8, 64, 2) X(8, 64, 3) X(8, 128, 2) X(8, 256, 2) X(8, 256, 4)
 #define SAR_LN_4(X) X(4, 4, 1) X(4, 4, 2) X(4, 8, 2) X(4, 8, 3) X(4, 16, 2) X(4, 16, 3) X(4, 32, 2) X(4, 32, 3) X(4, 64, 2) X(4, 64, 3) X(4, 128, 2) X(4, 128, 3) X(4, 256, 2) X(4, 256, 4) X(4, 256, 8)
 // ... bf16 that divides into fours but not eights, where the pass reads x: 16 columns a lane here, too.  A million rows of 100, us, 8 a
-// lane against 16: forward 92 / 92, with the checkpoint 167 / 151, backward 160 / 115; from the checkpoint 152 / 155
+// lane against 16: forward 95 / 93, with the checkpoint 160 / 140, backward 165 / 119
 #define SAR_LN_4H(X) X(4, 4, 1) X(4, 4, 2) X(4, 4, 4) X(4, 8, 3) X(4, 8, 4) X(4, 16, 3) X(4, 16, 4) X(4, 32, 3) X(4, 32, 4) X(4, 64, 3) X(4, 64, 4) X(4, 128, 4) X(4, 256, 4) X(4, 256, 8)
 #define SAR_LN_8S(X) X(8, 16, 2) X(8, 32, 2) X(8, 32, 3) X(8, 32, 4)
-#define SAR_LN_4S(X) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6) X(4, 32, 8)
+#define SAR_LN_4S(X) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6)
 // ... and narrow shifted rows, for what reads checkpoints or only packs
 #define SAR_LN_8N(X) X(8, 4, 1) X(8, 4, 2) X(8, 8, 2)
 #define SAR_LN_4N(X) X(4, 8, 1) X(4, 8, 2) X(4, 16, 2)
 #define SAR_LN_1(X) X(1, 4, 1) X(1, 4, 4) X(1, 4, 8) X(1, 8, 6) X(1, 8, 8) X(1, 16, 6) X(1, 16, 8) X(1, 32, 8) X(1, 256, 4) X(1, 256, 8)
 // Columns from which rows that are no whole vectors are taken shifted.  64 million values, us, one column a lane and slot against
-// shifted: 95 bf16 forward 93 / 96, with checkpoint 187 / 205, backward 157 / 162; 191 bf16 111 / 97, 265 / 203, 191 / 159; 191
-// float32 123 / 113, 289 / 275, 169 / 156.  Checkpoints: 47 bf16 packed 173 / 141, unpacked 117 / 99, backward from
-// one 228 / 180; 47 float32 191 / 189.
-constexpr int kLnShiftedFrom = 128, kCkptShiftedFrom = 16;
+// shifted: 95 bf16 forward 95 / 167, with the checkpoint 173 / 322, backward 168 / 273; 191 bf16 115 / 97, 261 / 196, 175 / 163; 191
+// float32 113 / 115, 253 / 271, 165 / 161; 333 bf16 410 / 142, 718 / 288, 616 / 239.  Packed: 47 bf16 105 / 138, float32 101 / 161; 95 bf16
+// 119 / 138, float32 115 / 168; 191 bf16 197 / 140.  Backward from a checkpoint: 47 bf16 205 / 184, float32 209 / 194; 95 bf16 214 / 172.
+// Unpacked: 95 bf16 92 / 81, float32 88 / 91.  Float32 up to 765 columns: 8 slots of 4 spill (84,000 rows of 761 in 6 slots forward 136 / 130,
+// backward 216 / 152, from the checkpoint 265 / 168, packed 171 / 128; 64,000 of 1,001 in 8 slots 113 / 113, 184 / 275, 222 / 299, 152 / 227).
+constexpr int kLnShiftedFrom = 128, kPackShiftedFrom = 128, kCkptShiftedFrom = 16;
 
 template <typename R>
 struct LnCfg {
     using row = R;
 };
 // Calls f(LnCfg<row>{}) with the shape's kind of row.
-enum LnPass { kLnFwd, kLnBwd, kLnBwd8, kLnCkpt };   // kLnBwd8: from a checkpoint; kLnCkpt: packing and unpacking
+// kLnBwd8: from a checkpoint; kLnCkpt: the kernels that pack and unpack, whose shapes are asked for as kLnPack and kLnCkpt
+enum LnPass { kLnFwd, kLnBwd, kLnBwd8, kLnCkpt, kLnPack };
 template <typename T, LnPass PASS, typename Fn>
 static inline sar_status ln_dispatch(const LnShape &s, Fn &&f) {
 #define SAR_LN_CASE(EE, GG, VV) \
@@ -961,7 +966,8 @@ static inline sar_status ln_dispatch(const LnShape &s, Fn &&f) {
 static inline LnShape ln_shape(int32_t C, sar_dtype t, LnPass pass, size_t arrays, size_t codes) {
     LnShape s{0, 32, 0, false};
     const int E = t == SAR_BF16 ? 8 : 4;
-    const bool from_ckpt = pass == kLnCkpt || pass == kLnBwd8;
+    const bool from_ckpt = pass == kLnCkpt || pass == kLnBwd8 || pass == kLnPack;
+    const int shifted_from = pass == kLnPack ? kPackShiftedFrom : from_ckpt ? kCkptShiftedFrom : kLnShiftedFrom;
     const auto may = [&](int e) { return C % e == 0 && arrays >= e * sar_elem_size(t) && codes >= (size_t)e; };
     int need = C;
 #define SAR_LN_FIT(EE, GG, VV) \
@@ -974,7 +980,7 @@ static inline LnShape ln_shape(int32_t C, sar_dtype t, LnPass pass, size_t array
         } else {
             SAR_LN_4(SAR_LN_FIT)
         }
-    } else if (C >= (from_ckpt ? kCkptShiftedFrom : kLnShiftedFrom) && arrays >= 16 && codes >= (size_t)E) {
+    } else if (C >= shifted_from && arrays >= 16 && codes >= (size_t)E) {
         s.shifted = true;
         need = C + E - 1;   // wherever in a vector the row starts
         if (E == 8) {

@@ -220,3 +220,18 @@ def test_what_rows_of_no_type_hold_reaches_nothing_in_a_typed_layer(checkpoint):
     got = step()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert not got[0][:20].any() and not got[1][250:].any() and not any(t.isnan().any() for t in got)
+
+
+def test_rows_whose_squares_leave_float32():
+    """As documented: 1 / sigma is zero and y is beta, from the mean or from the checkpoint alike; other rows are not touched."""
+    from paper_2111_06483_b200 import api
+    for c in (64, 333, 9000):
+        x = torch.randn(5, c, device="cuda")
+        clean, _ = api.ln_forward(x)
+        x[2] *= 1e20
+        beta = torch.randn(c, device="cuda")
+        y, (mean, rstd) = api.ln_forward(x, beta=beta)
+        assert torch.equal(y[2], beta) and rstd[2] == 0 and mean[2].isfinite()
+        assert torch.equal(api.ln_forward(x)[0][[0, 1, 3, 4]], clean[[0, 1, 3, 4]])
+        y8, (ck, rstd8) = api.ln_forward(x, beta=beta, checkpoint=True)
+        assert torch.equal(y8, y) and not ck.scales[2].any() and not ck.codes[2].any()
