@@ -110,3 +110,25 @@ def test_a_replayed_graph_reports_it_to_the_next_call(no_patience):
     with pytest.raises(B.SarError):
         api.typed_linear_forward(h, W, o)
     assert torch.equal(api.typed_linear_forward(h, W, o), want)
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    """The word that tells of waits is set up by the first call, whose host memory a capture must not refuse."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2111_06483_b200 import api
+h = torch.randn(300, 64, device="cuda").bfloat16()
+W = torch.randn(2, 64, 72, device="cuda").bfloat16()
+o = torch.tensor([0, 100, 300], device="cuda")
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    z = api.typed_linear_forward(h, W, o)
+graph.replay()
+torch.cuda.synchronize()
+assert torch.equal(z, api.typed_linear_forward(h, W, o)) and z.any()
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
