@@ -1,7 +1,7 @@
 // Layer normalisation of node rows and its backward pass (contracts in include/sar.h):
 //   xhat = (x - mean) rstd,  y = gamma xhat + beta,  mean and 1/rstd = sqrt(var + eps) taken over a row's C columns;
 //   g = gamma gy,  gx = rstd (g - <g, 1>/C - xhat <g, xhat>/C),  dgamma = sum over the rows of gy xhat,  dbeta = sum of gy.
-// Each pass reads and writes its arrays once and is bound by memory.  A group of G lanes holds a row in registers between its
+// Each pass reads and writes its arrays once and is bound by memory where rows are whole vectors, by instructions otherwise.  A group of G lanes holds a row in registers between its
 // sums and its result, so the variance is the mean of squared deviations (no cancellation) without a second read; the sums
 // over the rows are carried in registers from row to row, then one record per block, which a second launch adds up in a fixed
 // order (no atomics).  With a checkpoint the normalised rows leave the forward pass as 8-bit codes as well, and the backward

@@ -134,10 +134,10 @@ __device__ __forceinline__ float2 ln_splat(float x) { return make_float2(x, x); 
 // arrays are not aligned to that.  Few lanes with many columns each, 16 of bf16 and 8 of float32 where that covers the row,
 // rather than many lanes with few: a warp then has up to 8 rows in hand and joins their sums in 2 to 4 steps instead of 5
 // (a million rows of 256 bf16, forward: 32 lanes of 8 columns 208 us, 16 of 16 171).  Wide rows take 64 lanes and more, up to the
-// block, so that they too stay in registers and are read once (us: 250,000 rows of 1,024 bf16, a warp against 64 lanes, forward with
+// block, so that they too stay in registers and are read once (us, as the choice was made: 250,000 rows of 1,024 bf16, a warp against 64 lanes, forward with
 // the checkpoint 273 / 252, backward from it 292 / 252; float32, forward 326 / 309 with 128 lanes, with the checkpoint 449 / 357;
 // 120,000 rows of 2,048 bf16, a block that reads its row again for every pass against 128 lanes, forward 564 / 171, backward
-// 945 / 260, with the checkpoint 1091 / 239, from it 1261 / 278).
+// 945 / 260, with the checkpoint 1091 / 239, from it 1261 / 278; since the mean is divided, forward with the checkpoint 224 and 215).
 //
 // LnRow: E divides C (or is 1).  Slot v of lane gl holds the columns from (v G + gl) E on, all or none of them.
 template <typename T_, int E_, int G_, int V_>
