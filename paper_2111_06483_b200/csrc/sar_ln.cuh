@@ -476,7 +476,7 @@ constexpr int ln_blocks(bool bwd, bool ck) {
 // result before its rounding is within 2^-22 units of the quotient, and no quotient by C lies that close to the middle of two
 // floats).  The compiler keeps more in registers around the division; what that does to the passes, us, corrected / divided:
 // 60,000 rows of 5,000 308 / 255, with the checkpoint 481 / 390; 1,000,000 of 100 with it 160 / 140; but 120,000 of 2,048
-// (128 lanes) 177 / 196 and 31,000 of 2,047, column by column, 90 / 101.
+// (128 lanes) 177 / 196, 31,000 of 2,047, column by column, 90 / 101, and 562,000 of 16 (one slot a lane) with the checkpoint 31.3 / 32.5.
 template <typename T, bool DIVIDE>
 __device__ __forceinline__ float ln_mean(float sum, const LnArgs &a) {
     if constexpr (sizeof(T) == 2 && DIVIDE) return __fdiv_rn(sum, a.c);
@@ -516,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(false, CK)) ln_fwd_ke
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int q = 0; q < P; ++q) sum = __fadd2_rn(sum, x[v][q]);   // what is no column is zero
-        float mean = ln_mean<T, (Row::E > 1 && (CK || G != 128))>(ln_sum<G>(sum.x + sum.y, red, 0), a);
+        float mean = ln_mean<T, (Row::E > 1 && V > 1 && (CK || G != 128))>(ln_sum<G>(sum.x + sum.y, red, 0), a);
         float2 dev = make_float2(0.f, 0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -526,7 +526,8 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(false, CK)) ln_fwd_ke
 #pragma unroll
             for (int q = 0; q < P; ++q) dev = __ffma2_rn(x[v][q], x[v][q], dev);
         }
-        float var = ln_sum<G>(dev.x + dev.y, red, 1) * a.inv_c;
+        const float var = ln_sum<G>(dev.x + dev.y, red, 1) * a.inv_c;
+        float rstd = __frsqrt_rn(var + a.eps);   // before the vote, which would hold it up (69,288 rows of 136 float32 14.5 us, behind it 16)
         if (sizeof(T) == 4 && __any_sync(0xffffffffu, ln_far(mean, var, a.eps))) {   // the sums need all lanes; a group's lanes agree, and so do its warps
             float2 rest = make_float2(0.f, 0.f);
 #pragma unroll
@@ -535,7 +536,7 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(false, CK)) ln_fwd_ke
                 for (int q = 0; q < P; ++q) rest = __fadd2_rn(rest, x[v][q]);
             const float off = ln_sum<G>(rest.x + rest.y, red, 2) * a.inv_c;
             mean += off;
-            var = ln_variance(var, off);
+            rstd = __frsqrt_rn(ln_variance(var, off) + a.eps);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
 #pragma unroll
@@ -543,7 +544,6 @@ __global__ void __launch_bounds__(kThreads, ln_blocks<Row>(false, CK)) ln_fwd_ke
                 r.clean(v, x[v]);
             }
         }
-        const float rstd = __frsqrt_rn(var + a.eps);
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -910,7 +910,7 @@ struct LnShape {
 #define SAR_LN_4H(X) X(4, 4, 1) X(4, 4, 2) X(4, 4, 4) X(4, 8, 3) X(4, 8, 4) X(4, 16, 3) X(4, 16, 4) X(4, 32, 3) X(4, 32, 4) X(4, 64, 3) X(4, 64, 4) X(4, 128, 4) X(4, 256, 4) X(4, 256, 8)
 #define SAR_LN_8S(X) X(8, 16, 2) X(8, 32, 2) X(8, 32, 3) X(8, 32, 4)
 #define SAR_LN_4S(X) X(4, 32, 2) X(4, 32, 3) X(4, 32, 4) X(4, 32, 6)
-// ... and narrow shifted rows, for what reads checkpoints or only packs
+// ... and narrow shifted rows, for what reads checkpoints
 #define SAR_LN_8N(X) X(8, 4, 1) X(8, 4, 2) X(8, 8, 2)
 #define SAR_LN_4N(X) X(4, 8, 1) X(4, 8, 2) X(4, 16, 2)
 #define SAR_LN_1(X) X(1, 4, 1) X(1, 4, 4) X(1, 4, 8) X(1, 8, 6) X(1, 8, 8) X(1, 16, 6) X(1, 16, 8) X(1, 32, 8) X(1, 256, 4) X(1, 256, 8)
